@@ -21,6 +21,7 @@
  *   - Calls on one context are not thread-safe; use one context per host thread.
  *   - Every call is synchronous with respect to the host: when it returns, its
  *     results are in the caller's buffers.  Device work runs on the context's stream.
+ *     (The calls on token caches queue their work and return: see there.)
  *   - Pointers documented as "host" must be host memory; "device" ones must be memory
  *     of the context's device.  The caller keeps ownership of everything it passes.
  */
@@ -377,6 +378,123 @@ mure_status mure_expand_patches(mure_model *model, const mure_mutant *table, int
 mure_status mure_expand_patches_noalloc(mure_model *model, const mure_mutant *table, int64_t n_mutants,
                                         const int32_t *neuron_pool, int64_t pool_len, float *out_dev,
                                         int64_t out_len, int64_t *offsets);
+
+/* ------------------------------------------------------------------ token caches --
+ *
+ * For networks that attend over a sequence, what the layers before a mutation computed
+ * of the earlier tokens is the keys and values of each attention layer: the memo table
+ * (Algorithm 3) of a sequence model.  A token cache holds them for one attention layer
+ * in pages of page_size cells (a cell: one token's key and value, all n_kv_heads of
+ * them), and sequences name their pages in a table, so that the sequences of any number
+ * of mutants share the original's pages.  The paper has no counterpart of the paging.
+ *
+ * These calls queue their work on the context's stream and return without waiting for
+ * it, so that a layer's calls follow each other without a gap; mure_synchronize waits
+ * and reports what went wrong on the device.  All arguments are checked on the host
+ * before anything is queued: lengths and page tables are host arrays, given once per
+ * batch in a plan that every layer's calls then share.
+ *
+ * Pools, one for keys and one for values: [n_pages][n_kv_heads][page_size][head_dim].
+ * form MURE_FORM_SAME stores the values as they are.  MURE_FORM_E4M3 stores 8-bit codes
+ * (fn_e4m3: 4 exponent and 3 mantissa bits, no infinities) and a byte per token and
+ * head, [n_pages][n_kv_heads][page_size], whose scale is 2^(byte - 127): the least power
+ * of two, from 2^-127 up, that brings the row's largest magnitude to 448 or less.
+ * Scaling by it is exact, so a value is rounded once, to the nearest code, ties to even.
+ * A row with an infinity or a NaN gets byte 255, and all of it reads as NaN. */
+enum { MURE_F32 = 0, MURE_F16 = 1, MURE_BF16 = 2 };       /* types of activations */
+enum { MURE_FORM_SAME = 0, MURE_FORM_E4M3 = 1 };          /* forms of cells */
+
+typedef struct {
+    int32_t n_kv_heads;   /* 1..1024 */
+    int32_t head_dim;     /* a multiple of 8, 8..256 */
+    int32_t page_size;    /* cells per page: a power of two, 8..1024 */
+    int32_t dtype;        /* MURE_F32, MURE_F16 or MURE_BF16: keys, values, queries, outputs */
+    int32_t form;         /* MURE_FORM_* */
+    int32_t reserved;     /* 0 */
+    int64_t n_pages;      /* 1..2^31 - 1 */
+    /* device pools of the caller, 16-byte aligned, or all NULL: the library allocates them
+       and fills them with zeros.  The scales are NULL unless form is MURE_FORM_E4M3.
+       Cells that no sequence holds may have any content; a NaN among them costs time (rows
+       of a tile that holds one are computed again without the tensor cores) */
+    void *k, *v;
+    uint8_t *k_scale, *v_scale;
+} mure_tokens_desc;
+
+/* One batch: sequence b has kv_len[b] cells, in the pages page_table[b * table_stride ..],
+ * and new_len[b] new tokens at positions pos[b] .. pos[b] + new_len[b] - 1.  A new token
+ * at position p attends to the cells j < kv_len[b] with j <= p and, where window > 0,
+ * with j > p - window or j < sinks.  (pos[b] + new_len[b] <= kv_len[b] where the new
+ * tokens' own cells are among them.) */
+typedef struct {
+    int32_t n_seqs;                     /* 0..65,535 */
+    int32_t n_heads;                    /* query heads, a multiple of n_kv_heads: query head h
+                                           reads cached head h / (n_heads / n_kv_heads) */
+    const int32_t *new_len, *pos, *kv_len;   /* host [n_seqs], >= 0 */
+    const int32_t *page_table;          /* host [n_seqs][table_stride]; entries past a
+                                           sequence's last cell are not read */
+    int64_t table_stride;
+    int32_t window, sinks;              /* 0 0: causal over all cells */
+    float scale;                        /* factor of the scores; 0: head_dim^-1/2 */
+    int32_t reserved;                   /* 0 */
+} mure_tokens_batch;
+
+typedef struct mure_tokens mure_tokens;
+typedef struct mure_tokens_plan mure_tokens_plan;
+
+/* Create a cache.  Errors: INVALID_ARG (a size out of range, pools or scales given in
+ * part, unaligned pools), UNSUPPORTED (unknown dtype or form), OOM, CUDA. */
+mure_status mure_tokens_create(mure_ctx *ctx, const mure_tokens_desc *desc, mure_tokens **out);
+/* Frees what the library allocated (after the work queued on it). */
+void mure_tokens_free(mure_tokens *tokens);
+/* The cache's description with its pools' addresses. */
+mure_status mure_tokens_buffers(const mure_tokens *tokens, mure_tokens_desc *out);
+
+/* Check a batch, lay out its work and copy its tables to the device.  The plan serves
+ * every cache of the context with `tokens`' geometry (heads, head_dim, page_size, dtype,
+ * form, n_pages), not that one alone.  mure_tokens_plan_set gives an existing plan a new
+ * batch (the next step of the same sequences, say) and keeps its device memory; when it
+ * fails the plan is left without a batch.  Errors: INVALID_ARG (a NULL array, a negative
+ * length, positions past 2^30, a page id out of range, head counts that do not divide,
+ * a scale or window that is not usable), UNSUPPORTED (more rows or heads than the kernels
+ * index), OOM, CUDA. */
+mure_status mure_tokens_plan_create(mure_tokens *tokens, const mure_tokens_batch *batch, mure_tokens_plan **out);
+mure_status mure_tokens_plan_set(mure_tokens_plan *plan, const mure_tokens_batch *batch);
+void mure_tokens_plan_free(mure_tokens_plan *plan);
+
+/* Rows of activations: element (token, head, i) of a batch's packed tokens (the new
+ * tokens of sequence 0, then those of sequence 1, ...) is at
+ * p[token * token_stride + head * head_stride + i].  Strides count elements; rows need no
+ * more than their type's alignment (16-byte aligned rows are copied faster). */
+typedef struct {
+    void *p;                            /* device; may be NULL where the batch has no such rows */
+    int64_t token_stride, head_stride;
+} mure_tokens_rows;
+
+/* Write the batch's new tokens' keys and values (cached heads) into their cells.  The
+ * inputs are read only.  Errors: INVALID_ARG (plan and cache do not fit, a NULL or
+ * misaligned pointer, a sequence whose new tokens end past kv_len, two sequences that
+ * write to one cell), CUDA. */
+mure_status mure_tokens_append(mure_tokens *tokens, mure_tokens_plan *plan, const mure_tokens_rows *k,
+                               const mure_tokens_rows *v);
+/* Gather cells into dense rows: part 0 all cells of every sequence in order (kv_len[b]
+ * rows each), part 1 the cells of the new tokens (as appended).  Values that their type
+ * does not hold are rounded to it.  Errors as for mure_tokens_append. */
+mure_status mure_tokens_read(mure_tokens *tokens, mure_tokens_plan *plan, int32_t part, const mure_tokens_rows *k,
+                             const mure_tokens_rows *v);
+/* out = softmax(scale q k^T) v for the batch's new tokens (n_heads heads of q and out)
+ * over the cells each may attend to, sums held in fp32; a token that may attend to none
+ * gets zeros.  lse (nullable, device fp32 [tokens][n_heads], dense): log of the sum of
+ * exp(scale q k), -inf where there are no cells.  16-bit types: the probabilities are
+ * rounded to 16 bits before their product with v.  fp32: products and sums have fp32
+ * accuracy.  Cells that a token may not attend to never reach its output, whatever they
+ * hold.  Equal calls give equal bits.  Errors: INVALID_ARG (as above), CUDA. */
+mure_status mure_tokens_attend(mure_tokens *tokens, mure_tokens_plan *plan, const mure_tokens_rows *q,
+                               const mure_tokens_rows *out, float *lse);
+
+/* Wait for everything queued on the context's stream.  Errors: TIMEOUT (a device-side
+ * wait of a token call gave up; the outputs of the token calls since the last
+ * synchronisation are undefined, the context stays usable), CUDA. */
+mure_status mure_synchronize(mure_ctx *ctx);
 
 #ifdef __cplusplus
 }

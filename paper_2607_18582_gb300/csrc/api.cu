@@ -9,6 +9,7 @@
 
 #include "common.cuh"
 #include "device_util.cuh"
+#include "host.cuh"
 
 using namespace mure;
 
@@ -38,59 +39,6 @@ std::string tc_conv_env()
 }
 
 // ------------------------------------------------------------------ plumbing --
-
-struct Fail {
-    mure_status st;
-};
-
-void set_err(mure_ctx *c, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
-void set_err(mure_ctx *c, const char *fmt, ...)
-{
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    if (c) c->err = buf;
-}
-
-#define FAILIF(cond, ctx, status, ...)        \
-    do {                                      \
-        if (cond) {                           \
-            set_err(ctx, __VA_ARGS__);        \
-            throw Fail{status};               \
-        }                                     \
-    } while (0)
-
-#define CK(ctx, call)                                                                              \
-    do {                                                                                           \
-        cudaError_t e_ = (call);                                                                   \
-        FAILIF(e_ != cudaSuccess, ctx, MURE_ERR_CUDA, "%s: %s", #call, cudaGetErrorString(e_));    \
-    } while (0)
-
-void *dalloc(mure_ctx *c, size_t bytes)
-{
-    if (bytes == 0) bytes = 16;
-    void *p = nullptr;
-    if (c->has_alloc) {
-        p = c->alloc.alloc(bytes, (void *)c->stream, c->alloc.user);
-    } else {
-        if (cudaMallocAsync(&p, bytes, c->stream) != cudaSuccess) {
-            cudaGetLastError();
-            p = nullptr;
-        }
-    }
-    FAILIF(!p, c, MURE_ERR_OOM, "device allocation of %zu bytes failed", bytes);
-    return p;
-}
-
-void dfree(mure_ctx *c, const void *cp)
-{
-    void *p = const_cast<void *>(cp);
-    if (!p) return;
-    if (c->has_alloc) c->alloc.free(p, (void *)c->stream, c->alloc.user);
-    else cudaFreeAsync(p, c->stream);
-}
 
 // Device allocations owned by one call (freed on every exit path).  Small ones share blocks of
 // kBlock bytes: an allocation through a caller's allocator costs microseconds of host time, and
@@ -162,27 +110,6 @@ struct Results {
         used = 0;
     }
 };
-
-template <class F>
-mure_status run(mure_ctx *c, F &&fn)
-{
-    if (c) c->err.clear();
-    try {
-        fn();
-    } catch (const Fail &f) {
-        return f.st;
-    } catch (const std::bad_alloc &) {
-        set_err(c, "host allocation failed");
-        return MURE_ERR_OOM;
-    }
-    return MURE_OK;
-}
-
-void check_launch(mure_ctx *c)
-{
-    cudaError_t e = cudaGetLastError();
-    FAILIF(e != cudaSuccess, c, MURE_ERR_CUDA, "kernel launch: %s", cudaGetErrorString(e));
-}
 
 // Optional per-launch device timing: a pair of events around each launch, summed
 // per class (a layer's kernels, delta, gather, epilogue) once the stream is idle.

@@ -1,0 +1,392 @@
+// Token caches: the C entry points, and the host's layout of a batch's work.
+//
+// Lengths and page tables are host arrays, as the mutant tables are.  So every check runs before
+// anything is queued, no kernel can meet a page or a length out of range, and the work can be
+// laid out knowing every sequence's length.  A plan holds a batch's tables on the device; all
+// layers' calls of a step share it.
+#include <algorithm>
+#include <cmath>
+#include <cstdlib>
+#include <cstring>
+#include <memory>
+
+#include "host.cuh"
+#include "tokens.cuh"
+
+using namespace mure;
+
+struct mure_tokens {
+    mure_ctx *ctx = nullptr;
+    mure_tokens_desc d{};
+    void *own = nullptr;      // the library's allocation of the pools (null: the caller's pools)
+};
+
+struct mure_tokens_plan {
+    mure_ctx *ctx = nullptr;
+    mure_tokens_desc d{};     // the geometry it serves (pools ignored)
+    bool ready = false;
+    TokBatch b;
+    int64_t n_new = 0, n_cells = 0;          // packed rows of the new tokens / of all cells
+    int64_t tiles_new = 0, tiles_all = 0;
+    int new_past_end = -1;                   // a sequence whose new tokens end past its cells
+    std::string append_fault;                // why the batch's new tokens cannot be written ("" if they can)
+    void *mem = nullptr;
+    size_t mem_bytes = 0;
+};
+
+namespace {
+
+constexpr int64_t kMostPos = int64_t(1) << 30;
+
+int elt_bytes(int dtype) { return dtype == MURE_F32 ? 4 : 2; }
+
+int log2_of(int n)
+{
+    int l = 0;
+    while ((1 << l) < n) ++l;
+    return l;
+}
+
+void check_geometry(mure_ctx *c, const mure_tokens_desc &d)
+{
+    FAILIF(d.dtype != MURE_F32 && d.dtype != MURE_F16 && d.dtype != MURE_BF16, c, MURE_ERR_UNSUPPORTED, "unknown dtype %d",
+           d.dtype);
+    FAILIF(d.form != MURE_FORM_SAME && d.form != MURE_FORM_E4M3, c, MURE_ERR_UNSUPPORTED, "unknown form %d", d.form);
+    FAILIF(d.n_kv_heads < 1 || d.n_kv_heads > 1024, c, MURE_ERR_INVALID_ARG, "n_kv_heads %d not in 1..1024", d.n_kv_heads);
+    FAILIF(d.head_dim < 8 || d.head_dim > 256 || d.head_dim % 8, c, MURE_ERR_INVALID_ARG,
+           "head_dim %d is not a multiple of 8 in 8..256", d.head_dim);
+    FAILIF(d.page_size < 8 || d.page_size > 1024 || (d.page_size & (d.page_size - 1)), c, MURE_ERR_INVALID_ARG,
+           "page_size %d is not a power of two in 8..1024", d.page_size);
+    FAILIF(d.n_pages < 1 || d.n_pages > INT32_MAX, c, MURE_ERR_INVALID_ARG, "n_pages %lld not in 1..2^31 - 1",
+           (long long)d.n_pages);
+    FAILIF(d.reserved != 0, c, MURE_ERR_INVALID_ARG, "reserved fields must be 0");
+}
+
+TokPool pool_of(const mure_tokens *t)
+{
+    TokPool p;
+    p.k = t->d.k; p.v = t->d.v; p.ks = t->d.k_scale; p.vs = t->d.v_scale;
+    p.hk = t->d.n_kv_heads; p.d = t->d.head_dim; p.page_log2 = log2_of(t->d.page_size);
+    return p;
+}
+
+// The packed device image of a plan's tables: parts at 16-byte boundaries of one host buffer.
+struct Image {
+    std::vector<char> bytes;
+    template <class T>
+    size_t add(const std::vector<T> &v)
+    {
+        const size_t at = (bytes.size() + 15) / 16 * 16;
+        bytes.resize(at + std::max<size_t>(v.size() * sizeof(T), 16));
+        if (!v.empty()) memcpy(bytes.data() + at, v.data(), v.size() * sizeof(T));
+        return at;
+    }
+};
+
+void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
+{
+    mure_ctx *c = p->ctx;
+    p->ready = false;
+    FAILIF(!bp, c, MURE_ERR_INVALID_ARG, "NULL batch");
+    const mure_tokens_batch &b = *bp;
+    const mure_tokens_desc &d = p->d;
+    FAILIF(b.reserved != 0, c, MURE_ERR_INVALID_ARG, "reserved fields must be 0");
+    FAILIF(b.n_seqs < 0 || b.n_seqs > 65535, c, MURE_ERR_INVALID_ARG, "n_seqs %d not in 0..65535", b.n_seqs);
+    FAILIF(b.n_heads < 1 || b.n_heads % d.n_kv_heads != 0, c, MURE_ERR_INVALID_ARG,
+           "n_heads %d is not a positive multiple of n_kv_heads %d", b.n_heads, d.n_kv_heads);
+    FAILIF(b.n_heads > 65536, c, MURE_ERR_UNSUPPORTED, "more than 65,536 query heads");
+    FAILIF(b.n_seqs > 0 && (!b.new_len || !b.pos || !b.kv_len), c, MURE_ERR_INVALID_ARG, "NULL lengths");
+    FAILIF(b.window < 0 || b.sinks < 0, c, MURE_ERR_INVALID_ARG, "negative window or sinks");
+    FAILIF(b.window == 0 && b.sinks != 0, c, MURE_ERR_INVALID_ARG, "sinks without a window");
+    FAILIF(!(b.scale >= 0.f) || std::isinf(b.scale), c, MURE_ERR_INVALID_ARG, "scale must be finite and not negative");
+
+    const int page_log2 = log2_of(d.page_size), n = b.n_seqs;
+    std::vector<TokSeq> seq(n);
+    std::vector<int32_t> tile_new(n + 1, 0), tile_all(n + 1, 0), table;
+    int64_t n_new = 0, n_cells = 0, t_new = 0, t_all = 0;
+    struct Span {
+        int64_t page;
+        int first, last;   // slots
+    };
+    std::vector<Span> written;
+    std::string fault;
+    int past_end = -1;
+    for (int s = 0; s < n; ++s) {
+        const int64_t nn = b.new_len[s], pos = b.pos[s], kv = b.kv_len[s];
+        FAILIF(nn < 0 || pos < 0 || kv < 0, c, MURE_ERR_INVALID_ARG, "sequence %d: a negative length or position", s);
+        FAILIF(pos + nn > kMostPos || kv > kMostPos, c, MURE_ERR_INVALID_ARG, "sequence %d: positions past 2^30", s);
+        const int64_t pages = (kv + d.page_size - 1) >> page_log2;
+        FAILIF(pages > 0 && (!b.page_table || b.table_stride < pages), c, MURE_ERR_INVALID_ARG,
+               "sequence %d: %lld pages, a table of %lld", s, (long long)pages, (long long)(b.page_table ? b.table_stride : 0));
+        const int32_t *ids = b.page_table + (b.page_table ? s * b.table_stride : 0);
+        for (int64_t i = 0; i < pages; ++i)
+            FAILIF(ids[i] < 0 || ids[i] >= d.n_pages, c, MURE_ERR_INVALID_ARG, "sequence %d: page %d not in 0..%lld", s, ids[i],
+                   (long long)d.n_pages - 1);
+        seq[s] = {(int32_t)n_new, (int32_t)nn, (int32_t)pos, (int32_t)kv, (int64_t)table.size(), n_cells};
+        table.insert(table.end(), ids, ids + pages);
+        n_new += nn;
+        n_cells += kv;
+        t_new += (nn + kTokTileNew - 1) / kTokTileNew;
+        t_all += (kv + kTokTileAll - 1) / kTokTileAll;
+        FAILIF(n_new > INT32_MAX || t_all > INT32_MAX, c, MURE_ERR_UNSUPPORTED, "more than 2^31 - 1 new tokens or tiles of cells");
+        tile_new[s + 1] = (int32_t)t_new;
+        tile_all[s + 1] = (int32_t)t_all;
+        if (nn > 0 && pos + nn > kv) {
+            if (past_end < 0) past_end = s;
+            if (fault.empty())
+                fault = "sequence " + std::to_string(s) + ": new tokens end at " + std::to_string(pos + nn) + ", past its " +
+                        std::to_string(kv) + " cells";
+            continue;
+        }
+        for (int64_t q = pos; q < pos + nn;) {
+            const int64_t stop = std::min(pos + nn, ((q >> page_log2) + 1) << page_log2);
+            const int first = (int)(q & (d.page_size - 1));
+            written.push_back({ids[q >> page_log2], first, first + (int)(stop - q) - 1});
+            q = stop;
+        }
+    }
+    // two sequences may share a page that is written only where they write different cells of it
+    std::sort(written.begin(), written.end(),
+              [](const Span &x, const Span &y) { return x.page != y.page ? x.page < y.page : x.first < y.first; });
+    for (size_t i = 1; i < written.size() && fault.empty(); ++i)
+        if (written[i].page == written[i - 1].page && written[i].first <= written[i - 1].last)
+            fault = "two new tokens have the cell " + std::to_string(written[i].first) + " of page " +
+                    std::to_string(written[i].page);
+
+    Image im;
+    const size_t o_seq = im.add(seq), o_table = im.add(table), o_new = im.add(tile_new), o_all = im.add(tile_all);
+    if (im.bytes.size() > p->mem_bytes) {
+        dfree(c, p->mem);
+        p->mem = nullptr;
+        p->mem_bytes = 0;
+        const size_t room = im.bytes.size() + im.bytes.size() / 4;   // the next steps' tables grow
+        p->mem = dalloc(c, room);
+        p->mem_bytes = room;
+    }
+    // (from pageable memory: the call has taken its copy when it returns)
+    CK(c, cudaMemcpyAsync(p->mem, im.bytes.data(), im.bytes.size(), cudaMemcpyHostToDevice, c->stream));
+    char *m = static_cast<char *>(p->mem);
+    TokBatch &v = p->b;
+    v.seq = reinterpret_cast<TokSeq *>(m + o_seq);
+    v.table = reinterpret_cast<int32_t *>(m + o_table);
+    v.tile_new = reinterpret_cast<int32_t *>(m + o_new);
+    v.tile_all = reinterpret_cast<int32_t *>(m + o_all);
+    v.n_seqs = n;
+    v.n_heads = b.n_heads;
+    v.group = b.n_heads / d.n_kv_heads;
+    v.window = b.window;
+    v.sinks = b.sinks;
+    v.scale_log2 = (float)((b.scale > 0.f ? (double)b.scale : 1.0 / std::sqrt((double)d.head_dim)) * 1.4426950408889634);
+    p->n_new = n_new;
+    p->n_cells = n_cells;
+    p->tiles_new = t_new;
+    p->tiles_all = t_all;
+    p->new_past_end = past_end;
+    p->append_fault = fault;
+    p->ready = true;
+}
+
+// A call's cache and plan.
+void check_pair(mure_ctx *c, const mure_tokens *t, const mure_tokens_plan *p)
+{
+    FAILIF(!p, c, MURE_ERR_INVALID_ARG, "NULL plan");
+    FAILIF(p->ctx != c, c, MURE_ERR_INVALID_ARG, "cache and plan belong to different contexts");
+    FAILIF(!p->ready, c, MURE_ERR_INVALID_ARG, "the plan holds no batch");
+    const mure_tokens_desc &a = t->d, &b = p->d;
+    FAILIF(a.n_kv_heads != b.n_kv_heads || a.head_dim != b.head_dim || a.page_size != b.page_size || a.dtype != b.dtype ||
+               a.form != b.form || a.n_pages != b.n_pages,
+           c, MURE_ERR_INVALID_ARG, "the plan was made for caches of another geometry");
+}
+
+TokRows check_rows(mure_ctx *c, const mure_tokens_rows *r, const mure_tokens_desc &d, int64_t rows, int heads, const char *name)
+{
+    TokRows o;
+    if (rows == 0) return o;
+    const int e = elt_bytes(d.dtype);
+    FAILIF(!r || !r->p, c, MURE_ERR_INVALID_ARG, "NULL %s", name);
+    FAILIF((uintptr_t)r->p % e != 0, c, MURE_ERR_INVALID_ARG, "%s is not aligned to its type", name);
+    o.p = static_cast<char *>(r->p);
+    o.ts = r->token_stride;
+    o.hs = r->head_stride;
+    const int per = 16 / e;
+    o.vec = (uintptr_t)r->p % 16 == 0 && (rows == 1 || o.ts % per == 0) && (heads == 1 || o.hs % per == 0);
+    return o;
+}
+
+// Rows that are written must not lie on one another.
+void check_apart(mure_ctx *c, const TokRows &r, const mure_tokens_desc &d, int64_t rows, int heads, const char *name)
+{
+    if (rows == 0) return;
+    const int64_t ts = std::llabs(r.ts), hs = std::llabs(r.hs), D = d.head_dim;
+    const bool ok = (heads == 1 || rows == 1) ? (heads == 1 || hs >= D) && (rows == 1 || ts >= D)
+                                              : (hs >= D && ts >= hs * (heads - 1) + D) || (ts >= D && hs >= ts * (rows - 1) + D);
+    FAILIF(!ok, c, MURE_ERR_INVALID_ARG, "rows of %s overlap", name);
+}
+
+}  // namespace
+
+extern "C" {
+
+mure_status mure_tokens_create(mure_ctx *c, const mure_tokens_desc *desc, mure_tokens **out)
+{
+    if (!c) return MURE_ERR_INVALID_ARG;
+    return run(c, [&] {
+        FAILIF(!out, c, MURE_ERR_INVALID_ARG, "NULL out");
+        *out = nullptr;
+        FAILIF(!desc, c, MURE_ERR_INVALID_ARG, "NULL description");
+        const mure_tokens_desc &d = *desc;
+        check_geometry(c, d);
+        const bool q = d.form == MURE_FORM_E4M3, any = d.k || d.v || d.k_scale || d.v_scale;
+        FAILIF(any && (!d.k || !d.v || (q && (!d.k_scale || !d.v_scale))), c, MURE_ERR_INVALID_ARG,
+               "some of the pools are NULL");
+        FAILIF(!q && (d.k_scale || d.v_scale), c, MURE_ERR_INVALID_ARG, "scales without MURE_FORM_E4M3");
+        FAILIF((uintptr_t)d.k % 16 || (uintptr_t)d.v % 16, c, MURE_ERR_INVALID_ARG, "pools are not 16-byte aligned");
+        CK(c, cudaSetDevice(c->device));
+        auto t = std::make_unique<mure_tokens>();
+        t->ctx = c;
+        t->d = d;
+        if (!any) {
+            const int64_t rows = d.n_pages * d.n_kv_heads * d.page_size;
+            const int64_t pool = (rows * d.head_dim * (q ? 1 : elt_bytes(d.dtype)) + 255) / 256 * 256;
+            const int64_t scales = q ? (rows + 255) / 256 * 256 : 0;
+            char *m = static_cast<char *>(dalloc(c, 2 * (pool + scales)));
+            t->own = m;
+            t->d.k = m;
+            t->d.v = m + pool;
+            t->d.k_scale = q ? reinterpret_cast<uint8_t *>(m + 2 * pool) : nullptr;
+            t->d.v_scale = q ? t->d.k_scale + scales : nullptr;
+            const cudaError_t e = cudaMemsetAsync(m, 0, 2 * (pool + scales), c->stream);
+            if (e != cudaSuccess) dfree(c, m);
+            CK(c, e);
+        }
+        *out = t.release();
+    });
+}
+
+void mure_tokens_free(mure_tokens *t)
+{
+    if (!t) return;
+    if (t->own) {
+        cudaStreamSynchronize(t->ctx->stream);
+        dfree(t->ctx, t->own);
+    }
+    delete t;
+}
+
+mure_status mure_tokens_buffers(const mure_tokens *t, mure_tokens_desc *out)
+{
+    if (!t || !out) return MURE_ERR_INVALID_ARG;
+    *out = t->d;
+    return MURE_OK;
+}
+
+mure_status mure_tokens_plan_create(mure_tokens *t, const mure_tokens_batch *batch, mure_tokens_plan **out)
+{
+    if (!t) return MURE_ERR_INVALID_ARG;
+    mure_ctx *c = t->ctx;
+    return run(c, [&] {
+        FAILIF(!out, c, MURE_ERR_INVALID_ARG, "NULL out");
+        *out = nullptr;
+        CK(c, cudaSetDevice(c->device));
+        auto p = std::make_unique<mure_tokens_plan>();
+        p->ctx = c;
+        p->d = t->d;
+        try {
+            set_plan(p.get(), batch);
+        } catch (...) {
+            dfree(c, p->mem);
+            throw;
+        }
+        *out = p.release();
+    });
+}
+
+mure_status mure_tokens_plan_set(mure_tokens_plan *p, const mure_tokens_batch *batch)
+{
+    if (!p) return MURE_ERR_INVALID_ARG;
+    return run(p->ctx, [&] {
+        p->ready = false;
+        CK(p->ctx, cudaSetDevice(p->ctx->device));
+        set_plan(p, batch);
+    });
+}
+
+void mure_tokens_plan_free(mure_tokens_plan *p)
+{
+    if (!p) return;
+    dfree(p->ctx, p->mem);
+    delete p;
+}
+
+mure_status mure_tokens_append(mure_tokens *t, mure_tokens_plan *p, const mure_tokens_rows *k, const mure_tokens_rows *v)
+{
+    if (!t) return MURE_ERR_INVALID_ARG;
+    mure_ctx *c = t->ctx;
+    return run(c, [&] {
+        check_pair(c, t, p);
+        FAILIF(!p->append_fault.empty(), c, MURE_ERR_INVALID_ARG, "%s", p->append_fault.c_str());
+        const TokRows kr = check_rows(c, k, t->d, p->n_new, t->d.n_kv_heads, "k");
+        const TokRows vr = check_rows(c, v, t->d, p->n_new, t->d.n_kv_heads, "v");
+        CK(c, cudaSetDevice(c->device));
+        c->launches += launch_tokens_append(pool_of(t), p->b, t->d.dtype, t->d.form, kr, vr, p->tiles_new, c->stream);
+        check_launch(c);
+    });
+}
+
+mure_status mure_tokens_read(mure_tokens *t, mure_tokens_plan *p, int32_t part, const mure_tokens_rows *k,
+                             const mure_tokens_rows *v)
+{
+    if (!t) return MURE_ERR_INVALID_ARG;
+    mure_ctx *c = t->ctx;
+    return run(c, [&] {
+        check_pair(c, t, p);
+        FAILIF(part != 0 && part != 1, c, MURE_ERR_INVALID_ARG, "part must be 0 or 1");
+        // (the cells of new tokens past the cells held do not exist; shared ones may be read twice)
+        FAILIF(part == 1 && p->new_past_end >= 0, c, MURE_ERR_INVALID_ARG, "sequence %d: new tokens end past its cells",
+               p->new_past_end);
+        const int64_t rows = part ? p->n_new : p->n_cells;
+        const TokRows kr = check_rows(c, k, t->d, rows, t->d.n_kv_heads, "k");
+        const TokRows vr = check_rows(c, v, t->d, rows, t->d.n_kv_heads, "v");
+        check_apart(c, kr, t->d, rows, t->d.n_kv_heads, "k");
+        check_apart(c, vr, t->d, rows, t->d.n_kv_heads, "v");
+        CK(c, cudaSetDevice(c->device));
+        c->launches += launch_tokens_read(pool_of(t), p->b, t->d.dtype, t->d.form, part, kr, vr,
+                                          part ? p->tiles_new : p->tiles_all, c->stream);
+        check_launch(c);
+    });
+}
+
+mure_status mure_tokens_attend(mure_tokens *t, mure_tokens_plan *p, const mure_tokens_rows *q, const mure_tokens_rows *out,
+                               float *lse)
+{
+    if (!t) return MURE_ERR_INVALID_ARG;
+    mure_ctx *c = t->ctx;
+    return run(c, [&] {
+        check_pair(c, t, p);
+        const TokRows qr = check_rows(c, q, t->d, p->n_new, p->b.n_heads, "q");
+        const TokRows orow = check_rows(c, out, t->d, p->n_new, p->b.n_heads, "out");
+        check_apart(c, orow, t->d, p->n_new, p->b.n_heads, "out");
+        FAILIF((uintptr_t)lse % 4 != 0, c, MURE_ERR_INVALID_ARG, "lse is not aligned");
+        CK(c, cudaSetDevice(c->device));
+        c->launches += launch_tokens_attend_rows(pool_of(t), p->b, t->d.dtype, t->d.form, p->n_new, qr, orow, lse, c->stream);
+        check_launch(c);
+    });
+}
+
+mure_status mure_synchronize(mure_ctx *c)
+{
+    if (!c) return MURE_ERR_INVALID_ARG;
+    return run(c, [&] {
+        CK(c, cudaSetDevice(c->device));
+        int dev_err = 0;
+        CK(c, cudaMemcpyAsync(&dev_err, c->err_dev, sizeof(int), cudaMemcpyDeviceToHost, c->stream));
+        CK(c, cudaStreamSynchronize(c->stream));
+        if (dev_err) {
+            CK(c, cudaMemsetAsync(c->err_dev, 0, sizeof(int), c->stream));
+            FAILIF(true, c, dev_err == MURE_ERR_TIMEOUT ? MURE_ERR_TIMEOUT : MURE_ERR_UNSUPPORTED,
+                   "a device-side check failed (code %d)", dev_err);
+        }
+    });
+}
+
+}  // extern "C"

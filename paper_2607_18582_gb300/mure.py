@@ -22,12 +22,16 @@ KINDS = {"conv": 0, "dense": 1, "maxpool": 2, "flatten": 3, "add": 4, "gap": 5, 
          "embed": 8, "lstm": 9}
 ACTS = {"none": 0, "relu": 1, "relu6": 2}
 PRECISIONS = {"fp32": 0, "tf32x3": 1, "bf16": 2, "tf32": 3}
+TOKEN_DTYPES = {"f32": 0, "f16": 1, "bf16": 2}
+TOKEN_FORMS = {"same": 0, "e4m3": 1}
 
 # the exported entry points of include/mure.h
 EXPORTS = ("mure_create", "mure_destroy", "mure_last_error", "mure_model_load", "mure_model_free",
            "mure_model_n_layers", "mure_model_layer_kernel", "mure_kernel_launches", "mure_build_prefix_cache", "mure_cache_free", "mure_cache_outputs",
            "mure_eval_mutants", "mure_eval_vanilla", "mure_expand_patches", "mure_expand_patches_noalloc",
-           "mure_check_descriptors", "mure_set_wait_limit")
+           "mure_check_descriptors", "mure_set_wait_limit", "mure_tokens_create", "mure_tokens_free",
+           "mure_tokens_buffers", "mure_tokens_plan_create", "mure_tokens_plan_set", "mure_tokens_plan_free",
+           "mure_tokens_append", "mure_tokens_read", "mure_tokens_attend", "mure_synchronize")
 
 
 class MureError(RuntimeError):
@@ -81,6 +85,22 @@ class _Stats(C.Structure):
         return out
 
 
+class _TokensDesc(C.Structure):
+    _fields_ = [("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32), ("dtype", C.c_int32),
+                ("form", C.c_int32), ("reserved", C.c_int32), ("n_pages", C.c_int64), ("k", C.c_void_p),
+                ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class _TokensBatch(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_heads", C.c_int32), ("new_len", C.c_void_p), ("pos", C.c_void_p),
+                ("kv_len", C.c_void_p), ("page_table", C.c_void_p), ("table_stride", C.c_int64), ("window", C.c_int32),
+                ("sinks", C.c_int32), ("scale", C.c_float), ("reserved", C.c_int32)]
+
+
+class _TokensRows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
 _lib = None
 # Allocator thunks stay alive for the life of the process: a context's C object may
 # still call them while Python tears objects down in arbitrary (cyclic-GC) order.
@@ -125,9 +145,23 @@ def lib():
         L.mure_expand_patches_noalloc.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp]
         L.mure_check_descriptors.argtypes = [C.POINTER(_ModelDesc), vp, i64, vp, i64, C.c_char_p, C.c_size_t]
         L.mure_set_wait_limit.argtypes = [vp, i64]
+        rows = C.POINTER(_TokensRows)
+        L.mure_tokens_create.argtypes = [vp, C.POINTER(_TokensDesc), C.POINTER(vp)]
+        L.mure_tokens_free.argtypes = [vp]
+        L.mure_tokens_free.restype = None
+        L.mure_tokens_buffers.argtypes = [vp, C.POINTER(_TokensDesc)]
+        L.mure_tokens_plan_create.argtypes = [vp, C.POINTER(_TokensBatch), C.POINTER(vp)]
+        L.mure_tokens_plan_set.argtypes = [vp, C.POINTER(_TokensBatch)]
+        L.mure_tokens_plan_free.argtypes = [vp]
+        L.mure_tokens_plan_free.restype = None
+        L.mure_tokens_append.argtypes = [vp, vp, rows, rows]
+        L.mure_tokens_read.argtypes = [vp, vp, i32, rows, rows]
+        L.mure_tokens_attend.argtypes = [vp, vp, rows, rows, vp]
+        L.mure_synchronize.argtypes = [vp]
         for name in EXPORTS:
             if name not in ("mure_destroy", "mure_model_free", "mure_cache_free", "mure_last_error",
-                            "mure_model_n_layers", "mure_kernel_launches"):
+                            "mure_model_n_layers", "mure_kernel_launches", "mure_tokens_free",
+                            "mure_tokens_plan_free"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -151,8 +185,9 @@ class Context:
     C context is destroyed only once none is alive (and never during interpreter
     shutdown, when the process frees everything anyway)."""
 
-    def __init__(self, handle, keep):
+    def __init__(self, handle, keep, device=0, stream=0):
         self.h = handle
+        self.device, self.stream = device, stream   # stream: the cudaStream_t as an integer
         self._keep = keep
         self._children = 0
         self._released = False
@@ -209,7 +244,7 @@ def mure_create(device: int = 0, stream=None, torch_allocator: bool = True) -> C
     st = lib().mure_create(device, handle_stream, alloc_p, C.byref(out))
     if st != 0:
         raise MureError(st, "mure_create failed")
-    return Context(out.value, keep)
+    return Context(out.value, keep, device, int(handle_stream or 0))
 
 
 class Model:
@@ -442,3 +477,183 @@ def mure_check_descriptors(model, table=None, precision: str = "fp32"):
     st = lib().mure_check_descriptors(C.byref(desc), _ptr(arr) if n else None, n,
                                       _ptr(pool) if plen else None, plen, msg, 512)
     return int(st), msg.value.decode()
+
+
+# ----------------------------------------------------------------- token caches --
+
+class Tokens:
+    """A paged cache of one attention layer's keys and values (mure_tokens)."""
+
+    def __init__(self, ctx, handle, desc, dtype, form, keep):
+        self.ctx, self.h, self.dtype, self.form = ctx, handle, dtype, form
+        self.n_kv_heads, self.head_dim, self.page_size = desc.n_kv_heads, desc.head_dim, desc.page_size
+        self.n_pages = desc.n_pages
+        self._keep = keep          # the caller's pools
+        ctx._children += 1
+
+    def free(self):
+        if getattr(self, "h", None):
+            if not _finalizing():
+                lib().mure_tokens_free(self.h)
+            self.h = None
+            self.ctx._child_gone()
+
+    def __del__(self):
+        self.free()
+
+
+class TokensPlan:
+    """One batch's sequences, laid out on the device (mure_tokens_plan)."""
+
+    def __init__(self, ctx, handle, n_heads):
+        self.ctx, self.h = ctx, handle
+        ctx._children += 1
+
+    def free(self):
+        if getattr(self, "h", None):
+            if not _finalizing():
+                lib().mure_tokens_plan_free(self.h)
+            self.h = None
+            self.ctx._child_gone()
+
+    def __del__(self):
+        self.free()
+
+
+def _torch_dtype(name):
+    import torch
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+def mure_tokens_create(ctx: Context, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, dtype: str = "bf16",
+                       form: str = "same", buffers=None) -> Tokens:
+    """A cache of n_pages pages.  buffers: the caller's pools as CUDA tensors, (k, v) or with form
+    "e4m3" (k, v, k_scale, v_scale), [n_pages][n_kv_heads][page_size][head_dim] (scales: without the
+    last dimension); by default the library allocates them, filled with zeros."""
+    d = _TokensDesc(int(n_kv_heads), int(head_dim), int(page_size), TOKEN_DTYPES[dtype], TOKEN_FORMS[form], 0,
+                    int(n_pages))
+    if buffers is not None:
+        import torch
+        if len(buffers) != (4 if form == "e4m3" else 2):
+            raise ValueError("buffers: (k, v), with e4m3 cells (k, v, k_scale, v_scale)")
+        shape = (d.n_pages, d.n_kv_heads, d.page_size, d.head_dim)
+        for i, b in enumerate(buffers):
+            want = shape if i < 2 else shape[:3]
+            types = ((_torch_dtype(dtype),) if form == "same" else (torch.float8_e4m3fn, torch.uint8)) if i < 2 else (torch.uint8,)
+            if tuple(b.shape) != want or b.dtype not in types or not b.is_contiguous() or not b.is_cuda or b.device.index != ctx.device:
+                raise ValueError(f"buffers[{i}]: a contiguous CUDA tensor {want} of {types[0]} on device {ctx.device} is wanted")
+        _enter(ctx, buffers)
+        d.k, d.v = buffers[0].data_ptr(), buffers[1].data_ptr()
+        if form == "e4m3":
+            d.k_scale, d.v_scale = buffers[2].data_ptr(), buffers[3].data_ptr()
+    out = C.c_void_p()
+    ctx.check(lib().mure_tokens_create(ctx.h, C.byref(d), C.byref(out)))
+    return Tokens(ctx, out.value, d, dtype, form, buffers)
+
+
+def _tokens_batch(n_heads, new_len, pos, kv_len, page_table, window, sinks, scale):
+    new_len, pos, kv_len = (np.ascontiguousarray(a, np.int32).reshape(-1) for a in (new_len, pos, kv_len))
+    n = len(new_len)
+    if len(pos) != n or len(kv_len) != n:
+        raise ValueError("new_len, pos and kv_len have different lengths")
+    table = np.ascontiguousarray(page_table, np.int32)
+    if table.ndim != 2 or table.shape[0] < n:
+        raise ValueError("page_table: a row of page ids for every sequence")
+    b = _TokensBatch(n, int(n_heads), _ptr(new_len), _ptr(pos), _ptr(kv_len), _ptr(table), table.shape[1], int(window),
+                     int(sinks), float(scale or 0.0), 0)
+    return b, (new_len, pos, kv_len, table)
+
+
+def mure_tokens_plan(tokens: Tokens, n_heads: int, new_len, pos, kv_len, page_table, window: int = 0, sinks: int = 0,
+                     scale: float = 0.0, plan: TokensPlan = None) -> TokensPlan:
+    """Lay out a batch for caches of `tokens`' geometry: sequence b has kv_len[b] cells in the pages
+    page_table[b] and new_len[b] new tokens from position pos[b] on.  plan: an existing plan that
+    takes the batch (a decoding loop's next step)."""
+    b, keep = _tokens_batch(n_heads, new_len, pos, kv_len, page_table, window, sinks, scale)
+    ctx = tokens.ctx
+    if plan is None:
+        out = C.c_void_p()
+        ctx.check(lib().mure_tokens_plan_create(tokens.h, C.byref(b), C.byref(out)))
+        plan = TokensPlan(ctx, out.value, int(n_heads))
+    else:
+        ctx.check(lib().mure_tokens_plan_set(plan.h, C.byref(b)))
+    plan.n_heads = int(n_heads)
+    plan.n_new, plan.n_cells = int(keep[0].sum(dtype=np.int64)), int(keep[2].sum(dtype=np.int64))
+    return plan
+
+
+def _enter(ctx, tensors):
+    """Where torch's current stream is not the context's: the context's stream waits for what is
+    queued on it, and the tensors' memory is kept until the context's stream is done with it."""
+    import torch
+    cur = torch.cuda.current_stream(ctx.device)
+    if cur.cuda_stream == ctx.stream:
+        return None
+    mine = torch.cuda.ExternalStream(ctx.stream, device=ctx.device) if ctx.stream else torch.cuda.default_stream(ctx.device)
+    mine.wait_stream(cur)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(mine)
+    return cur, mine
+
+
+def _leave(streams):
+    if streams is not None:
+        streams[0].wait_stream(streams[1])
+
+
+def _token_rows(t, tokens, n, heads, name):
+    if t.dtype != _torch_dtype(tokens.dtype) or not t.is_cuda or t.device.index != tokens.ctx.device:
+        raise ValueError(f"{name}: a CUDA tensor of {tokens.dtype} on device {tokens.ctx.device} is wanted")
+    if tuple(t.shape) != (n, heads, tokens.head_dim) or (n and t.stride(2) != 1):
+        raise ValueError(f"{name}: shape {(n, heads, tokens.head_dim)} with a dense last dimension is wanted, "
+                         f"got {tuple(t.shape)}, strides {t.stride()}")
+    return C.byref(_TokensRows(t.data_ptr(), t.stride(0), t.stride(1)))
+
+
+def mure_tokens_append(tokens: Tokens, plan: TokensPlan, k, v) -> None:
+    """Write the batch's new tokens' keys and values [tokens][n_kv_heads][head_dim] (any token and head
+    strides) into their cells."""
+    kr = _token_rows(k, tokens, plan.n_new, tokens.n_kv_heads, "k")
+    vr = _token_rows(v, tokens, plan.n_new, tokens.n_kv_heads, "v")
+    st = _enter(tokens.ctx, (k, v))
+    tokens.ctx.check(lib().mure_tokens_append(tokens.h, plan.h, kr, vr))
+    _leave(st)
+
+
+def mure_tokens_read(tokens: Tokens, plan: TokensPlan, new: bool = False, out=None):
+    """(k, v) [cells][n_kv_heads][head_dim] of all the batch's cells, sequence after sequence (new: of
+    its new tokens' cells)."""
+    import torch
+    n = plan.n_new if new else plan.n_cells
+    if out is None:
+        shape = (n, tokens.n_kv_heads, tokens.head_dim)
+        dt, dev = _torch_dtype(tokens.dtype), tokens.ctx.device
+        out = torch.empty(shape, dtype=dt, device=dev), torch.empty(shape, dtype=dt, device=dev)
+    kr = _token_rows(out[0], tokens, n, tokens.n_kv_heads, "out[0]")
+    vr = _token_rows(out[1], tokens, n, tokens.n_kv_heads, "out[1]")
+    st = _enter(tokens.ctx, out)
+    tokens.ctx.check(lib().mure_tokens_read(tokens.h, plan.h, int(bool(new)), kr, vr))
+    _leave(st)
+    return out
+
+
+def mure_tokens_attend(tokens: Tokens, plan: TokensPlan, q, out=None, lse: bool = False):
+    """Attention of the batch's new tokens q [tokens][n_heads][head_dim] over their sequences' cells:
+    out (same shape), with lse=True also the logs of the rows' sums, fp32 [tokens][n_heads]."""
+    import torch
+    n = plan.n_new
+    qr = _token_rows(q, tokens, n, plan.n_heads, "q")
+    if out is None:
+        out = torch.empty((n, plan.n_heads, tokens.head_dim), dtype=q.dtype, device=q.device)
+    orow = _token_rows(out, tokens, n, plan.n_heads, "out")
+    ls = torch.empty((n, plan.n_heads), dtype=torch.float32, device=q.device) if lse else None
+    st = _enter(tokens.ctx, (q, out, ls))
+    tokens.ctx.check(lib().mure_tokens_attend(tokens.h, plan.h, qr, orow, ls.data_ptr() if lse else None))
+    _leave(st)
+    return (out, ls) if lse else out
+
+
+def mure_synchronize(ctx: Context) -> None:
+    """Wait for everything queued on the context's stream; raises if a device-side check failed."""
+    ctx.check(lib().mure_synchronize(ctx.h))
