@@ -412,7 +412,7 @@ typedef struct {
     int32_t form;         /* MURE_FORM_* */
     int32_t reserved;     /* 0 */
     int64_t n_pages;      /* 1..2^31 - 1 */
-    /* device pools of the caller, 16-byte aligned, or all NULL: the library allocates them
+    /* device pools and scales of the caller, 16-byte aligned, or all NULL: the library allocates them
        and fills them with zeros.  The scales are NULL unless form is MURE_FORM_E4M3.
        Cells that no sequence holds may have any content; a NaN among them costs time (rows
        of a tile that holds one are computed again without the tensor cores) */

@@ -1,0 +1,587 @@
+// Token caches: attention of few rows (a decoding step's single tokens) in 16-bit types.
+//
+// A sequence's cells are read once per cached head, all query heads of the group as the 16 rows of
+// one mma tile, so the kernel is bound by device memory: 4 D flops per row and cell against
+// 2 D bytes a cell.  What decides is the bytes in flight and an even split:
+//   - the cells of all (sequence, cached head) pairs form one line of tiles, cut into equal
+//     shares, one per resident block; a pair that is cut is joined by the block that finishes
+//     last, in the order of its parts (equal bits whatever the order of arrival);
+//   - each warp of a block takes a quarter of every tile with a running maximum and sum of its
+//     own, and a ring of cp.async stages of its own: no barrier in the loop;
+//   - e4m3 codes are widened in registers, their scales applied to the scores and (for bf16) the
+//     probabilities in fp32, so the products take exact values.
+// The running maximum moves only when it grows by more than 2^8: the sums then need no rescaling in
+// nearly all steps, and powers up to 2^8 lose nothing in either type.
+#include <type_traits>
+
+#include "tokens_util.cuh"
+
+namespace mure {
+
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kStages = 3;
+constexpr int kAlign = 16;
+
+template <class T, bool E4M3, int DP>
+struct Few {
+    static constexpr int kElt = E4M3 ? 1 : 2;
+    static constexpr int kRow = DP * kElt;                                   // bytes of a staged row
+    static constexpr int WK = (4096 / kRow < 16) ? 16 : (4096 / kRow > 64 ? 64 : 4096 / kRow);   // cells of a warp's step
+    static constexpr int kTile = kWarps * WK;
+    static constexpr int kScaleBytes = E4M3 ? 2 * WK : 0;
+    static constexpr int kStage = 2 * WK * kRow + kScaleBytes;               // K rows, V rows, scales
+    static constexpr int kStageAl = (kStage + 127) / 128 * 128;
+    static constexpr int kJoin = kWarps * kFewRows * (DP + 2) * 4;
+    static constexpr int kRing = kWarps * kStages * kStageAl;
+    // the fragments of q: in registers, for 256 values in shared memory (one copy for all warps)
+    static constexpr bool kSharedQ = DP > 128;
+    static constexpr int kQ = kSharedQ ? DP / 16 * 32 * 16 : 0;
+    static constexpr int kSmem = (kRing > kJoin ? kRing : kJoin) + kQ;
+};
+
+struct FewParams {
+    TokPool pool;
+    TokBatch b;
+    TokWork w;
+    TokRows q, out;
+    float *lse;
+};
+
+__device__ __forceinline__ uint32_t su32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// Byte `byte` of staged row `row`: the eight 16-byte chunks of a 128-byte line are exchanged by the
+// row's (rows of 64 bytes: the line's) number, so that ldmatrix meets no bank conflict.
+template <int ROW>
+__device__ __forceinline__ uint32_t swz(int row, int byte)
+{
+    const uint32_t o = row * ROW + byte;
+    return o ^ (uint32_t)(((ROW >= 128 ? row : row >> 1) & 7) << 4);
+}
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool on)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp8(uint32_t dst, const void *src, bool on)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(on ? 8 : 0) : "memory");
+}
+__device__ __forceinline__ void cp4(uint32_t dst, const void *src, bool on)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(on ? 4 : 0) : "memory");
+}
+
+__device__ __forceinline__ void ldsm4(uint32_t a, uint32_t *r)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t a, uint32_t *r)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+
+template <class T> struct Mma;
+template <> struct Mma<__nv_bfloat16> {
+    static __device__ __forceinline__ void go(float *c, const uint32_t *a, uint32_t b0, uint32_t b1)
+    {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi)
+    {
+        uint32_t r;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+    // two e4m3 codes in the low 16 bits
+    static __device__ __forceinline__ uint32_t widen(uint32_t two)
+    {
+        const float2 f = e4m3_values((uint16_t)two);
+        return pack(f.x, f.y);
+    }
+};
+template <> struct Mma<__half> {
+    static __device__ __forceinline__ void go(float *c, const uint32_t *a, uint32_t b0, uint32_t b1)
+    {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi)
+    {
+        uint32_t r;
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+    static __device__ __forceinline__ uint32_t widen(uint32_t two)
+    {
+        uint32_t h;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
+        return h;
+    }
+};
+
+// f16 values from codes: the scale 2^e goes to the value as far as f16 holds every code times it
+// (e in -14..7), the rest to the probability.
+__device__ __forceinline__ int value_exp(uint32_t byte) { return max(-14, min(7, (int)byte - 127)); }
+
+__device__ __forceinline__ uint32_t half2_pow2(int lo, int hi)
+{
+    return (uint32_t)(lo + 15) << 10 | (uint32_t)(hi + 15) << 26;
+}
+
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// Two neighbouring values of a row of q (element offset even; rows may start anywhere).
+template <class T>
+__device__ __forceinline__ uint32_t load2(const T *p, int vec)
+{
+    if (vec) return __ldg(reinterpret_cast<const unsigned int *>(p));
+    const uint16_t *u = reinterpret_cast<const uint16_t *>(p);
+    return (uint32_t)u[0] | (uint32_t)u[1] << 16;
+}
+
+template <class T, bool E4M3, int DP>
+__global__ void __launch_bounds__(kWarps * 32, DP == 256 ? 1 : 2) k_tokens_few(FewParams p)
+{
+    using F = Few<T, E4M3, DP>;
+    constexpr int KS = DP / 16, NT = F::WK / 8, ND = DP / 8, WK = F::WK;
+    extern __shared__ __align__(128) char smem[];
+    __shared__ TokItem w;
+    __shared__ int last;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int D = p.pool.d, psz = 1 << p.pool.page_log2;
+    const uint32_t ring = su32(smem) + warp * kStages * F::kStageAl;
+    const int row_bytes = D * F::kElt;
+
+    for (int it = p.w.first[blockIdx.x]; it < p.w.first[blockIdx.x + 1]; ++it) {
+        if (threadIdx.x < sizeof(TokItem) / 8)
+            reinterpret_cast<int2 *>(&w)[threadIdx.x] = __ldg(reinterpret_cast<const int2 *>(p.w.items + it) + threadIdx.x);
+        __syncthreads();
+        const int nA = (w.a1 + F::kTile - 1) / F::kTile, b_al = w.b0 & ~(kAlign - 1);
+        const int32_t *table = p.b.table + w.table0;
+
+        // one step of this warp: cells [start, start + WK), of which begin .. end - 1 take part
+        auto range = [&](int tile, int &start, int &begin, int &end) {
+            if (tile < nA) { start = tile * F::kTile; begin = 0; end = w.a1; }
+            else { start = b_al + (tile - nA) * F::kTile; begin = w.b0; end = w.b1; }
+            start += warp * WK;
+        };
+        // the page of group `lane` of eight cells of a step (0 where it has none that take part)
+        auto pages = [&](int tile) {
+            if (tile >= w.t1 || lane >= WK / 8) return 0;
+            int start, begin, end;
+            range(tile, start, begin, end);
+            const int j = start + lane * 8;
+            return j < end ? __ldg(table + (j >> p.pool.page_log2)) : 0;
+        };
+        auto issue = [&](int tile, int slot, int page_of_group) {
+            if (tile < w.t1) {
+                int start, begin, end;
+                range(tile, start, begin, end);
+                const uint32_t st = ring + slot * F::kStageAl;
+                constexpr int CH = F::kRow / 16;               // chunks of a staged row
+                constexpr int PER = 32 / CH;                   // rows that a warp's instruction covers
+                const int byte = lane % CH * 16, r0 = lane / CH;
+#pragma unroll
+                for (int grp = 0; grp < WK / 8; ++grp) {
+                    const int page = __shfl_sync(0xffffffffu, page_of_group, grp);
+                    const int j0 = start + grp * 8;
+                    const int64_t row = (((int64_t)page * p.pool.hk + w.h) << p.pool.page_log2) | (j0 & (psz - 1));
+                    const char *kb = static_cast<const char *>(p.pool.k) + row * row_bytes;
+                    const char *vb = static_cast<const char *>(p.pool.v) + row * row_bytes;
+                    if (j0 + 7 < begin || j0 >= end) kb = static_cast<const char *>(p.pool.k), vb = static_cast<const char *>(p.pool.v);
+#pragma unroll
+                    for (int i = 0; i < 8; i += PER) {
+                        const int r = i + r0;
+                        const bool in = j0 + r >= begin && j0 + r < end;
+                        const uint32_t o = swz<F::kRow>(grp * 8 + r, byte);
+                        if (!E4M3 || D % 16 == 0) {
+                            const bool on = in && byte < row_bytes;
+                            const int64_t off = on ? (int64_t)r * row_bytes + byte : 0;
+                            cp16(st + o, kb + off, on);
+                            cp16(st + WK * F::kRow + o, vb + off, on);
+                        } else {                               // rows of codes at 8-byte boundaries
+#pragma unroll
+                            for (int q = 0; q < 16; q += 8) {
+                                const bool on = in && byte + q < row_bytes;
+                                const int64_t off = on ? (int64_t)r * row_bytes + byte + q : 0;
+                                cp8(st + o + q, kb + off, on);
+                                cp8(st + WK * F::kRow + o + q, vb + off, on);
+                            }
+                        }
+                    }
+                }
+                const int scale_page = E4M3 ? __shfl_sync(0xffffffffu, page_of_group, lane / 2) : 0;
+                if (E4M3 && lane < WK / 4) {
+                    const int j = start + lane * 4, page = scale_page;
+                    const bool on = j + 3 >= begin && j < end;
+                    const int64_t row = on ? (((int64_t)page * p.pool.hk + w.h) << p.pool.page_log2) | (j & (psz - 1)) : 0;
+                    cp4(st + 2 * WK * F::kRow + lane * 4, p.pool.ks + row, on);
+                    cp4(st + 2 * WK * F::kRow + WK + lane * 4, p.pool.vs + row, on);
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+
+        // the first stages are on their way while q is fetched
+        int next_pages = pages(w.t0);
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) {
+            const int cur = next_pages;
+            next_pages = pages(w.t0 + i + 1);
+            issue(w.t0 + i, i, cur);
+        }
+
+        uint32_t qf[F::kSharedQ ? 1 : KS][4];
+        uint4 *q_shared = reinterpret_cast<uint4 *>(smem + F::kSmem - F::kQ);
+        int prow[2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int r = w.r0 + g + half * 8;
+            const bool on = g + half * 8 < w.rows;
+            prow[half] = w.pos + r / p.b.group;
+            const T *q = reinterpret_cast<const T *>(p.q.p) +
+                         (on ? (int64_t)(w.row0 + r / p.b.group) * p.q.ts + (int64_t)(w.h * p.b.group + r % p.b.group) * p.q.hs : 0);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                // the order of a row's values within a K16 step only has to be that of the codes
+                const int d0 = ks * 16 + (E4M3 ? 4 * t : 2 * t), d1 = d0 + (E4M3 ? 2 : 8);
+                const uint32_t x0 = on && d0 < D ? load2(q + d0, p.q.vec) : 0u;
+                const uint32_t x1 = on && d1 < D ? load2(q + d1, p.q.vec) : 0u;
+                if (!F::kSharedQ) {
+                    qf[ks][half] = x0;
+                    qf[ks][2 + half] = x1;
+                } else if (warp == 0) {
+                    uint32_t *f = reinterpret_cast<uint32_t *>(q_shared + ks * 32 + lane);
+                    f[half] = x0;
+                    f[2 + half] = x1;
+                }
+            }
+        }
+        if (F::kSharedQ) __syncthreads();
+        const int p_lo = w.pos + w.r0 / p.b.group, p_hi = w.pos + (w.r0 + w.rows - 1) / p.b.group;
+
+        float o[ND][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < ND; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+
+        int slot = 0;
+        for (int tile = w.t0; tile < w.t1; ++tile) {
+            {
+                const int cur = next_pages, nt = tile + kStages - 1;
+                next_pages = pages(nt + 1);
+                issue(nt, slot == 0 ? kStages - 1 : slot - 1, cur);
+            }
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+            __syncwarp();
+            const uint32_t st = ring + slot * F::kStageAl;
+            slot = slot + 1 == kStages ? 0 : slot + 1;
+            int start, begin, end;
+            range(tile, start, begin, end);
+            if (start >= end || start + WK <= begin) { __syncwarp(); continue; }
+            const char *sc = smem + (st - su32(smem)) + 2 * WK * F::kRow;
+
+            uint4 qa;
+            auto qfrag = [&](int ks, uint4 &x) -> const uint32_t * {
+                if (!F::kSharedQ) return qf[F::kSharedQ ? 0 : ks];
+                x = q_shared[ks * 32 + lane];
+                return reinterpret_cast<const uint32_t *>(&x);
+            };
+            float s[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+#pragma unroll
+                for (int kp = 0; kp < F::kRow / 64; ++kp) {        // four 16-byte chunks of eight rows
+                    uint32_t r[4];
+                    ldsm4(st + swz<F::kRow>(n * 8 + (lane & 7), (kp * 4 + (lane >> 3)) * 16), r);
+                    if (E4M3) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            Mma<T>::go(s[n], qfrag(kp * 4 + i, qa), Mma<T>::widen(r[i] & 0xffffu), Mma<T>::widen(r[i] >> 16));
+                    } else {
+                        Mma<T>::go(s[n], qfrag(2 * kp, qa), r[0], r[1]);
+                        Mma<T>::go(s[n], qfrag(2 * kp + 1, qa), r[2], r[3]);
+                    }
+                }
+            }
+            // scores in powers of two, masked
+            const bool open = start >= begin && start + WK <= end && start + WK - 1 <= p_lo &&
+                              (p.b.window == 0 || start > p_hi - p.b.window);
+            float top[2] = {-INFINITY, -INFINITY};
+            uint32_t seen = 0;                               // not open: a bit per score
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float f0 = p.b.scale_log2, f1 = f0;
+                if (E4M3) {
+                    const uint32_t two = *reinterpret_cast<const uint16_t *>(sc + n * 8 + 2 * t);
+                    f0 *= scale_of(two & 255u);
+                    f1 *= scale_of(two >> 8);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x = s[n][i] * (i & 1 ? f1 : f0);
+                    if (!open) {
+                        const int j = start + n * 8 + 2 * t + (i & 1);
+                        const bool see = j >= begin && j < end && tok_seen(j, prow[i >> 1], p.b.window, p.b.sinks);
+                        x = see ? x : -INFINITY;
+                        seen |= (uint32_t)see << (n * 4 + i);
+                    }
+                    s[n][i] = x;
+                    top[i >> 1] = fmaxf(top[i >> 1], x);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+            }
+            const bool up0 = top[0] > m[0] + 8.f;
+            const bool up1 = top[1] > m[1] + 8.f;
+            if (__any_sync(0xffffffffu, up0 || up1)) {
+                const float n0 = up0 ? top[0] : m[0], n1 = up1 ? top[1] : m[1];
+                const float k0 = m[0] == n0 ? 1.f : ex2(m[0] - n0), k1 = m[1] == n1 ? 1.f : ex2(m[1] - n1);
+                m[0] = n0;
+                m[1] = n1;
+                l[0] *= k0;
+                l[1] *= k1;
+#pragma unroll
+                for (int i = 0; i < ND; ++i) {
+                    o[i][0] *= k0; o[i][1] *= k0;
+                    o[i][2] *= k1; o[i][3] *= k1;
+                }
+            }
+            const float ref0 = m[0] == -INFINITY ? 0.f : m[0], ref1 = m[1] == -INFINITY ? 0.f : m[1];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                s[n][0] = ex2(s[n][0] - ref0);
+                s[n][1] = ex2(s[n][1] - ref0);
+                s[n][2] = ex2(s[n][2] - ref1);
+                s[n][3] = ex2(s[n][3] - ref1);
+                l[0] += s[n][0] + s[n][1];
+                l[1] += s[n][2] + s[n][3];
+            }
+            const uint32_t vst = st + WK * F::kRow;
+#pragma unroll
+            for (int kg = 0; kg < WK / 16; ++kg) {
+                uint32_t a[4], vs[2] = {0, 0};
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                    float *x = s[2 * kg + hh];
+                    if (E4M3) {
+                        const uint32_t two = *reinterpret_cast<const uint16_t *>(sc + WK + kg * 16 + hh * 8 + 2 * t);
+                        const uint32_t y0 = two & 255u, y1 = two >> 8;
+                        float f0, f1;
+                        if (std::is_same<T, __half>::value) {
+                            const int e0 = value_exp(y0), e1 = value_exp(y1);
+                            vs[hh] = half2_pow2(e0, e1);
+                            f0 = y0 == 255u ? NAN : scale_of((uint32_t)max(0, (int)y0 - e0));
+                            f1 = y1 == 255u ? NAN : scale_of((uint32_t)max(0, (int)y1 - e1));
+                        } else {
+                            f0 = scale_of(y0);
+                            f1 = scale_of(y1);
+                        }
+                        if (!open) {                         // a masked cell's scale may be anything
+                            const uint32_t b = seen >> (8 * kg + 4 * hh);
+                            x[0] = b & 1 ? x[0] * f0 : 0.f; x[1] = b & 2 ? x[1] * f1 : 0.f;
+                            x[2] = b & 4 ? x[2] * f0 : 0.f; x[3] = b & 8 ? x[3] * f1 : 0.f;
+                        } else {
+                            x[0] *= f0; x[1] *= f1; x[2] *= f0; x[3] *= f1;
+                        }
+                    }
+                    a[2 * hh] = Mma<T>::pack(x[0], x[1]);
+                    a[2 * hh + 1] = Mma<T>::pack(x[2], x[3]);
+                }
+#pragma unroll
+                for (int c = 0; c < F::kRow / 16; c += 2) {
+                    uint32_t r[4];
+                    ldsm4t(vst + swz<F::kRow>(kg * 16 + (lane & 15), (c + (lane >> 4)) * 16), r);
+                    if (E4M3) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            uint32_t e0 = Mma<T>::widen(__byte_perm(r[2 * i], 0, 0x4420)), e1 = Mma<T>::widen(__byte_perm(r[2 * i + 1], 0, 0x4420));
+                            uint32_t u0 = Mma<T>::widen(__byte_perm(r[2 * i], 0, 0x4431)), u1 = Mma<T>::widen(__byte_perm(r[2 * i + 1], 0, 0x4431));
+                            if (std::is_same<T, __half>::value) {
+                                e0 = hmul2(e0, vs[0]); u0 = hmul2(u0, vs[0]);
+                                e1 = hmul2(e1, vs[1]); u1 = hmul2(u1, vs[1]);
+                            }
+                            Mma<T>::go(o[2 * (c + i)], a, e0, e1);
+                            Mma<T>::go(o[2 * (c + i) + 1], a, u0, u1);
+                        }
+                    } else {
+                        Mma<T>::go(o[c], a, r[0], r[1]);
+                        Mma<T>::go(o[c + 1], a, r[2], r[3]);
+                    }
+                }
+            }
+            __syncwarp();
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+        }
+        __syncthreads();                                     // every warp is done with its ring
+        // the warps' sums, maxima and sums of powers, [warp][row][DP + 2]
+        float *join = reinterpret_cast<float *>(smem);
+        constexpr int JR = DP + 2;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            float *row = join + (warp * kFewRows + g + half * 8) * JR;
+#pragma unroll
+            for (int i = 0; i < ND; ++i) {
+                const int d = E4M3 ? (i >> 1) * 16 + 4 * t + (i & 1) : i * 8 + 2 * t;
+                row[d] = o[i][2 * half];
+                row[d + (E4M3 ? 2 : 1)] = o[i][2 * half + 1];
+            }
+            if (t == 0) { row[DP] = m[half]; row[DP + 1] = l[half]; }
+        }
+        __syncthreads();
+
+        // a row's parts -> its sums: parts at src[i * step], n of them, in that order; by 8 values
+        auto joined = [&](const float *src, int64_t step, int n, int c, float *x, float &mm, float &ll) {
+            mm = -INFINITY;
+            for (int i = 0; i < n; ++i) {
+                const float v = src[i * step + DP];
+                mm = isnan(v) || isnan(mm) ? NAN : fmaxf(mm, v);
+            }
+            const float ref = mm == -INFINITY ? 0.f : mm;
+            ll = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+            for (int i = 0; i < n; ++i) {
+                const float f = ex2(src[i * step + DP] - ref);
+                ll = fmaf(f, src[i * step + DP + 1], ll);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = fmaf(f, src[i * step + c + k], x[k]);
+            }
+        };
+        const int chunks = D / 8;
+        // rows whose sums are not numbers are done again by the definition, from the cells they may
+        // attend to alone: a masked cell's NaN or infinity has met a probability of 0
+        int nan_here = 0;
+        for (int u = threadIdx.x; u < w.rows * chunks; u += kWarps * 32) {
+            float x[8], mm, ll;
+            const int r = u / chunks, c = (u % chunks) * 8;
+            joined(join + r * JR, kFewRows * JR, kWarps, c, x, mm, ll);
+            bool bad = isnan(mm) || isnan(ll);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) bad = bad || isnan(x[i]) || isinf(x[i]);
+            nan_here |= bad;
+        }
+        if (__syncthreads_or(nan_here)) {
+            const int j0 = w.t0 < nA ? w.t0 * F::kTile : max(w.b0, b_al + (w.t0 - nA) * F::kTile);
+            const int j1 = w.t1 <= nA ? min(w.a1, w.t1 * F::kTile) : min(w.b1, b_al + (w.t1 - nA) * F::kTile);
+            for (int r = warp; r < w.rows; r += kWarps) {
+                const int rr = w.r0 + r;
+                const T *q = reinterpret_cast<const T *>(p.q.p) + (int64_t)(w.row0 + rr / p.b.group) * p.q.ts +
+                             (int64_t)(w.h * p.b.group + rr % p.b.group) * p.q.hs;
+                float x[8], mm, ll;
+                attend_row<T, E4M3>(p.pool, table, w.h, q, p.q.vec, w.pos + rr / p.b.group, j0, j1, p.b.window, p.b.sinks,
+                                    p.b.scale_log2, x, mm, ll);
+                for (int k = 0; k < kWarps; ++k) {
+                    float *row = join + (k * kFewRows + r) * JR;
+                    if (lane * 8 < D) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) row[lane * 8 + i] = k == 0 ? x[i] : 0.f;
+                    }
+                    if (lane == 0) { row[DP] = k == 0 ? mm : -INFINITY; row[DP + 1] = k == 0 ? ll : 0.f; }
+                }
+            }
+            __syncthreads();
+        }
+        const float *src = join;
+        int64_t step = kFewRows * JR;
+        int n = kWarps, stride = JR;
+        if (w.parts > 1) {
+            float *mine = p.w.part + (int64_t)w.part * kFewRows * JR;
+            for (int u = threadIdx.x; u < w.rows * chunks; u += kWarps * 32) {
+                float x[8], mm, ll;
+                const int r = u / chunks, c = (u % chunks) * 8;
+                joined(join + r * JR, kFewRows * JR, kWarps, c, x, mm, ll);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) mine[r * JR + c + i] = x[i];
+                if (c == 0) { mine[r * JR + DP] = mm; mine[r * JR + DP + 1] = ll; }
+            }
+            __threadfence();
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                last = atomicAdd(p.w.count + w.unit, 1) == w.parts - 1;
+                if (last) p.w.count[w.unit] = 0;
+            }
+            __syncthreads();
+            if (!last) continue;                             // (the barrier above is the item's last)
+            __threadfence();
+            src = p.w.part + (int64_t)w.part0 * kFewRows * JR;
+            n = w.parts;
+        }
+        for (int u = threadIdx.x; u < w.rows * chunks; u += kWarps * 32) {
+            float x[8], mm, ll;
+            const int r = u / chunks, c = (u % chunks) * 8, rr = w.r0 + r;
+            joined(src + r * stride, step, n, c, x, mm, ll);
+            const int token = w.row0 + rr / p.b.group, head = w.h * p.b.group + rr % p.b.group;
+            const float inv = ll == 0.f ? 0.f : 1.f / ll;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] *= inv;
+            store8(reinterpret_cast<T *>(p.out.p) + token * p.out.ts + head * p.out.hs + c, p.out.vec, x);
+            if (p.lse && c == 0)
+                p.lse[(int64_t)token * p.b.n_heads + head] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.693147180559945f;
+        }
+        __syncthreads();                                     // the joined sums' memory is the next ring
+    }
+}
+
+template <class T, bool E4M3, int DP>
+int go(const FewParams &p, cudaStream_t s)
+{
+    using F = Few<T, E4M3, DP>;
+    allow_dynamic_smem(k_tokens_few<T, E4M3, DP>, F::kSmem);
+    k_tokens_few<T, E4M3, DP><<<p.w.blocks, kWarps * 32, F::kSmem, s>>>(p);
+    return 1;
+}
+
+template <class T, bool E4M3>
+int by_dim(const FewParams &p, cudaStream_t s)
+{
+    if (p.pool.d <= 64) return go<T, E4M3, 64>(p, s);
+    if (p.pool.d <= 128) return go<T, E4M3, 128>(p, s);
+    return go<T, E4M3, 256>(p, s);
+}
+
+}  // namespace
+
+int few_tile_cells(int dtype, int form, int d)
+{
+    (void)dtype;
+    if (form == MURE_FORM_E4M3)
+        return d <= 64 ? Few<__half, true, 64>::kTile : d <= 128 ? Few<__half, true, 128>::kTile : Few<__half, true, 256>::kTile;
+    return d <= 64 ? Few<__half, false, 64>::kTile : d <= 128 ? Few<__half, false, 128>::kTile : Few<__half, false, 256>::kTile;
+}
+
+int few_blocks() { return 2 * sm_count(); }
+
+int few_part_floats(int d) { return kFewRows * ((d <= 64 ? 64 : d <= 128 ? 128 : 256) + 2); }
+
+int launch_tokens_few(const TokPool &pool, const TokBatch &b, const TokWork &w, int dtype, int form, TokRows q, TokRows out,
+                      float *lse, cudaStream_t s)
+{
+    if (w.blocks == 0) return 0;
+    const FewParams p{pool, b, w, q, out, lse};
+    const bool e = form == MURE_FORM_E4M3;
+    if (dtype == MURE_F16) return e ? by_dim<__half, true>(p, s) : by_dim<__half, false>(p, s);
+    return e ? by_dim<__nv_bfloat16, true>(p, s) : by_dim<__nv_bfloat16, false>(p, s);
+}
+
+}  // namespace mure

@@ -30,8 +30,9 @@ struct mure_tokens_plan {
     int64_t tiles_new = 0, tiles_all = 0;
     int new_past_end = -1;                   // a sequence whose new tokens end past its cells
     std::string append_fault;                // why the batch's new tokens cannot be written ("" if they can)
-    void *mem = nullptr;
-    size_t mem_bytes = 0;
+    TokWork few;                             // 16-bit types: the rows that the kernel for few rows takes
+    void *mem = nullptr, *part = nullptr;    // tables; partial results
+    size_t mem_bytes = 0, part_bytes = 0;
 };
 
 namespace {
@@ -68,6 +69,103 @@ TokPool pool_of(const mure_tokens *t)
     p.k = t->d.k; p.v = t->d.v; p.ks = t->d.k_scale; p.vs = t->d.v_scale;
     p.hk = t->d.n_kv_heads; p.d = t->d.head_dim; p.page_log2 = log2_of(t->d.page_size);
     return p;
+}
+
+// The tables' memory: at least `bytes`, and some more where it grows (the next steps' do).
+void reserve(mure_ctx *c, void *&mem, size_t &have, size_t bytes)
+{
+    if (bytes <= have) return;
+    dfree(c, mem);
+    mem = nullptr;
+    have = 0;
+    mem = dalloc(c, bytes + bytes / 4);
+    have = bytes + bytes / 4;
+}
+
+// Rows [r0, r0 + rows) of sequence s and head h and the tiles of the cells that they may attend to.
+struct Unit {
+    TokItem item;
+    int tiles;
+};
+
+// What a kernel's pieces are made of.
+struct Shape {
+    int rows;      // of a piece
+    int tile;      // cells
+    int align;     // of the first tile past the sinks
+    int blocks;    // that run at a time
+};
+
+void add_units(std::vector<Unit> &units, const TokSeq &q, int seq, int hk, int group, int window, int sinks, const Shape &sh)
+{
+    const int64_t n_rows = (int64_t)q.n_new * group;
+    for (int h = 0; h < hk; ++h)
+        for (int64_t r0 = 0; r0 < n_rows; r0 += sh.rows) {
+            Unit u{};
+            TokItem &w = u.item;
+            w.seq = seq; w.h = h; w.r0 = (int)r0; w.rows = (int)std::min<int64_t>(sh.rows, n_rows - r0);
+            w.pos = q.pos; w.row0 = q.row0; w.kv = q.kv; w.n_rows = (int)n_rows; w.table0 = q.table0;
+            const int lo = q.pos + (int)(r0 / group), hi = q.pos + (int)((r0 + w.rows - 1) / group);
+            const int end = std::min(q.kv, hi + 1);
+            w.b1 = end;
+            if (window > 0 && lo >= window) {
+                w.b0 = std::min(lo - window + 1, end);
+                w.a1 = std::min(sinks, end);
+                if (w.a1 >= w.b0 / sh.align * sh.align) w.a1 = w.b0 = 0;   // one run from the first cell on
+            }
+            const int from = w.b0 / sh.align * sh.align;
+            u.tiles = (w.a1 + sh.tile - 1) / sh.tile + (w.b0 < end ? (end - from + sh.tile - 1) / sh.tile : 0);
+            units.push_back(u);
+        }
+}
+
+// The units' tiles as one line, cut into equal shares, one per block that runs at a time; a unit that
+// is cut gets a slot for every part's result.
+struct Shares {
+    std::vector<TokItem> items;
+    std::vector<int32_t> first;
+    int parts = 0, cut = 0;
+};
+
+Shares share(const std::vector<Unit> &units, const Shape &sh)
+{
+    Shares r;
+    int64_t total = 0;
+    for (const Unit &u : units) total += std::max(u.tiles, 1);     // (rows without cells still get zeros)
+    const int64_t blocks = std::min<int64_t>(total, sh.blocks);
+    r.first.push_back(0);
+    int64_t at = 0;                                                 // of the line
+    int block = 0;
+    for (const Unit &u : units) {
+        const int64_t n = std::max(u.tiles, 1);
+        const size_t i0 = r.items.size();
+        for (int64_t t = 0; t < n;) {
+            while (at >= total * (block + 1) / blocks) {
+                r.first.push_back((int32_t)r.items.size());
+                ++block;
+            }
+            const int64_t take = std::min(n - t, total * (block + 1) / blocks - at);
+            TokItem w = u.item;
+            w.t0 = (int)t;
+            w.t1 = (int)std::min<int64_t>(t + take, u.tiles);
+            w.parts = 1;
+            r.items.push_back(w);
+            t += take;
+            at += take;
+        }
+        const int parts = (int)(r.items.size() - i0);
+        if (parts > 1) {
+            for (int k = 0; k < parts; ++k) {
+                TokItem &w = r.items[i0 + k];
+                w.part0 = r.parts; w.part = r.parts + k; w.parts = parts; w.unit = r.cut;
+            }
+            r.parts += parts;
+            ++r.cut;
+        }
+    }
+    r.first.push_back((int32_t)r.items.size());
+    if (units.empty()) r.first.assign(1, 0);
+    return r;
 }
 
 // The packed device image of a plan's tables: parts at 16-byte boundaries of one host buffer.
@@ -153,16 +251,24 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
             fault = "two new tokens have the cell " + std::to_string(written[i].first) + " of page " +
                     std::to_string(written[i].page);
 
+    // attention: the pieces of the kernels that take this type
+    const int group = b.n_heads / d.n_kv_heads;
+    const Shape few_shape{kFewRows, few_tile_cells(d.dtype, d.form, d.head_dim), 16, few_blocks()};
+    std::vector<Unit> few;
+    if (d.dtype != MURE_F32)
+        for (int s = 0; s < n; ++s) {
+            FAILIF((int64_t)seq[s].n_new * group > kMostPos, c, MURE_ERR_UNSUPPORTED, "sequence %d: more than 2^30 rows", s);
+            add_units(few, seq[s], s, d.n_kv_heads, group, b.window, b.sinks, few_shape);
+            FAILIF(few.size() > ((size_t)1 << 27), c, MURE_ERR_UNSUPPORTED, "more than 2^27 pieces of work");
+        }
+    const Shares fs = share(few, few_shape);
+    FAILIF(fs.items.size() > ((size_t)1 << 28), c, MURE_ERR_UNSUPPORTED, "more than 2^28 pieces of work");
+
     Image im;
     const size_t o_seq = im.add(seq), o_table = im.add(table), o_new = im.add(tile_new), o_all = im.add(tile_all);
-    if (im.bytes.size() > p->mem_bytes) {
-        dfree(c, p->mem);
-        p->mem = nullptr;
-        p->mem_bytes = 0;
-        const size_t room = im.bytes.size() + im.bytes.size() / 4;   // the next steps' tables grow
-        p->mem = dalloc(c, room);
-        p->mem_bytes = room;
-    }
+    const size_t o_few = im.add(fs.items), o_few1 = im.add(fs.first), o_fewc = im.add(std::vector<int32_t>(fs.cut, 0));
+    reserve(c, p->mem, p->mem_bytes, im.bytes.size());
+    reserve(c, p->part, p->part_bytes, (size_t)fs.parts * few_part_floats(d.head_dim) * 4);
     // (from pageable memory: the call has taken its copy when it returns)
     CK(c, cudaMemcpyAsync(p->mem, im.bytes.data(), im.bytes.size(), cudaMemcpyHostToDevice, c->stream));
     char *m = static_cast<char *>(p->mem);
@@ -171,9 +277,14 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
     v.table = reinterpret_cast<int32_t *>(m + o_table);
     v.tile_new = reinterpret_cast<int32_t *>(m + o_new);
     v.tile_all = reinterpret_cast<int32_t *>(m + o_all);
+    p->few.items = reinterpret_cast<TokItem *>(m + o_few);
+    p->few.first = reinterpret_cast<int32_t *>(m + o_few1);
+    p->few.blocks = (int)fs.first.size() - 1;
+    p->few.part = static_cast<float *>(p->part);
+    p->few.count = reinterpret_cast<int32_t *>(m + o_fewc);
     v.n_seqs = n;
     v.n_heads = b.n_heads;
-    v.group = b.n_heads / d.n_kv_heads;
+    v.group = group;
     v.window = b.window;
     v.sinks = b.sinks;
     v.scale_log2 = (float)((b.scale > 0.f ? (double)b.scale : 1.0 / std::sqrt((double)d.head_dim)) * 1.4426950408889634);
@@ -240,7 +351,7 @@ mure_status mure_tokens_create(mure_ctx *c, const mure_tokens_desc *desc, mure_t
         FAILIF(any && (!d.k || !d.v || (q && (!d.k_scale || !d.v_scale))), c, MURE_ERR_INVALID_ARG,
                "some of the pools are NULL");
         FAILIF(!q && (d.k_scale || d.v_scale), c, MURE_ERR_INVALID_ARG, "scales without MURE_FORM_E4M3");
-        FAILIF((uintptr_t)d.k % 16 || (uintptr_t)d.v % 16, c, MURE_ERR_INVALID_ARG, "pools are not 16-byte aligned");
+        FAILIF((uintptr_t)d.k % 16 || (uintptr_t)d.v % 16 || (uintptr_t)d.k_scale % 16 || (uintptr_t)d.v_scale % 16, c, MURE_ERR_INVALID_ARG, "pools are not 16-byte aligned");
         CK(c, cudaSetDevice(c->device));
         auto t = std::make_unique<mure_tokens>();
         t->ctx = c;
@@ -295,6 +406,7 @@ mure_status mure_tokens_plan_create(mure_tokens *t, const mure_tokens_batch *bat
             set_plan(p.get(), batch);
         } catch (...) {
             dfree(c, p->mem);
+            dfree(c, p->part);
             throw;
         }
         *out = p.release();
@@ -315,6 +427,7 @@ void mure_tokens_plan_free(mure_tokens_plan *p)
 {
     if (!p) return;
     dfree(p->ctx, p->mem);
+    dfree(p->ctx, p->part);
     delete p;
 }
 
@@ -368,7 +481,10 @@ mure_status mure_tokens_attend(mure_tokens *t, mure_tokens_plan *p, const mure_t
         check_apart(c, orow, t->d, p->n_new, p->b.n_heads, "out");
         FAILIF((uintptr_t)lse % 4 != 0, c, MURE_ERR_INVALID_ARG, "lse is not aligned");
         CK(c, cudaSetDevice(c->device));
-        c->launches += launch_tokens_attend_rows(pool_of(t), p->b, t->d.dtype, t->d.form, p->n_new, qr, orow, lse, c->stream);
+        if (t->d.dtype == MURE_F32)
+            c->launches += launch_tokens_attend_rows(pool_of(t), p->b, t->d.dtype, t->d.form, p->n_new, qr, orow, lse, c->stream);
+        else
+            c->launches += launch_tokens_few(pool_of(t), p->b, p->few, t->d.dtype, t->d.form, qr, orow, lse, c->stream);
         check_launch(c);
     });
 }

@@ -43,6 +43,36 @@ struct TokRows {
     int vec = 0;
 };
 
+// A piece of an attention call's work: rows r0 .. r0 + rows of one sequence and cached head (row r is
+// new token r / group, query head h * group + r % group) over the tiles t0 .. t1 - 1 of the cells
+// that any of them may attend to: first those of a0 .. a1 - 1 (the sinks, where they lie
+// apart), then those of b0 .. b1 - 1, tiles from b0 rounded down to the kernel's alignment.
+struct TokItem {
+    int32_t seq, h, r0, rows;
+    int32_t pos, row0, kv, n_rows;    // the sequence's, and its rows n_new * group
+    int32_t a1, b0, b1, t0;           // (a0 is 0)
+    int32_t t1, part, part0, parts;   // parts > 1: partial result `part` of part0 .. part0 + parts - 1
+    int64_t table0;
+    int32_t unit, reserved;           // parts > 1: the counter of the rows' finished parts
+};
+
+// The pieces, block by block, and room for partial results.
+struct TokWork {
+    const TokItem *items = nullptr;
+    const int32_t *first = nullptr;   // [blocks + 1] a block's first item
+    int blocks = 0;
+    float *part = nullptr;            // [parts][rows of a piece][padded d + 2]: sums, maximum, sum of powers
+    int32_t *count = nullptr;         // [units], zero between calls
+};
+
+// Rows of a piece and cells of a tile of the kernel for few rows.
+constexpr int kFewRows = 16;
+int few_tile_cells(int dtype, int form, int d);
+int few_blocks();                     // blocks that run at a time
+int few_part_floats(int d);
+int launch_tokens_few(const TokPool &pool, const TokBatch &b, const TokWork &w, int dtype, int form, TokRows q, TokRows out,
+                      float *lse, cudaStream_t s);
+
 int launch_tokens_append(const TokPool &pool, const TokBatch &b, int dtype, int form, TokRows k, TokRows v, int64_t tiles,
                          cudaStream_t s);
 int launch_tokens_read(const TokPool &pool, const TokBatch &b, int dtype, int form, int part, TokRows k, TokRows v,

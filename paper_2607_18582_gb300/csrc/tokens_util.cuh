@@ -43,6 +43,14 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax)
 // x / scale, exact unless it leaves the normal numbers far below the codes: x * 2^(127 - byte), byte <= 247.
 __device__ __forceinline__ float unscale(float x, uint32_t byte) { return x * __uint_as_float((254u - byte) << 23); }
 
+// 2^x by the hardware's approximation (2 units in the last place; results below 2^-126 are 0).
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 __device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi)
 {
     uint16_t r;
