@@ -105,6 +105,23 @@ __global__ void __launch_bounds__(kThreads) k_tokens_read(CellParams p)
     }
 }
 
+// Whole pages of codes as 16-bit pages, in the order of the list.
+template <class T>
+__global__ void __launch_bounds__(kThreads) k_tokens_widen(TokPool p, const int32_t *pages, int64_t rows, int lanes, T *k, T *v)
+{
+    const int c = (threadIdx.x & (lanes - 1)) * 8;
+    if (c >= p.d) return;
+    const int64_t per_page = (int64_t)p.hk << p.page_log2;
+    for (int64_t r = (int64_t)blockIdx.x * (kThreads / lanes) + threadIdx.x / lanes; r < rows; r += (int64_t)gridDim.x * (kThreads / lanes)) {
+        const int64_t i = r / per_page, row = __ldg(pages + i) * per_page + (r - i * per_page);
+        float x[8], y[8];
+        cell8<T, true>(p.k, p.ks, row, p.d, c, x);
+        cell8<T, true>(p.v, p.vs, row, p.d, c, y);
+        store8(k + r * p.d + c, 1, x);
+        store8(v + r * p.d + c, 1, y);
+    }
+}
+
 template <class T, bool E4M3>
 int go(const CellParams &p, bool read, int64_t tiles, cudaStream_t s)
 {
@@ -130,6 +147,21 @@ int row_lanes(int d)
 }
 
 }  // namespace
+
+int launch_tokens_widen(const TokPool &pool, int dtype, const int32_t *pages, int64_t n_list, void *k, void *v, cudaStream_t s)
+{
+    const int lanes = row_lanes(pool.d);
+    const int64_t rows = n_list * pool.hk << pool.page_log2;
+    const int64_t blocks = (rows + kThreads / lanes - 1) / (kThreads / lanes);
+    if (blocks == 0) return 0;
+    const unsigned grid = (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20));
+    if (dtype == MURE_F16)
+        k_tokens_widen<__half><<<grid, kThreads, 0, s>>>(pool, pages, rows, lanes, static_cast<__half *>(k), static_cast<__half *>(v));
+    else
+        k_tokens_widen<__nv_bfloat16><<<grid, kThreads, 0, s>>>(pool, pages, rows, lanes, static_cast<__nv_bfloat16 *>(k),
+                                                                static_cast<__nv_bfloat16 *>(v));
+    return 1;
+}
 
 int launch_tokens_append(const TokPool &pool, const TokBatch &b, int dtype, int form, TokRows k, TokRows v, int64_t tiles,
                          cudaStream_t s)

@@ -9,6 +9,9 @@
 #include <cstdlib>
 #include <cstring>
 #include <memory>
+#include <numeric>
+#include <queue>
+#include <unordered_map>
 
 #include "host.cuh"
 #include "tokens.cuh"
@@ -19,6 +22,7 @@ struct mure_tokens {
     mure_ctx *ctx = nullptr;
     mure_tokens_desc d{};
     void *own = nullptr;      // the library's allocation of the pools (null: the caller's pools)
+    CUtensorMap map_k, map_v; // 16-bit cells of up to kChunkDim values: the pools
 };
 
 struct mure_tokens_plan {
@@ -31,12 +35,19 @@ struct mure_tokens_plan {
     int new_past_end = -1;                   // a sequence whose new tokens end past its cells
     std::string append_fault;                // why the batch's new tokens cannot be written ("" if they can)
     TokWork few;                             // 16-bit types: the rows that the kernel for few rows takes
-    void *mem = nullptr, *part = nullptr;    // tables; partial results
-    size_t mem_bytes = 0, part_bytes = 0;
+    TokChunk chunk;                          // ... and those that the kernel for chunks takes
+    // E4M3: the pages that chunks read, as 16-bit pages
+    const int32_t *wide_pages = nullptr, *wide_table = nullptr;
+    int64_t n_wide = 0;
+    CUtensorMap map_k, map_v;
+    void *mem = nullptr, *part = nullptr, *wide = nullptr;    // tables; partial results; 16-bit pages
+    size_t mem_bytes = 0, part_bytes = 0, wide_bytes = 0;
 };
 
 namespace {
 
+// E4M3 rows of a sequence and head up to which the kernel for few rows takes them.
+constexpr int kFewRowsWide = 64;
 constexpr int64_t kMostPos = int64_t(1) << 30;
 
 int elt_bytes(int dtype) { return dtype == MURE_F32 ? 4 : 2; }
@@ -122,9 +133,9 @@ void add_units(std::vector<Unit> &units, const TokSeq &q, int seq, int hk, int g
 // The units' tiles as one line, cut into equal shares, one per block that runs at a time; a unit that
 // is cut gets a slot for every part's result.
 struct Shares {
-    std::vector<TokItem> items;
+    std::vector<TokItem> items, cut;   // cut: the first part of every cut unit
     std::vector<int32_t> first;
-    int parts = 0, cut = 0;
+    int parts = 0;
 };
 
 Shares share(const std::vector<Unit> &units, const Shape &sh)
@@ -157,14 +168,86 @@ Shares share(const std::vector<Unit> &units, const Shape &sh)
         if (parts > 1) {
             for (int k = 0; k < parts; ++k) {
                 TokItem &w = r.items[i0 + k];
-                w.part0 = r.parts; w.part = r.parts + k; w.parts = parts; w.unit = r.cut;
+                w.part0 = r.parts; w.part = r.parts + k; w.parts = parts; w.unit = (int)r.cut.size();
             }
             r.parts += parts;
-            ++r.cut;
+            r.cut.push_back(r.items[i0]);
         }
     }
     r.first.push_back((int32_t)r.items.size());
     if (units.empty()) r.first.assign(1, 0);
+    return r;
+}
+
+// The same for the kernel for chunks, whose pieces read the same cells again for every 256 rows: whole
+// units, the longest first, each to the block with the least work, while they fit its share; the units
+// that are left are cut to fill the blocks up.  Units of one sequence have about one length, so
+// blocks that work at a time read the same cells (a batch whose cells exceed the L2 cache: 880 MB
+// from device memory where shares were cut along the line).  A unit that is cut writes and
+// reads its sums once more, so few are.
+Shares pack(const std::vector<Unit> &units, const Shape &sh)
+{
+    Shares r;
+    r.first.push_back(0);
+    if (units.empty()) return r;
+    // in tiles: a tile of one half (up to 128 rows) takes 0.6 of the time, a unit's beginning and end about 3
+    constexpr double kStart = 3.0;
+    auto tile_cost = [&](const Unit &u) { return u.item.rows > sh.rows / 2 ? 1.0 : 0.6; };
+    auto cost = [&](const Unit &u) { return u.tiles * tile_cost(u) + kStart; };
+    std::vector<int> order(units.size());
+    std::iota(order.begin(), order.end(), 0);
+    std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return cost(units[a]) > cost(units[b]); });
+    double total = 0;
+    for (const Unit &u : units) total += cost(u);
+    const int blocks = (int)std::min<double>(sh.blocks, std::max(1.0, std::ceil(total / (kStart + 1))));
+    const double share = total / blocks * 1.02;
+    using Load = std::pair<double, int>;                            // work so far, block
+    std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
+    for (int b = 0; b < blocks; ++b) least.push({0.0, b});
+    std::vector<std::vector<TokItem>> mine(blocks);
+    std::vector<int> left;
+    for (int i : order) {
+        const Unit &u = units[i];
+        const Load l = least.top();
+        if (l.first + cost(u) > share) { left.push_back(i); continue; }
+        least.pop();
+        least.push({l.first + cost(u), l.second});
+        TokItem w = u.item;
+        w.t0 = 0; w.t1 = u.tiles; w.parts = 1;
+        mine[l.second].push_back(w);
+    }
+    constexpr int kLeast = 4;                                       // tiles of a part, at least
+    for (int i : left) {
+        const Unit &u = units[i];
+        std::vector<std::pair<int, TokItem>> parts;
+        for (int t = 0; t < u.tiles || (u.tiles == 0 && t == 0);) {
+            const Load l = least.top();
+            least.pop();
+            int take = std::max((int)((share - l.first - kStart) / tile_cost(u)), kLeast);
+            if (u.tiles - t - take < kLeast) take = u.tiles - t;
+            TokItem w = u.item;
+            w.t0 = t; w.t1 = t + take;
+            parts.push_back({l.second, w});
+            least.push({l.first + take * tile_cost(u) + kStart, l.second});
+            t += std::max(take, 1);
+        }
+        for (size_t k = 0; k < parts.size(); ++k) {
+            TokItem &w = parts[k].second;
+            w.parts = (int)parts.size();
+            if (parts.size() > 1) {
+                w.part0 = r.parts; w.part = r.parts + (int)k; w.unit = (int)r.cut.size();
+            }
+            mine[parts[k].first].push_back(w);
+        }
+        if (parts.size() > 1) {
+            r.parts += (int)parts.size();
+            r.cut.push_back(parts[0].second);
+        }
+    }
+    for (const auto &m : mine) {
+        r.items.insert(r.items.end(), m.begin(), m.end());
+        r.first.push_back((int32_t)r.items.size());
+    }
     return r;
 }
 
@@ -253,22 +336,52 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
 
     // attention: the pieces of the kernels that take this type
     const int group = b.n_heads / d.n_kv_heads;
+    const bool wide = d.form == MURE_FORM_E4M3;
     const Shape few_shape{kFewRows, few_tile_cells(d.dtype, d.form, d.head_dim), 16, few_blocks()};
-    std::vector<Unit> few;
+    const Shape chunk_shape{kChunkRows, kChunkTile, chunk_box(d.page_size), chunk_blocks()};
+    std::vector<Unit> few, chunk;
+    std::vector<int32_t> wide_table, wide_pages;
+    std::unordered_map<int32_t, int32_t> wide_of;
     if (d.dtype != MURE_F32)
         for (int s = 0; s < n; ++s) {
-            FAILIF((int64_t)seq[s].n_new * group > kMostPos, c, MURE_ERR_UNSUPPORTED, "sequence %d: more than 2^30 rows", s);
-            add_units(few, seq[s], s, d.n_kv_heads, group, b.window, b.sinks, few_shape);
-            FAILIF(few.size() > ((size_t)1 << 27), c, MURE_ERR_UNSUPPORTED, "more than 2^27 pieces of work");
+            const TokSeq &q = seq[s];
+            const int64_t rows = (int64_t)q.n_new * group;
+            FAILIF(rows > kMostPos, c, MURE_ERR_UNSUPPORTED, "sequence %d: more than 2^30 rows", s);
+            const bool as_chunk = d.head_dim <= kChunkDim && rows > (wide ? kFewRowsWide : kFewRows);
+            add_units(as_chunk ? chunk : few, q, s, d.n_kv_heads, group, b.window, b.sinks, as_chunk ? chunk_shape : few_shape);
+            FAILIF(few.size() + chunk.size() > ((size_t)1 << 27), c, MURE_ERR_UNSUPPORTED, "more than 2^27 pieces of work");
+            if (!as_chunk || !wide) continue;
+            // the pages that any of its rows reads
+            wide_table.resize(table.size(), 0);
+            const int64_t end = std::min<int64_t>(q.kv, (int64_t)q.pos + q.n_new);
+            const int64_t from = b.window > 0 ? std::max(0, q.pos - b.window + 1) : 0;
+            for (int64_t i = 0; i << page_log2 < end; ++i) {
+                if (((i + 1) << page_log2) <= from && i << page_log2 >= b.sinks) continue;
+                const int32_t id = table[q.table0 + i];
+                const auto at = wide_of.emplace(id, (int32_t)wide_pages.size());
+                if (at.second) wide_pages.push_back(id);
+                wide_table[q.table0 + i] = at.first->second;
+            }
         }
-    const Shares fs = share(few, few_shape);
-    FAILIF(fs.items.size() > ((size_t)1 << 28), c, MURE_ERR_UNSUPPORTED, "more than 2^28 pieces of work");
+    const Shares fs = share(few, few_shape), cs = pack(chunk, chunk_shape);
+    FAILIF(fs.items.size() + cs.items.size() > ((size_t)1 << 28), c, MURE_ERR_UNSUPPORTED, "more than 2^28 pieces of work");
 
     Image im;
     const size_t o_seq = im.add(seq), o_table = im.add(table), o_new = im.add(tile_new), o_all = im.add(tile_all);
-    const size_t o_few = im.add(fs.items), o_few1 = im.add(fs.first), o_fewc = im.add(std::vector<int32_t>(fs.cut, 0));
+    const size_t o_few = im.add(fs.items), o_few1 = im.add(fs.first), o_fewc = im.add(std::vector<int32_t>(fs.cut.size(), 0));
+    const size_t o_chunk = im.add(cs.items), o_chunk1 = im.add(cs.first), o_cut = im.add(cs.cut);
+    const size_t o_wt = im.add(wide_table), o_wp = im.add(wide_pages);
+    const size_t few_part = ((size_t)fs.parts * few_part_floats(d.head_dim) * 4 + 255) / 256 * 256;
     reserve(c, p->mem, p->mem_bytes, im.bytes.size());
-    reserve(c, p->part, p->part_bytes, (size_t)fs.parts * few_part_floats(d.head_dim) * 4);
+    reserve(c, p->part, p->part_bytes, few_part + (size_t)cs.parts * chunk_part_floats(d.head_dim) * 4);
+    if (!wide_pages.empty()) {
+        const int64_t pool = (int64_t)wide_pages.size() * d.n_kv_heads * d.page_size * d.head_dim * 2;
+        reserve(c, p->wide, p->wide_bytes, 2 * (size_t)pool);
+        FAILIF(!chunk_map(p->map_k, p->wide, d.dtype, d.n_kv_heads, d.head_dim, d.page_size, (int64_t)wide_pages.size()) ||
+                   !chunk_map(p->map_v, static_cast<char *>(p->wide) + pool, d.dtype, d.n_kv_heads, d.head_dim, d.page_size,
+                              (int64_t)wide_pages.size()),
+               c, MURE_ERR_CUDA, "no tensor map of the widened pages");
+    }
     // (from pageable memory: the call has taken its copy when it returns)
     CK(c, cudaMemcpyAsync(p->mem, im.bytes.data(), im.bytes.size(), cudaMemcpyHostToDevice, c->stream));
     char *m = static_cast<char *>(p->mem);
@@ -282,6 +395,16 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
     p->few.blocks = (int)fs.first.size() - 1;
     p->few.part = static_cast<float *>(p->part);
     p->few.count = reinterpret_cast<int32_t *>(m + o_fewc);
+    p->chunk.w.items = reinterpret_cast<TokItem *>(m + o_chunk);
+    p->chunk.w.first = reinterpret_cast<int32_t *>(m + o_chunk1);
+    p->chunk.w.blocks = (int)cs.first.size() - 1;
+    p->chunk.w.part = reinterpret_cast<float *>(static_cast<char *>(p->part) + few_part);
+    p->chunk.ml = p->chunk.w.part + (int64_t)cs.parts * (chunk_part_floats(d.head_dim) - 2 * kChunkRows);
+    p->chunk.cut = reinterpret_cast<TokItem *>(m + o_cut);
+    p->chunk.n_cut = (int)cs.cut.size();
+    p->wide_table = reinterpret_cast<int32_t *>(m + o_wt);
+    p->wide_pages = reinterpret_cast<int32_t *>(m + o_wp);
+    p->n_wide = (int64_t)wide_pages.size();
     v.n_seqs = n;
     v.n_heads = b.n_heads;
     v.group = group;
@@ -370,6 +493,12 @@ mure_status mure_tokens_create(mure_ctx *c, const mure_tokens_desc *desc, mure_t
             if (e != cudaSuccess) dfree(c, m);
             CK(c, e);
         }
+        if (d.dtype != MURE_F32 && !q && d.head_dim <= kChunkDim) {
+            const bool ok = chunk_map(t->map_k, t->d.k, d.dtype, d.n_kv_heads, d.head_dim, d.page_size, d.n_pages) &&
+                            chunk_map(t->map_v, t->d.v, d.dtype, d.n_kv_heads, d.head_dim, d.page_size, d.n_pages);
+            if (!ok) dfree(c, t->own);
+            FAILIF(!ok, c, MURE_ERR_CUDA, "no tensor map of the pools");
+        }
         *out = t.release();
     });
 }
@@ -407,6 +536,7 @@ mure_status mure_tokens_plan_create(mure_tokens *t, const mure_tokens_batch *bat
         } catch (...) {
             dfree(c, p->mem);
             dfree(c, p->part);
+            dfree(c, p->wide);
             throw;
         }
         *out = p.release();
@@ -428,6 +558,7 @@ void mure_tokens_plan_free(mure_tokens_plan *p)
     if (!p) return;
     dfree(p->ctx, p->mem);
     dfree(p->ctx, p->part);
+    dfree(p->ctx, p->wide);
     delete p;
 }
 
@@ -481,10 +612,26 @@ mure_status mure_tokens_attend(mure_tokens *t, mure_tokens_plan *p, const mure_t
         check_apart(c, orow, t->d, p->n_new, p->b.n_heads, "out");
         FAILIF((uintptr_t)lse % 4 != 0, c, MURE_ERR_INVALID_ARG, "lse is not aligned");
         CK(c, cudaSetDevice(c->device));
-        if (t->d.dtype == MURE_F32)
-            c->launches += launch_tokens_attend_rows(pool_of(t), p->b, t->d.dtype, t->d.form, p->n_new, qr, orow, lse, c->stream);
-        else
-            c->launches += launch_tokens_few(pool_of(t), p->b, p->few, t->d.dtype, t->d.form, qr, orow, lse, c->stream);
+        const mure_tokens_desc &d = t->d;
+        if (d.dtype == MURE_F32) {
+            c->launches += launch_tokens_attend_rows(pool_of(t), p->b, d.dtype, d.form, p->n_new, qr, orow, lse, c->stream);
+        } else {
+            c->launches += launch_tokens_few(pool_of(t), p->b, p->few, d.dtype, d.form, qr, orow, lse, c->stream);
+            if (d.form == MURE_FORM_SAME) {
+                c->launches += launch_tokens_chunk(pool_of(t), p->b, p->chunk, d.dtype, qr, orow, lse, d.n_pages, t->map_k, t->map_v,
+                                                   c->err_dev, c->wait_limit, c->stream);
+            } else if (p->n_wide > 0) {
+                TokPool w = pool_of(t);
+                const int64_t pool = p->n_wide * d.n_kv_heads * d.page_size * d.head_dim * 2;
+                w.k = p->wide;
+                w.v = static_cast<char *>(p->wide) + pool;
+                c->launches += launch_tokens_widen(pool_of(t), d.dtype, p->wide_pages, p->n_wide, w.k, w.v, c->stream);
+                TokBatch b = p->b;
+                b.table = p->wide_table;
+                c->launches += launch_tokens_chunk(w, b, p->chunk, d.dtype, qr, orow, lse, p->n_wide, p->map_k, p->map_v, c->err_dev,
+                                                   c->wait_limit, c->stream);
+            }
+        }
         check_launch(c);
     });
 }

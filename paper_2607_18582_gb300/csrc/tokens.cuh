@@ -1,6 +1,8 @@
 // Token caches: what the host lays out for a batch and the kernels read (not part of the ABI).
 #pragma once
 
+#include <cuda.h>
+
 #include "common.cuh"
 
 namespace mure {
@@ -72,6 +74,23 @@ int few_blocks();                     // blocks that run at a time
 int few_part_floats(int d);
 int launch_tokens_few(const TokPool &pool, const TokBatch &b, const TokWork &w, int dtype, int form, TokRows q, TokRows out,
                       float *lse, cudaStream_t s);
+
+// Pieces of the kernel for chunks: up to 256 rows over tiles of 128 cells.
+constexpr int kChunkRows = 256, kChunkTile = 128, kChunkDim = 128;
+struct TokChunk {
+    TokWork w;
+    float *ml = nullptr;              // partial results' maxima and sums
+    const TokItem *cut = nullptr;     // [n_cut] the first part of every cut unit
+    int n_cut = 0;
+};
+int chunk_blocks();
+int chunk_box(int page_size);         // cells of a box its copies take (and its tiles' alignment)
+int64_t chunk_part_floats(int d);
+bool chunk_map(CUtensorMap &map, void *pool, int dtype, int hk, int d, int page_size, int64_t n_pages);
+int launch_tokens_chunk(const TokPool &pool, const TokBatch &b, const TokChunk &c, int dtype, TokRows q, TokRows out, float *lse,
+                        int64_t n_pages, const CUtensorMap &map_k, const CUtensorMap &map_v, int *err, int64_t spin, cudaStream_t s);
+// E4M3 pages pages[0 .. n_list) as pages 0 .. n_list - 1 of 16-bit pools k and v.
+int launch_tokens_widen(const TokPool &pool, int dtype, const int32_t *pages, int64_t n_list, void *k, void *v, cudaStream_t s);
 
 int launch_tokens_append(const TokPool &pool, const TokBatch &b, int dtype, int form, TokRows k, TokRows v, int64_t tiles,
                          cudaStream_t s);
