@@ -10,7 +10,7 @@
 // tile's products.  Warps:
 //   0-3, 4-7  softmax of the two row tiles, a thread per row: no shuffles; they also fetch Q and
 //             write the rows out;
-//   8         issues the MMAs;
+//   8, 11     issue the MMAs of either row tile;
 //   9, 10     copy K and V tiles by tensor maps, a box per page (or 128 cells of a larger page).
 // The maximum a row is scaled by moves only when it grows by more than 2^8 (powers up to 2^8 lose
 // nothing in 16 bits), so O is hardly ever rescaled; where it is, S's arrival has shown that every
@@ -27,7 +27,7 @@ namespace mure {
 
 namespace {
 
-constexpr int kThreads = 352;
+constexpr int kThreads = 384;
 constexpr int kCells = kChunkTile;        // cells of a tile
 constexpr uint32_t kPanel = 128 * 128;    // bytes of 128 rows of 64 values
 
@@ -174,10 +174,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
     using C = Chunk<DP>;
     extern __shared__ char smem_raw[];
     // stages 0 .. kStages / 2 - 1 hold K tiles, the others V tiles
-    __shared__ __align__(8) uint64_t bar_full[C::kStages], bar_empty[C::kStages], bar_q[2], bar_s[2], bar_p[2][2], bar_o[2], bar_drain;
+    __shared__ __align__(8) uint64_t bar_full[C::kStages], bar_empty[C::kStages], bar_q[2], bar_s[2], bar_p[2][2], bar_o[2], bar_turn[2], bar_drain[2];
     __shared__ uint32_t tmem_sh;
     __shared__ WaitCtl ctl_sh;
-    __shared__ TokItem item_sh[11];           // each warp's piece of work
+    __shared__ TokItem item_sh[12];           // each warp's piece of work
     __shared__ int page_sh[2][2][16];         // copying warps: the pages of a tile's boxes
     volatile WaitCtl *ctl = &ctl_sh;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
         ctl_sh.limit = p.spin > 0 ? p.spin : kSpin;
         for (int i = 0; i < C::kStages; ++i) {
             mbar_init(smem_u32(&bar_full[i]), 1);
-            mbar_init(smem_u32(&bar_empty[i]), 1);
+            mbar_init(smem_u32(&bar_empty[i]), 2);      // the products of both row tiles
         }
         for (int h = 0; h < 2; ++h) {
             mbar_init(smem_u32(&bar_q[h]), 4);
@@ -202,8 +202,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
             mbar_init(smem_u32(&bar_p[h][0]), 4);
             mbar_init(smem_u32(&bar_p[h][1]), 4);
             mbar_init(smem_u32(&bar_o[h]), 1);
+            mbar_init(smem_u32(&bar_turn[h]), 1);
+            mbar_init(smem_u32(&bar_drain[h]), 1);
         }
-        mbar_init(smem_u32(&bar_drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     fence_before();
@@ -211,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
     fence_after();
     const uint32_t tmem = tmem_sh;
     const int it0 = p.w.first[blockIdx.x], it1 = p.w.first[blockIdx.x + 1];
-    const TokItem &w = item_sh[warp < 11 ? warp : 0];
+    const TokItem &w = item_sh[warp];
     auto take = [&](int it) {
         __syncwarp();
         if (lane < (int)sizeof(TokItem) / 4)
@@ -239,21 +240,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
             constexpr int kLanes = DP / 8, kPer = 32 / kLanes;
             const int chunk = lane % kLanes;
             const int64_t q_at = real ? (w.row0 + row / p.b.group) * p.q.ts + (w.h * p.b.group + row % p.b.group) * p.q.hs : -1;
+            uint4 v[kLanes];
 #pragma unroll
-            for (int i = 0; i < 32; i += kPer) {
-                const int64_t off = __shfl_sync(0xffffffffu, q_at, i + lane / kLanes);
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (off >= 0 && chunk * 8 < D) {
-                    const T *q = reinterpret_cast<const T *>(p.q.p) + off + chunk * 8;
-                    if (p.q.vec) v = __ldg(reinterpret_cast<const uint4 *>(q));
-                    else {
-                        const uint16_t *u = reinterpret_cast<const uint16_t *>(q);
-                        v.x = u[0] | (uint32_t)u[1] << 16; v.y = u[2] | (uint32_t)u[3] << 16;
-                        v.z = u[4] | (uint32_t)u[5] << 16; v.w = u[6] | (uint32_t)u[7] << 16;
-                    }
+            for (int i = 0; i < kLanes; ++i) {                       // (all on their way before the first is stored)
+                const int64_t off = __shfl_sync(0xffffffffu, q_at, i * kPer + lane / kLanes);
+                v[i] = make_uint4(0, 0, 0, 0);
+                if (off < 0 || chunk * 8 >= D) continue;
+                const T *q = reinterpret_cast<const T *>(p.q.p) + off + chunk * 8;
+                if (p.q.vec) v[i] = __ldg(reinterpret_cast<const uint4 *>(q));
+                else {
+                    const uint16_t *u = reinterpret_cast<const uint16_t *>(q);
+                    v[i].x = u[0] | (uint32_t)u[1] << 16; v[i].y = u[2] | (uint32_t)u[3] << 16;
+                    v[i].z = u[4] | (uint32_t)u[5] << 16; v[i].w = u[6] | (uint32_t)u[7] << 16;
                 }
-                st_shared16(qs + (chunk >> 3) * kPanel + sw128_off((r & ~31) + i + lane / kLanes, chunk & 7), v);
             }
+#pragma unroll
+            for (int i = 0; i < kLanes; ++i)
+                st_shared16(qs + (chunk >> 3) * kPanel + sw128_off((r & ~31) + i * kPer + lane / kLanes, chunk & 7), v[i]);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bar_q[h]));
@@ -324,19 +327,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                     tmem_st16(to, y);
                 };
                 // P lies over the scores of the second 64 cells, which go first; those of the first 64 are
-                // fetched once more.  The product with the second 64 starts as soon as they are there.
+                // fetched once more.  The products with all but cells 32 .. 63 start as soon as those are there.
                 uint32_t x[32];
                 tmem_ld32(tS, x);
                 powers(s, tP + 32);
                 powers(s + 32, tP + 48);
                 tmem_wait_ld();
+                mask(x, 0, 32);
+                powers(x, tP);
+                tmem_ld32(tS + 32, x);
                 tmem_wait_st();
                 fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&bar_p[h][1]));
-                mask(x, 0, 32);
-                powers(x, tP);
-                tmem_ld32(tS + 32, x);
                 tmem_wait_ld();
                 mask(x, 32, 32);
                 powers(x, tP + 16);
@@ -454,89 +457,115 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 }
             }
         }
-    } else if (warp == 8) {
-        // ---------------------------------------------------------------- MMA issue --
-        uint32_t n_q[2] = {0, 0}, n_p[2] = {0, 0}, n_k = 0, n_v = 0;  // phases; K and V tiles taken
+    } else if (warp == 8 || warp == 11) {
+        // ------------------------------------------- MMA issue: warp 8 rows 0-127, warp 11 the others --
+        // The two take turns, a turn being a tile's P V and the next tile's Q K^T, handed over half-way
+        // through the latter: each row tile's softmax then runs while the other one's products do.
+        // Measured per 256 rows x 128 cells (D = 128; 2,270 cycles of tensor pipe): one warp for both 3,200
+        // cycles (what it does between two batches leaves the pipe empty), two warps without turns 3,300
+        // (the pipe interleaves them and both softmaxes wait at a time), with turns 2,800.
         constexpr uint32_t NS = C::kStages / 2;
+        const int h = warp == 8 ? 0 : 1;
+        uint32_t n_q = 0, n_p = 0, n_turn = 0, n_k = 0, n_v = 0;     // phases; K and V tiles taken
         const uint32_t id_s = idesc_16<T>(kCells, false), id_o = idesc_16<T>((D + 15) & ~15, true);
+        const uint32_t tS = tmem + h * 128, tP = tS + 64, tO = tmem + 256 + h * 128;
         const int ks_q = (D + 15) / 16;
+        const uint64_t qd = sw128_desc(q_smem + h * C::kPanels * kPanel);
         bool ok = true;
-        auto scores = [&](int h, uint32_t stage, bool last) {
-            const uint64_t a = sw128_desc(q_smem + h * C::kPanels * kPanel), b = sw128_desc(ring + stage * C::kStage);
+        auto scores = [&](uint32_t stage, bool pass) {               // S = Q K^T from a stage; pass: the turn, half-way
+            const uint64_t b = sw128_desc(ring + stage * C::kStage);
             if (elect_one()) {
+                if (ks_q == DP / 16) {
 #pragma unroll
-                for (int ks = 0; ks < DP / 16; ++ks)
-                    if (ks < ks_q) {
+                    for (int ks = 0; ks < DP / 16; ++ks) {
                         const uint64_t o = (uint64_t)((ks >> 2) * (kPanel >> 4) + 2 * (ks & 3));
-                        mma_ss(tmem + h * 128, a + o, b + o, id_s, ks > 0);
+                        mma_ss(tS, qd + o, b + o, id_s, ks > 0);
+                        if (ks == DP / 32 - 1 && pass) mbar_arrive(smem_u32(&bar_turn[1 - h]));
                     }
+                } else {
+                    for (int ks = 0; ks < ks_q; ++ks) {
+                        const uint64_t o = (uint64_t)((ks >> 2) * (kPanel >> 4) + 2 * (ks & 3));
+                        mma_ss(tS, qd + o, b + o, id_s, ks > 0);
+                        if (ks == (ks_q - 1) / 2 && pass) mbar_arrive(smem_u32(&bar_turn[1 - h]));
+                    }
+                }
                 mma_commit(smem_u32(&bar_s[h]));
-                if (last) mma_commit(smem_u32(&bar_empty[stage]));
+                mma_commit(smem_u32(&bar_empty[stage]));
             }
             __syncwarp();
         };
         for (int it = it0; it < it1 && ok; ++it) {
             take(it);
-            const int rows = w.rows, t0 = w.t0, t1 = w.t1, halves = rows > 128 ? 2 : 1;
-            for (int t = t0; t < t1 && ok; ++t) {
+            const int rows = w.rows, t0 = w.t0, t1 = w.t1;
+            if (h * 128 >= rows) {
+                // no rows here: the stages go by one at a time (a barrier's parity names a phase only to
+                // a waiter that is at most one behind)
+                for (int t = t0; t < t1 && ok; ++t, ++n_k, ++n_v) {
+                    ok = warp_wait_phase(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
+                    if (ok && lane == 0) mbar_arrive(smem_u32(&bar_empty[n_k % NS]));
+                    ok = ok && warp_wait_phase(smem_u32(&bar_full[NS + n_v % NS]), (n_v / NS) & 1, ctl);
+                    if (ok && lane == 0) mbar_arrive(smem_u32(&bar_empty[NS + n_v % NS]));
+                }
+                continue;
+            }
+            ok = warp_wait_phase(smem_u32(&bar_q[h]), n_q++ & 1, ctl);
+            if (!ok || t1 <= t0) continue;                           // (rows without cells: their Q is not read)
+            ok = warp_wait_phase(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
+            if (!ok) break;
+            fence_after();
+            scores(n_k % NS, false);
+            ++n_k;
+            for (int t = t0; t < t1; ++t, ++n_v) {
                 const TileCells tc = tile_cells(w, t, p.box);
                 const int ks_v = min(kCells, tc.end - tc.start + 15) / 16;   // cells past the end have probability 0
                 const uint32_t v_stage = NS + n_v % NS;
-                if (t == t0) {
-                    ok = warp_wait_phase(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
-                    for (int h = 0; h < halves && ok; ++h) {
-                        ok = warp_wait_phase(smem_u32(&bar_q[h]), n_q[h]++ & 1, ctl);
-                        if (!ok) break;
-                        fence_after();
-                        scores(h, n_k % NS, h == halves - 1);
-                    }
-                    ++n_k;
-                }
-                ok = ok && warp_wait_phase(smem_u32(&bar_full[v_stage]), (n_v / NS) & 1, ctl);
                 const bool more = t + 1 < t1;
                 const uint64_t b = mn_desc(ring + v_stage * C::kStage);
-                for (int h = 0; h < halves && ok; ++h) {
-                    bool acc = t > t0;
+                // (turn n of warp 8 follows turn n - 1 of warp 11, turn n of warp 11 turn n of warp 8)
+                ok = warp_wait_phase(smem_u32(&bar_full[v_stage]), (n_v / NS) & 1, ctl) &&
+                     warp_wait_phase(smem_u32(&bar_p[h][1]), n_p & 1, ctl) &&
+                     (rows <= 128 || (h == 0 && n_turn == 0) || warp_wait_phase(smem_u32(&bar_turn[h]), (n_turn - (h == 0)) & 1, ctl));
+                if (!ok) break;
+                fence_after();
+                auto product = [&](int ks, uint32_t acc) { mma_ts(tO, tP + ks * 8, b + (uint64_t)(ks * (2048 >> 4)), id_o, acc); };
+                if (elect_one()) {                                   // cells 64 .. 127 and 0 .. 31
+                    if (ks_v == 8) {
+                        product(4, t > t0);
 #pragma unroll
-                    for (int half = 1; half >= 0; --half) {
-                        ok = ok && warp_wait_phase(smem_u32(&bar_p[h][half]), n_p[h] & 1, ctl);
-                        if (!ok) break;
-                        fence_after();
-                        if (elect_one()) {
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const int ks = half * 4 + k;
-                                if (ks < ks_v)
-                                    mma_ts(tmem + 256 + h * 128, tmem + h * 128 + 64 + ks * 8, b + (uint64_t)(ks * (2048 >> 4)), id_o,
-                                           acc || k > 0);
-                            }
-                            if (half == 0 && h == halves - 1) mma_commit(smem_u32(&bar_empty[v_stage]));
-                            if (half == 0 && !more) mma_commit(smem_u32(&bar_o[h]));
-                        }
-                        __syncwarp();
-                        acc = acc || ks_v > 4;
-                    }
-                    if (!ok) break;
-                    ++n_p[h];
-                    if (more) {
-                        if (h == 0) {
-                            ok = warp_wait_phase(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
-                            if (!ok) break;
-                            fence_after();
-                        }
-                        scores(h, n_k % NS, h == halves - 1);
+                        for (int ks = 5; ks < 10; ++ks) product(ks & 7, 1);
+                    } else {
+                        for (int ks = 4; ks < ks_v; ++ks) product(ks, t > t0 || ks > 4);
+                        for (int ks = 0; ks < min(ks_v, 2); ++ks) product(ks, t > t0 || ks > 0 || ks_v > 4);
                     }
                 }
-                ++n_v;
-                if (more) ++n_k;
+                __syncwarp();
+                ok = warp_wait_phase(smem_u32(&bar_p[h][0]), n_p & 1, ctl);
+                if (!ok) break;
+                ++n_p;
+                fence_after();
+                if (elect_one()) {                                   // cells 32 .. 63
+                    if (ks_v > 2) product(2, 1);
+                    if (ks_v > 3) product(3, 1);
+                    mma_commit(smem_u32(&bar_empty[v_stage]));
+                    if (!more) mma_commit(smem_u32(&bar_o[h]));
+                }
+                __syncwarp();
+                if (more) {
+                    ok = warp_wait_phase(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
+                    if (!ok) break;
+                    fence_after();
+                    scores(n_k % NS, rows > 128);
+                    ++n_k;
+                } else if (rows > 128 && lane == 0) {
+                    mbar_arrive(smem_u32(&bar_turn[1 - h]));
+                }
+                n_turn += rows > 128;
             }
-            // rows without cells: their Q is not read
-            for (int h = 0; h < halves && ok && t1 <= t0; ++h) ok = warp_wait_phase(smem_u32(&bar_q[h]), n_q[h]++ & 1, ctl);
         }
         // products in flight finish before shared and tensor memory are released
-        if (elect_one()) mma_commit(smem_u32(&bar_drain));
+        if (elect_one()) mma_commit(smem_u32(&bar_drain[h]));
         __syncwarp();
-        wait_phase_drain(smem_u32(&bar_drain), 0);
+        wait_phase_drain(smem_u32(&bar_drain[h]), 0);
     } else if (warp == 9 || warp == 10) {
         // -------------------------------------------- copies: warp 9 K tiles, warp 10 V tiles --
         constexpr uint32_t NS = C::kStages / 2;

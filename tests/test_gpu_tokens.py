@@ -305,6 +305,17 @@ def test_rows_without_cells(M, ctx, dtype, d):
         Batch(M, ctx, new, pos, kv, 4, 2, d, 16, dtype, "same", window=window, sinks=sinks).check()
 
 
+@pytest.mark.parametrize("dtype,form", [("bf16", "same"), ("f16", "e4m3")])
+def test_many_chunks_of_all_lengths(M, ctx, dtype, form):
+    """More pieces of work than blocks, short ones (one tile of rows) before and after long ones."""
+    rng = np.random.default_rng(5)
+    new = [int(x) for x in rng.integers(1, 150, 300)]
+    past = [int(x) for x in rng.integers(0, 1500, 300)]
+    t = Batch(M, ctx, new, past, [a + b for a, b in zip(new, past)], 12, 4, 64, 32, dtype, form)
+    for _ in range(3):
+        t.check()
+
+
 @pytest.mark.parametrize("scale", [1.0, 0.01, 3.0])
 def test_scale(M, ctx, scale):
     Batch(M, ctx, [70, 1], [40, 300], [110, 301], 4, 2, 64, 16, "bf16", "same", scale=scale).check()
