@@ -1,4 +1,4 @@
-// Token caches: attention of few rows (a decoding step's single tokens) in 16-bit types.
+// Token caches: attention of few rows (a decoding step's single tokens), and of any rows in fp32.
 //
 // A sequence's cells are read once per cached head, all query heads of the group as the 16 rows of
 // one mma tile, so the kernel is bound by device memory: 4 D flops per row and cell against
@@ -10,6 +10,8 @@
 //     own, and a ring of cp.async stages of its own: no barrier in the loop;
 //   - e4m3 codes are widened in registers, their scales applied to the scores and (for bf16) the
 //     probabilities in fp32, so the products take exact values.
+// fp32 rows take the same way with TF32 products: every operand is split in two TF32 halves, a = a_hi + a_lo,
+// and a product is a_hi b_hi + a_hi b_lo + a_lo b_hi (codes are TF32 values as they are: two products).
 // The running maximum moves only when it grows by more than 2^8: the sums then need no rescaling in
 // nearly all steps, and powers up to 2^8 lose nothing in either type.
 #include <type_traits>
@@ -26,19 +28,23 @@ constexpr int kAlign = 16;
 
 template <class T, bool E4M3, int DP>
 struct Few {
-    static constexpr int kElt = E4M3 ? 1 : 2;
+    static constexpr bool kF32 = std::is_same<T, float>::value;
+    static constexpr int kElt = E4M3 ? 1 : (int)sizeof(T);
     static constexpr int kRow = DP * kElt;                                   // bytes of a staged row
-    static constexpr int WK = (4096 / kRow < 16) ? 16 : (4096 / kRow > 64 ? 64 : 4096 / kRow);   // cells of a warp's step
+    static constexpr int kLeast = kF32 ? 8 : 16;
+    static constexpr int WK = (4096 / kRow < kLeast) ? kLeast : (4096 / kRow > 64 ? 64 : 4096 / kRow);   // cells of a warp's step
     static constexpr int kTile = kWarps * WK;
     static constexpr int kScaleBytes = E4M3 ? 2 * WK : 0;
     static constexpr int kStage = 2 * WK * kRow + kScaleBytes;               // K rows, V rows, scales
     static constexpr int kStageAl = (kStage + 127) / 128 * 128;
     static constexpr int kJoin = kWarps * kFewRows * (DP + 2) * 4;
     static constexpr int kRing = kWarps * kStages * kStageAl;
-    // the fragments of q: in registers, for 256 values in shared memory (one copy for all warps)
-    static constexpr bool kSharedQ = DP > 128;
-    static constexpr int kQ = kSharedQ ? DP / 16 * 32 * 16 : 0;
+    // the fragments of q: in registers; for 256 values and for fp32 in shared memory (one copy for all warps)
+    static constexpr bool kSharedQ = DP > 128 || kF32;
+    static constexpr int kQSteps = kF32 ? DP / 8 : DP / 16;
+    static constexpr int kQ = kSharedQ ? kQSteps * 32 * 16 : 0;
     static constexpr int kSmem = (kRing > kJoin ? kRing : kJoin) + kQ;
+    static constexpr int kBlocks = kSmem > 110 * 1024 ? 1 : 2;               // per SM
 };
 
 struct FewParams {
@@ -52,12 +58,15 @@ struct FewParams {
 __device__ __forceinline__ uint32_t su32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 // Byte `byte` of staged row `row`: the eight 16-byte chunks of a 128-byte line are exchanged by the
-// row's (rows of 64 bytes: the line's) number, so that ldmatrix meets no bank conflict.
-template <int ROW>
-__device__ __forceinline__ uint32_t swz(int row, int byte)
+// row's (rows of 64 bytes: the line's) number, so that the loads meet no bank conflict: ldmatrix reads a
+// chunk of eight rows; with fp32 cells eight lanes read four chunks of two rows of K, or two chunks of
+// four rows, each second one, of V.
+template <int ROW, bool F32>
+__device__ __forceinline__ uint32_t swz(int row, int byte, bool v)
 {
     const uint32_t o = row * ROW + byte;
-    return o ^ (uint32_t)(((ROW >= 128 ? row : row >> 1) & 7) << 4);
+    const int x = F32 ? (v ? row & 6 : (row & 1) << 2 | (row >> 1 & 3)) : (ROW >= 128 ? row : row >> 1) & 7;
+    return o ^ (uint32_t)(x << 4);
 }
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool on)
@@ -84,7 +93,57 @@ __device__ __forceinline__ void ldsm4t(uint32_t a, uint32_t *r)
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
 }
 
+__device__ __forceinline__ float4 lds16(uint32_t a)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds4(uint32_t a)
+{
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+
+// TF32 halves: the high one rounded to the nearest, the low one the exact remainder (the product reads its
+// upper bits).
+__device__ __forceinline__ void halves(float x, uint32_t &hi, uint32_t &lo)
+{
+    hi = (__float_as_uint(x) + 0x1000u) & 0xFFFFE000u;
+    lo = __float_as_uint(x - __uint_as_float(hi));
+}
+
+__device__ __forceinline__ void mma_tf32(float *c, const uint32_t *a, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// c += a b, the operands in halves (b exact in TF32: EXACT); b0, b1 as fp32.
+template <bool EXACT>
+__device__ __forceinline__ void mma_f32(float *c, const uint32_t *hi, const uint32_t *lo, float b0, float b1)
+{
+    if (EXACT) {
+        mma_tf32(c, lo, __float_as_uint(b0), __float_as_uint(b1));
+        mma_tf32(c, hi, __float_as_uint(b0), __float_as_uint(b1));
+    } else {
+        uint32_t h0, l0, h1, l1;
+        halves(b0, h0, l0);
+        halves(b1, h1, l1);
+        mma_tf32(c, lo, h0, h1);
+        mma_tf32(c, hi, l0, l1);
+        mma_tf32(c, hi, h0, h1);
+    }
+}
+
 template <class T> struct Mma;
+template <> struct Mma<float> {     // (for the names alone: fp32 rows have products of their own)
+    static __device__ __forceinline__ void go(float *, const uint32_t *, uint32_t, uint32_t) {}
+    static __device__ __forceinline__ uint32_t pack(float, float) { return 0; }
+    static __device__ __forceinline__ uint32_t widen(uint32_t) { return 0; }
+};
 template <> struct Mma<__nv_bfloat16> {
     static __device__ __forceinline__ void go(float *c, const uint32_t *a, uint32_t b0, uint32_t b1)
     {
@@ -152,10 +211,10 @@ __device__ __forceinline__ uint32_t load2(const T *p, int vec)
 }
 
 template <class T, bool E4M3, int DP>
-__global__ void __launch_bounds__(kWarps * 32, DP == 256 ? 1 : 2) k_tokens_few(FewParams p)
+__global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_tokens_few(FewParams p)
 {
     using F = Few<T, E4M3, DP>;
-    constexpr int KS = DP / 16, NT = F::WK / 8, ND = DP / 8, WK = F::WK;
+    constexpr int KS = F::kQSteps, NT = F::WK / 8, ND = DP / 8, WK = F::WK;
     extern __shared__ __align__(128) char smem[];
     __shared__ TokItem w;
     __shared__ int last;
@@ -191,8 +250,10 @@ __global__ void __launch_bounds__(kWarps * 32, DP == 256 ? 1 : 2) k_tokens_few(F
                 range(tile, start, begin, end);
                 const uint32_t st = ring + slot * F::kStageAl;
                 constexpr int CH = F::kRow / 16;               // chunks of a staged row
-                constexpr int PER = 32 / CH;                   // rows that a warp's instruction covers
-                const int byte = lane % CH * 16, r0 = lane / CH;
+                constexpr int PER = CH < 32 ? 32 / CH : 1;     // rows that a warp's instruction covers,
+                constexpr int REP = CH > 32 ? CH / 32 : 1;     // or instructions a row takes
+                static_assert(PER * CH == 32 || REP * 32 == CH, "rows and lanes do not divide");
+                const int r0 = CH < 32 ? lane / CH : 0;
 #pragma unroll
                 for (int grp = 0; grp < WK / 8; ++grp) {
                     const int page = __shfl_sync(0xffffffffu, page_of_group, grp);
@@ -202,22 +263,23 @@ __global__ void __launch_bounds__(kWarps * 32, DP == 256 ? 1 : 2) k_tokens_few(F
                     const char *vb = static_cast<const char *>(p.pool.v) + row * row_bytes;
                     if (j0 + 7 < begin || j0 >= end) kb = static_cast<const char *>(p.pool.k), vb = static_cast<const char *>(p.pool.v);
 #pragma unroll
-                    for (int i = 0; i < 8; i += PER) {
-                        const int r = i + r0;
+                    for (int e = 0; e < 8 * REP; e += PER) {
+                        const int r = e / REP + r0, byte = (REP > 1 ? lane + e % REP * 32 : lane % CH) * 16;
                         const bool in = j0 + r >= begin && j0 + r < end;
-                        const uint32_t o = swz<F::kRow>(grp * 8 + r, byte);
+                        const uint32_t o = swz<F::kRow, F::kF32 && !E4M3>(grp * 8 + r, byte, false);
+                        const uint32_t ov = WK * F::kRow + swz<F::kRow, F::kF32 && !E4M3>(grp * 8 + r, byte, true);
                         if (!E4M3 || D % 16 == 0) {
                             const bool on = in && byte < row_bytes;
                             const int64_t off = on ? (int64_t)r * row_bytes + byte : 0;
                             cp16(st + o, kb + off, on);
-                            cp16(st + WK * F::kRow + o, vb + off, on);
+                            cp16(st + ov, vb + off, on);
                         } else {                               // rows of codes at 8-byte boundaries
 #pragma unroll
                             for (int q = 0; q < 16; q += 8) {
                                 const bool on = in && byte + q < row_bytes;
                                 const int64_t off = on ? (int64_t)r * row_bytes + byte + q : 0;
                                 cp8(st + o + q, kb + off, on);
-                                cp8(st + WK * F::kRow + o + q, vb + off, on);
+                                cp8(st + ov + q, vb + off, on);
                             }
                         }
                     }
@@ -255,13 +317,20 @@ __global__ void __launch_bounds__(kWarps * 32, DP == 256 ? 1 : 2) k_tokens_few(F
                          (on ? (int64_t)(w.row0 + r / p.b.group) * p.q.ts + (int64_t)(w.h * p.b.group + r % p.b.group) * p.q.hs : 0);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                // the order of a row's values within a K16 step only has to be that of the codes
-                const int d0 = ks * 16 + (E4M3 ? 4 * t : 2 * t), d1 = d0 + (E4M3 ? 2 : 8);
-                const uint32_t x0 = on && d0 < D ? load2(q + d0, p.q.vec) : 0u;
-                const uint32_t x1 = on && d1 < D ? load2(q + d1, p.q.vec) : 0u;
+                // the order of a row's values within a step only has to be that of the cells' values
+                uint32_t x0, x1;
+                if constexpr (F::kF32) {
+                    const int d0 = ks / 2 * 16 + 4 * t + ks % 2 * 2;
+                    x0 = on && d0 < D ? __float_as_uint(q[d0]) : 0u;
+                    x1 = on && d0 < D ? __float_as_uint(q[d0 + 1]) : 0u;
+                } else {
+                    const int d0 = ks * 16 + (E4M3 ? 4 * t : 2 * t), d1 = d0 + (E4M3 ? 2 : 8);
+                    x0 = on && d0 < D ? load2(q + d0, p.q.vec) : 0u;
+                    x1 = on && d1 < D ? load2(q + d1, p.q.vec) : 0u;
+                }
                 if (!F::kSharedQ) {
-                    qf[ks][half] = x0;
-                    qf[ks][2 + half] = x1;
+                    qf[F::kSharedQ ? 0 : ks][half] = x0;
+                    qf[F::kSharedQ ? 0 : ks][2 + half] = x1;
                 } else if (warp == 0) {
                     uint32_t *f = reinterpret_cast<uint32_t *>(q_shared + ks * 32 + lane);
                     f[half] = x0;
@@ -300,12 +369,40 @@ __global__ void __launch_bounds__(kWarps * 32, DP == 256 ? 1 : 2) k_tokens_few(F
             };
             float s[NT][4];
 #pragma unroll
+            for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+            if constexpr (F::kF32) {
+#pragma unroll
+                for (int i = 0; i < DP / 16; ++i) {            // 16 values of a row: two steps
+                    uint32_t hi[2][4], lo[2][4];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint4 a = q_shared[(2 * i + e) * 32 + lane];
+                        halves(__uint_as_float(a.x), hi[e][0], lo[e][0]);
+                        halves(__uint_as_float(a.y), hi[e][1], lo[e][1]);
+                        halves(__uint_as_float(a.z), hi[e][2], lo[e][2]);
+                        halves(__uint_as_float(a.w), hi[e][3], lo[e][3]);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        float4 b;
+                        if (E4M3) {
+                            const uint32_t c = lds4(st + swz<F::kRow, false>(n * 8 + g, i * 16, false) + 4 * t);
+                            const float2 u = e4m3_values((uint16_t)c), v = e4m3_values((uint16_t)(c >> 16));
+                            b = make_float4(u.x, u.y, v.x, v.y);
+                        } else {
+                            b = lds16(st + swz<F::kRow, true>(n * 8 + g, (4 * i + t) * 16, false));
+                        }
+                        mma_f32<E4M3>(s[n], hi[0], lo[0], b.x, b.y);
+                        mma_f32<E4M3>(s[n], hi[1], lo[1], b.z, b.w);
+                    }
+                }
+            } else {
+#pragma unroll
             for (int n = 0; n < NT; ++n) {
-                s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
 #pragma unroll
                 for (int kp = 0; kp < F::kRow / 64; ++kp) {        // four 16-byte chunks of eight rows
                     uint32_t r[4];
-                    ldsm4(st + swz<F::kRow>(n * 8 + (lane & 7), (kp * 4 + (lane >> 3)) * 16), r);
+                    ldsm4(st + swz<F::kRow, false>(n * 8 + (lane & 7), (kp * 4 + (lane >> 3)) * 16, false), r);
                     if (E4M3) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
@@ -315,6 +412,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP == 256 ? 1 : 2) k_tokens_few(F
                         Mma<T>::go(s[n], qfrag(2 * kp + 1, qa), r[2], r[3]);
                     }
                 }
+            }
             }
             // scores in powers of two, masked
             const bool open = start >= begin && start + WK <= end && start + WK - 1 <= p_lo &&
@@ -373,6 +471,47 @@ __global__ void __launch_bounds__(kWarps * 32, DP == 256 ? 1 : 2) k_tokens_few(F
                 l[1] += s[n][2] + s[n][3];
             }
             const uint32_t vst = st + WK * F::kRow;
+            if constexpr (F::kF32) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {                 // eight cells: the step's cells 2t and 2t + 1 are this lane's
+                    float *x = s[n];
+                    if (E4M3) {
+                        const uint32_t two = *reinterpret_cast<const uint16_t *>(sc + WK + n * 8 + 2 * t);
+                        const float f0 = scale_of(two & 255u), f1 = scale_of(two >> 8);
+                        if (!open) {                         // a masked cell's scale may be anything
+                            const uint32_t b = seen >> (4 * n);
+                            x[0] = b & 1 ? x[0] * f0 : 0.f; x[1] = b & 2 ? x[1] * f1 : 0.f;
+                            x[2] = b & 4 ? x[2] * f0 : 0.f; x[3] = b & 8 ? x[3] * f1 : 0.f;
+                        } else {
+                            x[0] *= f0; x[1] *= f1; x[2] *= f0; x[3] *= f1;
+                        }
+                    }
+                    uint32_t hi[4], lo[4];
+                    halves(x[0], hi[0], lo[0]);
+                    halves(x[2], hi[1], lo[1]);
+                    halves(x[1], hi[2], lo[2]);
+                    halves(x[3], hi[3], lo[3]);
+#pragma unroll
+                    for (int J = 0; J < DP / 32; ++J) {        // 32 values of a row: lane group g has 4g .. 4g + 3
+                        float4 b0, b1;
+                        if (E4M3) {
+                            const uint32_t c0 = lds4(vst + swz<F::kRow, false>(n * 8 + 2 * t, (2 * J + g / 4) * 16, true) + g % 4 * 4);
+                            const uint32_t c1 = lds4(vst + swz<F::kRow, false>(n * 8 + 2 * t + 1, (2 * J + g / 4) * 16, true) + g % 4 * 4);
+                            const float2 u0 = e4m3_values((uint16_t)c0), v0 = e4m3_values((uint16_t)(c0 >> 16));
+                            const float2 u1 = e4m3_values((uint16_t)c1), v1 = e4m3_values((uint16_t)(c1 >> 16));
+                            b0 = make_float4(u0.x, u0.y, v0.x, v0.y);
+                            b1 = make_float4(u1.x, u1.y, v1.x, v1.y);
+                        } else {
+                            b0 = lds16(vst + swz<F::kRow, true>(n * 8 + 2 * t, (8 * J + g) * 16, true));
+                            b1 = lds16(vst + swz<F::kRow, true>(n * 8 + 2 * t + 1, (8 * J + g) * 16, true));
+                        }
+                        mma_f32<E4M3>(o[4 * J], hi, lo, b0.x, b1.x);
+                        mma_f32<E4M3>(o[4 * J + 1], hi, lo, b0.y, b1.y);
+                        mma_f32<E4M3>(o[4 * J + 2], hi, lo, b0.z, b1.z);
+                        mma_f32<E4M3>(o[4 * J + 3], hi, lo, b0.w, b1.w);
+                    }
+                }
+            } else {
 #pragma unroll
             for (int kg = 0; kg < WK / 16; ++kg) {
                 uint32_t a[4], vs[2] = {0, 0};
@@ -406,7 +545,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP == 256 ? 1 : 2) k_tokens_few(F
 #pragma unroll
                 for (int c = 0; c < F::kRow / 16; c += 2) {
                     uint32_t r[4];
-                    ldsm4t(vst + swz<F::kRow>(kg * 16 + (lane & 15), (c + (lane >> 4)) * 16), r);
+                    ldsm4t(vst + swz<F::kRow, false>(kg * 16 + (lane & 15), (c + (lane >> 4)) * 16, true), r);
                     if (E4M3) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
@@ -425,6 +564,7 @@ __global__ void __launch_bounds__(kWarps * 32, DP == 256 ? 1 : 2) k_tokens_few(F
                     }
                 }
             }
+            }
             __syncwarp();
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -442,9 +582,9 @@ __global__ void __launch_bounds__(kWarps * 32, DP == 256 ? 1 : 2) k_tokens_few(F
             float *row = join + (warp * kFewRows + g + half * 8) * JR;
 #pragma unroll
             for (int i = 0; i < ND; ++i) {
-                const int d = E4M3 ? (i >> 1) * 16 + 4 * t + (i & 1) : i * 8 + 2 * t;
+                const int d = F::kF32 ? (i >> 2) * 32 + 8 * t + (i & 3) : E4M3 ? (i >> 1) * 16 + 4 * t + (i & 1) : i * 8 + 2 * t;
                 row[d] = o[i][2 * half];
-                row[d + (E4M3 ? 2 : 1)] = o[i][2 * half + 1];
+                row[d + (F::kF32 ? 4 : E4M3 ? 2 : 1)] = o[i][2 * half + 1];
             }
             if (t == 0) { row[DP] = m[half]; row[DP + 1] = l[half]; }
         }
@@ -562,15 +702,22 @@ int by_dim(const FewParams &p, cudaStream_t s)
 
 }  // namespace
 
-int few_tile_cells(int dtype, int form, int d)
+template <class T, bool E4M3>
+static FewShape shape_of(int d)
 {
-    (void)dtype;
-    if (form == MURE_FORM_E4M3)
-        return d <= 64 ? Few<__half, true, 64>::kTile : d <= 128 ? Few<__half, true, 128>::kTile : Few<__half, true, 256>::kTile;
-    return d <= 64 ? Few<__half, false, 64>::kTile : d <= 128 ? Few<__half, false, 128>::kTile : Few<__half, false, 256>::kTile;
+    if (d <= 64) return {Few<T, E4M3, 64>::kTile, Few<T, E4M3, 64>::kBlocks};
+    if (d <= 128) return {Few<T, E4M3, 128>::kTile, Few<T, E4M3, 128>::kBlocks};
+    return {Few<T, E4M3, 256>::kTile, Few<T, E4M3, 256>::kBlocks};
 }
 
-int few_blocks() { return 2 * sm_count(); }
+FewShape few_shape(int dtype, int form, int d)
+{
+    const bool e = form == MURE_FORM_E4M3;
+    FewShape f = dtype == MURE_F32 ? (e ? shape_of<float, true>(d) : shape_of<float, false>(d))
+                                   : (e ? shape_of<__half, true>(d) : shape_of<__half, false>(d));
+    f.blocks *= sm_count();
+    return f;
+}
 
 int few_part_floats(int d) { return kFewRows * ((d <= 64 ? 64 : d <= 128 ? 128 : 256) + 2); }
 
@@ -580,6 +727,7 @@ int launch_tokens_few(const TokPool &pool, const TokBatch &b, const TokWork &w, 
     if (w.blocks == 0) return 0;
     const FewParams p{pool, b, w, q, out, lse};
     const bool e = form == MURE_FORM_E4M3;
+    if (dtype == MURE_F32) return e ? by_dim<float, true>(p, s) : by_dim<float, false>(p, s);
     if (dtype == MURE_F16) return e ? by_dim<__half, true>(p, s) : by_dim<__half, false>(p, s);
     return e ? by_dim<__nv_bfloat16, true>(p, s) : by_dim<__nv_bfloat16, false>(p, s);
 }

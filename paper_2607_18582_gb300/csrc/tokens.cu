@@ -337,32 +337,32 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
     // attention: the pieces of the kernels that take this type
     const int group = b.n_heads / d.n_kv_heads;
     const bool wide = d.form == MURE_FORM_E4M3;
-    const Shape few_shape{kFewRows, few_tile_cells(d.dtype, d.form, d.head_dim), 16, few_blocks()};
+    const FewShape fshape = mure::few_shape(d.dtype, d.form, d.head_dim);
+    const Shape few_shape{kFewRows, fshape.tile, 16, fshape.blocks};
     const Shape chunk_shape{kChunkRows, kChunkTile, chunk_box(d.page_size), chunk_blocks()};
     std::vector<Unit> few, chunk;
     std::vector<int32_t> wide_table, wide_pages;
     std::unordered_map<int32_t, int32_t> wide_of;
-    if (d.dtype != MURE_F32)
-        for (int s = 0; s < n; ++s) {
-            const TokSeq &q = seq[s];
-            const int64_t rows = (int64_t)q.n_new * group;
-            FAILIF(rows > kMostPos, c, MURE_ERR_UNSUPPORTED, "sequence %d: more than 2^30 rows", s);
-            const bool as_chunk = d.head_dim <= kChunkDim && rows > (wide ? kFewRowsWide : kFewRows);
-            add_units(as_chunk ? chunk : few, q, s, d.n_kv_heads, group, b.window, b.sinks, as_chunk ? chunk_shape : few_shape);
-            FAILIF(few.size() + chunk.size() > ((size_t)1 << 27), c, MURE_ERR_UNSUPPORTED, "more than 2^27 pieces of work");
-            if (!as_chunk || !wide) continue;
-            // the pages that any of its rows reads
-            wide_table.resize(table.size(), 0);
-            const int64_t end = std::min<int64_t>(q.kv, (int64_t)q.pos + q.n_new);
-            const int64_t from = b.window > 0 ? std::max(0, q.pos - b.window + 1) : 0;
-            for (int64_t i = 0; i << page_log2 < end; ++i) {
-                if (((i + 1) << page_log2) <= from && i << page_log2 >= b.sinks) continue;
-                const int32_t id = table[q.table0 + i];
-                const auto at = wide_of.emplace(id, (int32_t)wide_pages.size());
-                if (at.second) wide_pages.push_back(id);
-                wide_table[q.table0 + i] = at.first->second;
-            }
+    for (int s = 0; s < n; ++s) {
+        const TokSeq &q = seq[s];
+        const int64_t rows = (int64_t)q.n_new * group;
+        FAILIF(rows > kMostPos, c, MURE_ERR_UNSUPPORTED, "sequence %d: more than 2^30 rows", s);
+        const bool as_chunk = d.dtype != MURE_F32 && d.head_dim <= kChunkDim && rows > (wide ? kFewRowsWide : kFewRows);
+        add_units(as_chunk ? chunk : few, q, s, d.n_kv_heads, group, b.window, b.sinks, as_chunk ? chunk_shape : few_shape);
+        FAILIF(few.size() + chunk.size() > ((size_t)1 << 27), c, MURE_ERR_UNSUPPORTED, "more than 2^27 pieces of work");
+        if (!as_chunk || !wide) continue;
+        // the pages that any of its rows reads
+        wide_table.resize(table.size(), 0);
+        const int64_t end = std::min<int64_t>(q.kv, (int64_t)q.pos + q.n_new);
+        const int64_t from = b.window > 0 ? std::max(0, q.pos - b.window + 1) : 0;
+        for (int64_t i = 0; i << page_log2 < end; ++i) {
+            if (((i + 1) << page_log2) <= from && i << page_log2 >= b.sinks) continue;
+            const int32_t id = table[q.table0 + i];
+            const auto at = wide_of.emplace(id, (int32_t)wide_pages.size());
+            if (at.second) wide_pages.push_back(id);
+            wide_table[q.table0 + i] = at.first->second;
         }
+    }
     const Shares fs = share(few, few_shape), cs = pack(chunk, chunk_shape);
     FAILIF(fs.items.size() + cs.items.size() > ((size_t)1 << 28), c, MURE_ERR_UNSUPPORTED, "more than 2^28 pieces of work");
 
@@ -613,24 +613,21 @@ mure_status mure_tokens_attend(mure_tokens *t, mure_tokens_plan *p, const mure_t
         FAILIF((uintptr_t)lse % 4 != 0, c, MURE_ERR_INVALID_ARG, "lse is not aligned");
         CK(c, cudaSetDevice(c->device));
         const mure_tokens_desc &d = t->d;
-        if (d.dtype == MURE_F32) {
-            c->launches += launch_tokens_attend_rows(pool_of(t), p->b, d.dtype, d.form, p->n_new, qr, orow, lse, c->stream);
-        } else {
-            c->launches += launch_tokens_few(pool_of(t), p->b, p->few, d.dtype, d.form, qr, orow, lse, c->stream);
-            if (d.form == MURE_FORM_SAME) {
-                c->launches += launch_tokens_chunk(pool_of(t), p->b, p->chunk, d.dtype, qr, orow, lse, d.n_pages, t->map_k, t->map_v,
-                                                   c->err_dev, c->wait_limit, c->stream);
-            } else if (p->n_wide > 0) {
-                TokPool w = pool_of(t);
-                const int64_t pool = p->n_wide * d.n_kv_heads * d.page_size * d.head_dim * 2;
-                w.k = p->wide;
-                w.v = static_cast<char *>(p->wide) + pool;
-                c->launches += launch_tokens_widen(pool_of(t), d.dtype, p->wide_pages, p->n_wide, w.k, w.v, c->stream);
-                TokBatch b = p->b;
+        c->launches += launch_tokens_few(pool_of(t), p->b, p->few, d.dtype, d.form, qr, orow, lse, c->stream);
+        if (p->chunk.w.blocks > 0) {
+            TokPool pool = pool_of(t);
+            TokBatch b = p->b;
+            const bool wide = d.form == MURE_FORM_E4M3;
+            if (wide) {
+                const int64_t bytes = p->n_wide * d.n_kv_heads * d.page_size * d.head_dim * 2;
+                pool.k = p->wide;
+                pool.v = static_cast<char *>(p->wide) + bytes;
                 b.table = p->wide_table;
-                c->launches += launch_tokens_chunk(w, b, p->chunk, d.dtype, qr, orow, lse, p->n_wide, p->map_k, p->map_v, c->err_dev,
-                                                   c->wait_limit, c->stream);
+                c->launches += launch_tokens_widen(pool_of(t), d.dtype, p->wide_pages, p->n_wide, pool.k, pool.v, c->stream);
             }
+            c->launches += launch_tokens_chunk(pool, b, p->chunk, d.dtype, qr, orow, lse, wide ? p->n_wide : d.n_pages,
+                                               wide ? p->map_k : t->map_k, wide ? p->map_v : t->map_v, c->err_dev, c->wait_limit,
+                                               c->stream);
         }
         check_launch(c);
     });

@@ -69,8 +69,10 @@ struct TokWork {
 
 // Rows of a piece and cells of a tile of the kernel for few rows.
 constexpr int kFewRows = 16;
-int few_tile_cells(int dtype, int form, int d);
-int few_blocks();                     // blocks that run at a time
+struct FewShape {
+    int tile, blocks;                 // cells of a tile; blocks that run at a time
+};
+FewShape few_shape(int dtype, int form, int d);
 int few_part_floats(int d);
 int launch_tokens_few(const TokPool &pool, const TokBatch &b, const TokWork &w, int dtype, int form, TokRows q, TokRows out,
                       float *lse, cudaStream_t s);
@@ -96,7 +98,5 @@ int launch_tokens_append(const TokPool &pool, const TokBatch &b, int dtype, int 
                          cudaStream_t s);
 int launch_tokens_read(const TokPool &pool, const TokBatch &b, int dtype, int form, int part, TokRows k, TokRows v,
                        int64_t tiles, cudaStream_t s);
-int launch_tokens_attend_rows(const TokPool &pool, const TokBatch &b, int dtype, int form, int64_t n_tokens, TokRows q,
-                              TokRows out, float *lse, cudaStream_t s);
 
 }  // namespace mure
