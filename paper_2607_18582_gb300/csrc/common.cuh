@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <string>
 #include <vector>
 
@@ -182,6 +183,19 @@ template <class Kern>
 inline void allow_dynamic_smem(Kern kern, int most)
 {
     cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+}
+
+// The same once per kernel and device, for kernels whose launches are short beside the call (1 us).
+template <auto Kern>
+inline void allow_dynamic_smem_once(int most)
+{
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev > 63) dev = 63;
+    const uint64_t bit = dev == 63 ? 0 : uint64_t(1) << dev;
+    if (bit && (done.load(std::memory_order_acquire) & bit)) return;
+    allow_dynamic_smem(Kern, most);
+    done.fetch_or(bit, std::memory_order_release);
 }
 
 // Stage v over R rows: z (optional) and y = post(act1(conv(x) + b)).  tmp: the stage's row

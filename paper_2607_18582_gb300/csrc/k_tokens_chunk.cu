@@ -659,7 +659,7 @@ __global__ void __launch_bounds__(256) k_tokens_join(const TokItem *cut, int DP,
 template <class T, int DP>
 int go(const ChunkParams &p, const TokChunk &c, cudaStream_t s)
 {
-    allow_dynamic_smem(k_tokens_chunk<T, DP>, Chunk<DP>::kSmem);
+    allow_dynamic_smem_once<k_tokens_chunk<T, DP>>(Chunk<DP>::kSmem);
     k_tokens_chunk<T, DP><<<p.w.blocks, kThreads, Chunk<DP>::kSmem, s>>>(p);
     if (c.n_cut == 0) return 1;
     k_tokens_join<T><<<dim3(c.n_cut, 32), 256, 0, s>>>(c.cut, DP, p.b, p.pool.d, p.out, p.lse, p.w.part, p.ml);

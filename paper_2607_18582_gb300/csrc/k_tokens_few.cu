@@ -687,7 +687,7 @@ template <class T, bool E4M3, int DP>
 int go(const FewParams &p, cudaStream_t s)
 {
     using F = Few<T, E4M3, DP>;
-    allow_dynamic_smem(k_tokens_few<T, E4M3, DP>, F::kSmem);
+    allow_dynamic_smem_once<k_tokens_few<T, E4M3, DP>>(F::kSmem);
     k_tokens_few<T, E4M3, DP><<<p.w.blocks, kWarps * 32, F::kSmem, s>>>(p);
     return 1;
 }

@@ -488,6 +488,8 @@ class Tokens:
         self.ctx, self.h, self.dtype, self.form = ctx, handle, dtype, form
         self.n_kv_heads, self.head_dim, self.page_size = desc.n_kv_heads, desc.head_dim, desc.page_size
         self.n_pages = desc.n_pages
+        import torch
+        self.torch_dtype, self.torch_device = _torch_dtype(dtype), torch.device("cuda", ctx.device)
         self._keep = keep          # the caller's pools
         ctx._children += 1
 
@@ -603,21 +605,23 @@ def _leave(streams):
 
 
 def _token_rows(t, tokens, n, heads, name):
-    if t.dtype != _torch_dtype(tokens.dtype) or not t.is_cuda or t.device.index != tokens.ctx.device:
-        raise ValueError(f"{name}: a CUDA tensor of {tokens.dtype} on device {tokens.ctx.device} is wanted")
-    if tuple(t.shape) != (n, heads, tokens.head_dim) or (n and t.stride(2) != 1):
+    if t.dtype is not tokens.torch_dtype or t.device != tokens.torch_device:
+        raise ValueError(f"{name}: a {tokens.torch_dtype} tensor on {tokens.torch_device} is wanted")
+    s = t.stride()
+    if t.shape != (n, heads, tokens.head_dim) or (n and s[2] != 1):
         raise ValueError(f"{name}: shape {(n, heads, tokens.head_dim)} with a dense last dimension is wanted, "
-                         f"got {tuple(t.shape)}, strides {t.stride()}")
-    return C.byref(_TokensRows(t.data_ptr(), t.stride(0), t.stride(1)))
+                         f"got {tuple(t.shape)}, strides {s}")
+    return _TokensRows(t.data_ptr(), s[0], s[1])
 
 
 def mure_tokens_append(tokens: Tokens, plan: TokensPlan, k, v) -> None:
     """Write the batch's new tokens' keys and values [tokens][n_kv_heads][head_dim] (any token and head
     strides) into their cells."""
+    ctx = tokens.ctx
     kr = _token_rows(k, tokens, plan.n_new, tokens.n_kv_heads, "k")
     vr = _token_rows(v, tokens, plan.n_new, tokens.n_kv_heads, "v")
-    st = _enter(tokens.ctx, (k, v))
-    tokens.ctx.check(lib().mure_tokens_append(tokens.h, plan.h, kr, vr))
+    st = _enter(ctx, (k, v))
+    ctx.check(lib().mure_tokens_append(tokens.h, plan.h, kr, vr))
     _leave(st)
 
 
@@ -625,15 +629,16 @@ def mure_tokens_read(tokens: Tokens, plan: TokensPlan, new: bool = False, out=No
     """(k, v) [cells][n_kv_heads][head_dim] of all the batch's cells, sequence after sequence (new: of
     its new tokens' cells)."""
     import torch
+    ctx = tokens.ctx
     n = plan.n_new if new else plan.n_cells
     if out is None:
         shape = (n, tokens.n_kv_heads, tokens.head_dim)
-        dt, dev = _torch_dtype(tokens.dtype), tokens.ctx.device
-        out = torch.empty(shape, dtype=dt, device=dev), torch.empty(shape, dtype=dt, device=dev)
+        out = (torch.empty(shape, dtype=tokens.torch_dtype, device=tokens.torch_device),
+               torch.empty(shape, dtype=tokens.torch_dtype, device=tokens.torch_device))
     kr = _token_rows(out[0], tokens, n, tokens.n_kv_heads, "out[0]")
     vr = _token_rows(out[1], tokens, n, tokens.n_kv_heads, "out[1]")
-    st = _enter(tokens.ctx, out)
-    tokens.ctx.check(lib().mure_tokens_read(tokens.h, plan.h, int(bool(new)), kr, vr))
+    st = _enter(ctx, out)
+    ctx.check(lib().mure_tokens_read(tokens.h, plan.h, 1 if new else 0, kr, vr))
     _leave(st)
     return out
 
@@ -642,14 +647,14 @@ def mure_tokens_attend(tokens: Tokens, plan: TokensPlan, q, out=None, lse: bool 
     """Attention of the batch's new tokens q [tokens][n_heads][head_dim] over their sequences' cells:
     out (same shape), with lse=True also the logs of the rows' sums, fp32 [tokens][n_heads]."""
     import torch
-    n = plan.n_new
+    ctx, n = tokens.ctx, plan.n_new
     qr = _token_rows(q, tokens, n, plan.n_heads, "q")
     if out is None:
-        out = torch.empty((n, plan.n_heads, tokens.head_dim), dtype=q.dtype, device=q.device)
+        out = torch.empty((n, plan.n_heads, tokens.head_dim), dtype=tokens.torch_dtype, device=tokens.torch_device)
     orow = _token_rows(out, tokens, n, plan.n_heads, "out")
-    ls = torch.empty((n, plan.n_heads), dtype=torch.float32, device=q.device) if lse else None
-    st = _enter(tokens.ctx, (q, out, ls))
-    tokens.ctx.check(lib().mure_tokens_attend(tokens.h, plan.h, qr, orow, ls.data_ptr() if lse else None))
+    ls = torch.empty((n, plan.n_heads), dtype=torch.float32, device=tokens.torch_device) if lse else None
+    st = _enter(ctx, (q, out, ls))
+    ctx.check(lib().mure_tokens_attend(tokens.h, plan.h, qr, orow, ls.data_ptr() if lse else None))
     _leave(st)
     return (out, ls) if lse else out
 
