@@ -12,10 +12,12 @@
 //             write the rows out;
 //   8, 11     issue the MMAs of either row tile;
 //   9, 10     copy K and V tiles by tensor maps, a box per page (or 128 cells of a larger page).
-// The maximum a row is scaled by moves only when it grows by more than 2^8 (powers up to 2^8 lose
-// nothing in 16 bits), so O is hardly ever rescaled; where it is, S's arrival has shown that every
-// earlier product is done.  All (rows, cells) tiles form one line, cut into equal shares, one per
-// CTA; rows that are cut are joined by a second kernel in the order of their parts.
+// What a row's scores are taken relative to lies 7 below their running maximum and moves only when that
+// grows by more than 8 (in powers of two; f16 holds powers up to 2^15, and those down to 2^-21 of the
+// largest keep all its bits), so O is hardly ever rescaled; where it is, S's arrival has shown that
+// every earlier product is done.  Whole units of work go to the CTAs, the longest first; the ones that
+// do not fit an even share are cut along the cells and joined by a second kernel in the order of
+// their parts.
 // Every wait is bounded, as in the GEMM kernel.
 #include <type_traits>
 
@@ -294,9 +296,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                     for (int i = 0; i < 64; ++i) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(s[i]));
                 }
                 const float mt = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.b.scale_log2;
-                const bool up = mt > m + 8.f;
+                const bool up = mt > m + 15.f;
                 if (__any_sync(0xffffffffu, up)) {
-                    const float mn = up ? mt : m, keep = up ? ex2(m - mn) : 1.f;
+                    const float mn = up ? mt - 7.f : m, keep = up ? ex2(m - mn) : 1.f;
                     m = mn;
                     l *= keep;
                     if (t > t0) {

@@ -8,12 +8,16 @@
 //     last, in the order of its parts (equal bits whatever the order of arrival);
 //   - each warp of a block takes a quarter of every tile with a running maximum and sum of its
 //     own, and a ring of cp.async stages of its own: no barrier in the loop;
-//   - e4m3 codes are widened in registers, their scales applied to the scores and (for bf16) the
-//     probabilities in fp32, so the products take exact values.
+//   - e4m3 codes are widened in registers to f16 (one conversion for two, exact), whatever the rows' type:
+//     bf16 rows of q become f16 ones with their largest magnitude brought to 8 .. 16 by a power of two,
+//     exact down to 2^-18 of it.  A cell's scale of K goes to its score, in fp32.  A cell's scale of
+//     V goes to the value, relative to the largest scale met so far and down to 2^-14 of it (exact:
+//     the codes' least bit is then 2^-23), what is left of it to the probability.
 // fp32 rows take the same way with TF32 products: every operand is split in two TF32 halves, a = a_hi + a_lo,
 // and a product is a_hi b_hi + a_hi b_lo + a_lo b_hi (codes are TF32 values as they are: two products).
-// The running maximum moves only when it grows by more than 2^8: the sums then need no rescaling in
-// nearly all steps, and powers up to 2^8 lose nothing in either type.
+// What a row's scores are taken relative to lies 7 below their running maximum and moves only when that
+// grows by more than 8 (in powers of two): the sums then need no rescaling in nearly all steps. Powers
+// reach 2^15, which f16 holds, and those down to 2^-21 of the largest keep all its bits.
 #include <type_traits>
 
 #include "tokens_util.cuh"
@@ -23,28 +27,29 @@ namespace mure {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kStages = 3;
 constexpr int kAlign = 16;
 
 template <class T, bool E4M3, int DP>
 struct Few {
     static constexpr bool kF32 = std::is_same<T, float>::value;
+    using Prod = typename std::conditional<E4M3 && !kF32, __half, T>::type;   // type of the products' operands
     static constexpr int kElt = E4M3 ? 1 : (int)sizeof(T);
     static constexpr int kRow = DP * kElt;                                   // bytes of a staged row
     static constexpr int kLeast = kF32 ? 8 : 16;
-    static constexpr int WK = (4096 / kRow < kLeast) ? kLeast : (4096 / kRow > 64 ? 64 : 4096 / kRow);   // cells of a warp's step
+    static constexpr int kBytes = 4096, kStages = kRow < 128 ? 4 : 2;         // of a step's K or V rows
+    static constexpr int WK = (kBytes / kRow < kLeast) ? kLeast : (kBytes / kRow > 32 ? 32 : kBytes / kRow);   // cells of a warp's step
     static constexpr int kTile = kWarps * WK;
     static constexpr int kScaleBytes = E4M3 ? 2 * WK : 0;
     static constexpr int kStage = 2 * WK * kRow + kScaleBytes;               // K rows, V rows, scales
     static constexpr int kStageAl = (kStage + 127) / 128 * 128;
-    static constexpr int kJoin = kWarps * kFewRows * (DP + 2) * 4;
+    static constexpr int kJoin = kWarps * kFewRows * (DP + 2) * 4 + kWarps * kFewRows * 4;   // (and the parts' weights)
     static constexpr int kRing = kWarps * kStages * kStageAl;
-    // the fragments of q: in registers; for 256 values and for fp32 in shared memory (one copy for all warps)
-    static constexpr bool kSharedQ = DP > 128 || kF32;
+    // the fragments of q: in registers; for 256 values, fp32 and codes in shared memory (one copy for all warps)
+    static constexpr bool kSharedQ = DP > 128 || kF32 || E4M3;
     static constexpr int kQSteps = kF32 ? DP / 8 : DP / 16;
     static constexpr int kQ = kSharedQ ? kQSteps * 32 * 16 : 0;
     static constexpr int kSmem = (kRing > kJoin ? kRing : kJoin) + kQ;
-    static constexpr int kBlocks = kSmem > 110 * 1024 ? 1 : 2;               // per SM
+    static constexpr int kBlocks = kSmem > 110 * 1024 ? 1 : DP > 128 || kSmem > 74 * 1024 || (kF32 && E4M3 && DP > 64) ? 2 : 3;   // per SM
 };
 
 struct FewParams {
@@ -72,6 +77,10 @@ __device__ __forceinline__ uint32_t swz(int row, int byte, bool v)
 __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool on)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp8(uint32_t dst, const void *src, bool on)
 {
@@ -142,7 +151,6 @@ template <class T> struct Mma;
 template <> struct Mma<float> {     // (for the names alone: fp32 rows have products of their own)
     static __device__ __forceinline__ void go(float *, const uint32_t *, uint32_t, uint32_t) {}
     static __device__ __forceinline__ uint32_t pack(float, float) { return 0; }
-    static __device__ __forceinline__ uint32_t widen(uint32_t) { return 0; }
 };
 template <> struct Mma<__nv_bfloat16> {
     static __device__ __forceinline__ void go(float *c, const uint32_t *a, uint32_t b0, uint32_t b1)
@@ -156,12 +164,6 @@ template <> struct Mma<__nv_bfloat16> {
         uint32_t r;
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
         return r;
-    }
-    // two e4m3 codes in the low 16 bits
-    static __device__ __forceinline__ uint32_t widen(uint32_t two)
-    {
-        const float2 f = e4m3_values((uint16_t)two);
-        return pack(f.x, f.y);
     }
 };
 template <> struct Mma<__half> {
@@ -177,18 +179,17 @@ template <> struct Mma<__half> {
         asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
         return r;
     }
-    static __device__ __forceinline__ uint32_t widen(uint32_t two)
-    {
-        uint32_t h;
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
-        return h;
-    }
 };
 
-// f16 values from codes: the scale 2^e goes to the value as far as f16 holds every code times it
-// (e in -14..7), the rest to the probability.
-__device__ __forceinline__ int value_exp(uint32_t byte) { return max(-14, min(7, (int)byte - 127)); }
+// Two e4m3 codes in the low 16 bits.
+__device__ __forceinline__ uint32_t widen(uint32_t two)
+{
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
+    return h;
+}
 
+// 2^lo and 2^hi as f16 values, -14 .. 15.
 __device__ __forceinline__ uint32_t half2_pow2(int lo, int hi)
 {
     return (uint32_t)(lo + 15) << 10 | (uint32_t)(hi + 15) << 26;
@@ -214,21 +215,24 @@ template <class T, bool E4M3, int DP>
 __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_tokens_few(FewParams p)
 {
     using F = Few<T, E4M3, DP>;
+    using M = Mma<typename F::Prod>;
     constexpr int KS = F::kQSteps, NT = F::WK / 8, ND = DP / 8, WK = F::WK;
     extern __shared__ __align__(128) char smem[];
     __shared__ TokItem w;
+    __shared__ int ends[2];                                  // positions of the first and the last row
     __shared__ int last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int D = p.pool.d, psz = 1 << p.pool.page_log2;
-    const uint32_t ring = su32(smem) + warp * kStages * F::kStageAl;
+    const uint32_t ring = su32(smem) + warp * F::kStages * F::kStageAl;
     const int row_bytes = D * F::kElt;
 
     for (int it = p.w.first[blockIdx.x]; it < p.w.first[blockIdx.x + 1]; ++it) {
         if (threadIdx.x < sizeof(TokItem) / 8)
             reinterpret_cast<int2 *>(&w)[threadIdx.x] = __ldg(reinterpret_cast<const int2 *>(p.w.items + it) + threadIdx.x);
         __syncthreads();
+        if (threadIdx.x < 2) ends[threadIdx.x] = w.pos + (w.r0 + (threadIdx.x ? w.rows - 1 : 0)) / p.b.group;
+        __syncthreads();
         const int nA = (w.a1 + F::kTile - 1) / F::kTile, b_al = w.b0 & ~(kAlign - 1);
-        const int32_t *table = p.b.table + w.table0;
 
         // one step of this warp: cells [start, start + WK), of which begin .. end - 1 take part
         auto range = [&](int tile, int &start, int &begin, int &end) {
@@ -242,7 +246,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
             int start, begin, end;
             range(tile, start, begin, end);
             const int j = start + lane * 8;
-            return j < end ? __ldg(table + (j >> p.pool.page_log2)) : 0;
+            return j < end ? __ldg(p.b.table + w.table0 + (j >> p.pool.page_log2)) : 0;
         };
         auto issue = [&](int tile, int slot, int page_of_group) {
             if (tile < w.t1) {
@@ -254,6 +258,23 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                 constexpr int REP = CH > 32 ? CH / 32 : 1;     // or instructions a row takes
                 static_assert(PER * CH == 32 || REP * 32 == CH, "rows and lanes do not divide");
                 const int r0 = CH < 32 ? lane / CH : 0;
+                // whole steps of rows without padding (nearly all): plain copies
+                if (start >= begin && start + WK <= end && row_bytes == F::kRow) {
+#pragma unroll
+                    for (int grp = 0; grp < WK / 8; ++grp) {
+                        const int page = __shfl_sync(0xffffffffu, page_of_group, grp);
+                        const int64_t row = (((int64_t)page * p.pool.hk + w.h) << p.pool.page_log2) | ((start + grp * 8) & (psz - 1));
+                        const int64_t at = row * F::kRow + r0 * F::kRow + (REP > 1 ? lane : lane % CH) * 16;
+                        const char *kb = static_cast<const char *>(p.pool.k) + at, *vb = static_cast<const char *>(p.pool.v) + at;
+#pragma unroll
+                        for (int e = 0; e < 8 * REP; e += PER) {
+                            const int r = e / REP + r0, byte = (REP > 1 ? lane + e % REP * 32 : lane % CH) * 16;
+                            const int off = e / REP * F::kRow + e % REP * 512;
+                            cp16(st + swz<F::kRow, F::kF32 && !E4M3>(grp * 8 + r, byte, false), kb + off);
+                            cp16(st + WK * F::kRow + swz<F::kRow, F::kF32 && !E4M3>(grp * 8 + r, byte, true), vb + off);
+                        }
+                    }
+                } else {
 #pragma unroll
                 for (int grp = 0; grp < WK / 8; ++grp) {
                     const int page = __shfl_sync(0xffffffffu, page_of_group, grp);
@@ -284,6 +305,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                         }
                     }
                 }
+                }
                 const int scale_page = E4M3 ? __shfl_sync(0xffffffffu, page_of_group, lane / 2) : 0;
                 if (E4M3 && lane < WK / 4) {
                     const int j = start + lane * 4, page = scale_page;
@@ -299,7 +321,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
         // the first stages are on their way while q is fetched
         int next_pages = pages(w.t0);
 #pragma unroll
-        for (int i = 0; i < kStages - 1; ++i) {
+        for (int i = 0; i < F::kStages - 1; ++i) {
             const int cur = next_pages;
             next_pages = pages(w.t0 + i + 1);
             issue(w.t0 + i, i, cur);
@@ -307,12 +329,19 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
 
         uint32_t qf[F::kSharedQ ? 1 : KS][4];
         uint4 *q_shared = reinterpret_cast<uint4 *>(smem + F::kSmem - F::kQ);
-        int prow[2];
+        // every fragment of q (shared ones: `all`, or by warp 0 alone)
+        auto for_q = [&](bool all, auto fn) {
+            if (!F::kSharedQ) {
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) fn(qf[F::kSharedQ ? 0 : ks]);
+            } else if (all || warp == 0) {
+                for (int ks = 0; ks < KS; ++ks) fn(reinterpret_cast<uint32_t *>(q_shared + ks * 32 + lane));
+            }
+        };
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int r = w.r0 + g + half * 8;
             const bool on = g + half * 8 < w.rows;
-            prow[half] = w.pos + r / p.b.group;
             const T *q = reinterpret_cast<const T *>(p.q.p) +
                          (on ? (int64_t)(w.row0 + r / p.b.group) * p.q.ts + (int64_t)(w.h * p.b.group + r % p.b.group) * p.q.hs : 0);
 #pragma unroll
@@ -338,35 +367,56 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                 }
             }
         }
+        // scores: products times rowf (and a cell's scale) are powers of two
+        float rowf[2] = {p.b.scale_log2, p.b.scale_log2};
+        if constexpr (E4M3 && std::is_same<T, __nv_bfloat16>::value) {
+            uint32_t top[2] = {0, 0};
+            auto magnitude = [](uint32_t two) { return max(two & 0x7FFFu, two >> 16 & 0x7FFFu); };
+            if (F::kSharedQ) __syncthreads();
+            for_q(true, [&](uint32_t *f) {
+                top[0] = max(top[0], max(magnitude(f[0]), magnitude(f[2])));
+                top[1] = max(top[1], max(magnitude(f[1]), magnitude(f[3])));
+            });
+            float up[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+                top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+                const uint32_t e = top[i] >> 7;                        // 255: an infinity or a NaN, left as it is
+                const uint32_t f = e == 255u ? 127u : min(257u - e, 253u);
+                up[i] = __uint_as_float(f << 23);
+                rowf[i] *= __uint_as_float((254u - f) << 23);
+            }
+            if (F::kSharedQ) __syncthreads();
+            for_q(false, [&](uint32_t *f) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    f[i] = M::pack(__uint_as_float(f[i] << 16) * up[i & 1], __uint_as_float(f[i] & 0xFFFF0000u) * up[i & 1]);
+            });
+        }
         if (F::kSharedQ) __syncthreads();
-        const int p_lo = w.pos + w.r0 / p.b.group, p_hi = w.pos + (w.r0 + w.rows - 1) / p.b.group;
 
         float o[ND][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        int v_top = 0;                                       // E4M3: the largest scale byte of V so far; o is in its unit
 #pragma unroll
         for (int i = 0; i < ND; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
 
         int slot = 0;
         for (int tile = w.t0; tile < w.t1; ++tile) {
             {
-                const int cur = next_pages, nt = tile + kStages - 1;
+                const int cur = next_pages, nt = tile + F::kStages - 1;
                 next_pages = pages(nt + 1);
-                issue(nt, slot == 0 ? kStages - 1 : slot - 1, cur);
+                issue(nt, slot == 0 ? F::kStages - 1 : slot - 1, cur);
             }
-            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(F::kStages - 1) : "memory");
             __syncwarp();
             const uint32_t st = ring + slot * F::kStageAl;
-            slot = slot + 1 == kStages ? 0 : slot + 1;
+            slot = slot + 1 == F::kStages ? 0 : slot + 1;
             int start, begin, end;
             range(tile, start, begin, end);
             if (start >= end || start + WK <= begin) { __syncwarp(); continue; }
             const char *sc = smem + (st - su32(smem)) + 2 * WK * F::kRow;
 
-            uint4 qa;
-            auto qfrag = [&](int ks, uint4 &x) -> const uint32_t * {
-                if (!F::kSharedQ) return qf[F::kSharedQ ? 0 : ks];
-                x = q_shared[ks * 32 + lane];
-                return reinterpret_cast<const uint32_t *>(&x);
-            };
             float s[NT][4];
 #pragma unroll
             for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
@@ -396,43 +446,61 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                         mma_f32<E4M3>(s[n], hi[1], lo[1], b.z, b.w);
                     }
                 }
-            } else {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
+            } else if constexpr (E4M3) {
 #pragma unroll
                 for (int kp = 0; kp < F::kRow / 64; ++kp) {        // four 16-byte chunks of eight rows
-                    uint32_t r[4];
-                    ldsm4(st + swz<F::kRow, false>(n * 8 + (lane & 7), (kp * 4 + (lane >> 3)) * 16, false), r);
-                    if (E4M3) {
+                    uint4 qa[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) qa[i] = q_shared[(kp * 4 + i) * 32 + lane];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        uint32_t r[4];
+                        ldsm4(st + swz<F::kRow, false>(n * 8 + (lane & 7), (kp * 4 + (lane >> 3)) * 16, false), r);
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            Mma<T>::go(s[n], qfrag(kp * 4 + i, qa), Mma<T>::widen(r[i] & 0xffffu), Mma<T>::widen(r[i] >> 16));
-                    } else {
-                        Mma<T>::go(s[n], qfrag(2 * kp, qa), r[0], r[1]);
-                        Mma<T>::go(s[n], qfrag(2 * kp + 1, qa), r[2], r[3]);
+                            M::go(s[n], reinterpret_cast<const uint32_t *>(&qa[i]), widen(r[i] & 0xffffu), widen(r[i] >> 16));
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int kp = 0; kp < F::kRow / 64; ++kp) {
+                    uint4 qa[2];
+                    if (F::kSharedQ) { qa[0] = q_shared[2 * kp * 32 + lane]; qa[1] = q_shared[(2 * kp + 1) * 32 + lane]; }
+                    const uint32_t *q0 = F::kSharedQ ? reinterpret_cast<const uint32_t *>(&qa[0]) : qf[F::kSharedQ ? 0 : 2 * kp];
+                    const uint32_t *q1 = F::kSharedQ ? reinterpret_cast<const uint32_t *>(&qa[1]) : qf[F::kSharedQ ? 0 : 2 * kp + 1];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        uint32_t r[4];
+                        ldsm4(st + swz<F::kRow, false>(n * 8 + (lane & 7), (kp * 4 + (lane >> 3)) * 16, false), r);
+                        M::go(s[n], q0, r[0], r[1]);
+                        M::go(s[n], q1, r[2], r[3]);
                     }
                 }
             }
-            }
             // scores in powers of two, masked
-            const bool open = start >= begin && start + WK <= end && start + WK - 1 <= p_lo &&
-                              (p.b.window == 0 || start > p_hi - p.b.window);
+            const bool open = start >= begin && start + WK <= end && start + WK - 1 <= ends[0] &&
+                              (p.b.window == 0 || start > ends[1] - p.b.window);
             float top[2] = {-INFINITY, -INFINITY};
             uint32_t seen = 0;                               // not open: a bit per score
+            int row_pos[2] = {0, 0};
+            if (!open) {
+                row_pos[0] = w.pos + (w.r0 + g) / p.b.group;
+                row_pos[1] = w.pos + (w.r0 + g + 8) / p.b.group;
+            }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                float f0 = p.b.scale_log2, f1 = f0;
+                float f0 = 1.f, f1 = 1.f;
                 if (E4M3) {
                     const uint32_t two = *reinterpret_cast<const uint16_t *>(sc + n * 8 + 2 * t);
-                    f0 *= scale_of(two & 255u);
-                    f1 *= scale_of(two >> 8);
+                    f0 = scale_of(two & 255u);
+                    f1 = scale_of(two >> 8);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float x = s[n][i] * (i & 1 ? f1 : f0);
+                    float x = E4M3 ? s[n][i] * (i & 1 ? f1 : f0) : s[n][i];
                     if (!open) {
                         const int j = start + n * 8 + 2 * t + (i & 1);
-                        const bool see = j >= begin && j < end && tok_seen(j, prow[i >> 1], p.b.window, p.b.sinks);
+                        const bool see = j >= begin && j < end && tok_seen(j, row_pos[i >> 1], p.b.window, p.b.sinks);
                         x = see ? x : -INFINITY;
                         seen |= (uint32_t)see << (n * 4 + i);
                     }
@@ -443,13 +511,13 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
-                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2)) * rowf[i];
             }
             const bool up0 = top[0] > m[0] + 8.f;
             const bool up1 = top[1] > m[1] + 8.f;
             if (__any_sync(0xffffffffu, up0 || up1)) {
-                const float n0 = up0 ? top[0] : m[0], n1 = up1 ? top[1] : m[1];
-                const float k0 = m[0] == n0 ? 1.f : ex2(m[0] - n0), k1 = m[1] == n1 ? 1.f : ex2(m[1] - n1);
+                const float n0 = up0 ? top[0] - 7.f : m[0], n1 = up1 ? top[1] - 7.f : m[1];
+                const float k0 = up0 ? ex2(m[0] - n0) : 1.f, k1 = up1 ? ex2(m[1] - n1) : 1.f;
                 m[0] = n0;
                 m[1] = n1;
                 l[0] *= k0;
@@ -460,13 +528,13 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                     o[i][2] *= k1; o[i][3] *= k1;
                 }
             }
-            const float ref0 = m[0] == -INFINITY ? 0.f : m[0], ref1 = m[1] == -INFINITY ? 0.f : m[1];
+            const float ref0 = m[0] == -INFINITY ? 0.f : -m[0], ref1 = m[1] == -INFINITY ? 0.f : -m[1];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                s[n][0] = ex2(s[n][0] - ref0);
-                s[n][1] = ex2(s[n][1] - ref0);
-                s[n][2] = ex2(s[n][2] - ref1);
-                s[n][3] = ex2(s[n][3] - ref1);
+                s[n][0] = ex2(fmaf(s[n][0], rowf[0], ref0));
+                s[n][1] = ex2(fmaf(s[n][1], rowf[0], ref0));
+                s[n][2] = ex2(fmaf(s[n][2], rowf[1], ref1));
+                s[n][3] = ex2(fmaf(s[n][3], rowf[1], ref1));
                 l[0] += s[n][0] + s[n][1];
                 l[1] += s[n][2] + s[n][3];
             }
@@ -512,6 +580,27 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                     }
                 }
             } else {
+            bool plain = true;                               // no part of a scale goes to a probability
+            if constexpr (E4M3) {
+                uint32_t most = 0;
+#pragma unroll
+                for (int i = 0; i < (WK + 31) / 32; ++i) {
+                    const int k = lane + 32 * i, j = start + k;
+                    const bool in = k < WK && j >= begin && j < end;
+                    const uint32_t y = in ? *reinterpret_cast<const uint8_t *>(sc + WK + k) : 0u;
+                    most = max(most, y == 255u ? 0u : y);
+                    plain = plain && (!in || (y != 255u && (int)y >= v_top - 14));
+                }
+                most = __reduce_max_sync(0xffffffffu, most);
+                if ((int)most > v_top) {
+                    const float f = scale_of((uint32_t)max(127 + v_top - (int)most, 0));
+#pragma unroll
+                    for (int i = 0; i < ND; ++i) { o[i][0] *= f; o[i][1] *= f; o[i][2] *= f; o[i][3] *= f; }
+                    v_top = (int)most;
+                    plain = false;                           // (judged by the scale before)
+                }
+                plain = __all_sync(0xffffffffu, plain);
+            }
 #pragma unroll
             for (int kg = 0; kg < WK / 16; ++kg) {
                 uint32_t a[4], vs[2] = {0, 0};
@@ -520,27 +609,20 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                     float *x = s[2 * kg + hh];
                     if (E4M3) {
                         const uint32_t two = *reinterpret_cast<const uint16_t *>(sc + WK + kg * 16 + hh * 8 + 2 * t);
-                        const uint32_t y0 = two & 255u, y1 = two >> 8;
-                        float f0, f1;
-                        if (std::is_same<T, __half>::value) {
-                            const int e0 = value_exp(y0), e1 = value_exp(y1);
-                            vs[hh] = half2_pow2(e0, e1);
-                            f0 = y0 == 255u ? NAN : scale_of((uint32_t)max(0, (int)y0 - e0));
-                            f1 = y1 == 255u ? NAN : scale_of((uint32_t)max(0, (int)y1 - e1));
-                        } else {
-                            f0 = scale_of(y0);
-                            f1 = scale_of(y1);
-                        }
-                        if (!open) {                         // a masked cell's scale may be anything
-                            const uint32_t b = seen >> (8 * kg + 4 * hh);
+                        const int y0 = two & 255u, y1 = two >> 8;
+                        const int e0 = max(-14, min(0, y0 - v_top)), e1 = max(-14, min(0, y1 - v_top));
+                        vs[hh] = half2_pow2(e0, e1);
+                        if (!plain) {
+                            const float f0 = y0 == 255 ? NAN : scale_of((uint32_t)max(0, 127 + y0 - v_top - e0));
+                            const float f1 = y1 == 255 ? NAN : scale_of((uint32_t)max(0, 127 + y1 - v_top - e1));
+                            // (a masked cell's scale may be anything)
+                            const uint32_t b = open ? 15u : seen >> (8 * kg + 4 * hh);
                             x[0] = b & 1 ? x[0] * f0 : 0.f; x[1] = b & 2 ? x[1] * f1 : 0.f;
                             x[2] = b & 4 ? x[2] * f0 : 0.f; x[3] = b & 8 ? x[3] * f1 : 0.f;
-                        } else {
-                            x[0] *= f0; x[1] *= f1; x[2] *= f0; x[3] *= f1;
                         }
                     }
-                    a[2 * hh] = Mma<T>::pack(x[0], x[1]);
-                    a[2 * hh + 1] = Mma<T>::pack(x[2], x[3]);
+                    a[2 * hh] = M::pack(x[0], x[1]);
+                    a[2 * hh + 1] = M::pack(x[2], x[3]);
                 }
 #pragma unroll
                 for (int c = 0; c < F::kRow / 16; c += 2) {
@@ -549,18 +631,16 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                     if (E4M3) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            uint32_t e0 = Mma<T>::widen(__byte_perm(r[2 * i], 0, 0x4420)), e1 = Mma<T>::widen(__byte_perm(r[2 * i + 1], 0, 0x4420));
-                            uint32_t u0 = Mma<T>::widen(__byte_perm(r[2 * i], 0, 0x4431)), u1 = Mma<T>::widen(__byte_perm(r[2 * i + 1], 0, 0x4431));
-                            if (std::is_same<T, __half>::value) {
-                                e0 = hmul2(e0, vs[0]); u0 = hmul2(u0, vs[0]);
-                                e1 = hmul2(e1, vs[1]); u1 = hmul2(u1, vs[1]);
-                            }
-                            Mma<T>::go(o[2 * (c + i)], a, e0, e1);
-                            Mma<T>::go(o[2 * (c + i) + 1], a, u0, u1);
+                            uint32_t e0 = widen(__byte_perm(r[2 * i], 0, 0x4420)), e1 = widen(__byte_perm(r[2 * i + 1], 0, 0x4420));
+                            uint32_t u0 = widen(__byte_perm(r[2 * i], 0, 0x4431)), u1 = widen(__byte_perm(r[2 * i + 1], 0, 0x4431));
+                            e0 = hmul2(e0, vs[0]); u0 = hmul2(u0, vs[0]);
+                            e1 = hmul2(e1, vs[1]); u1 = hmul2(u1, vs[1]);
+                            M::go(o[2 * (c + i)], a, e0, e1);
+                            M::go(o[2 * (c + i) + 1], a, u0, u1);
                         }
                     } else {
-                        Mma<T>::go(o[c], a, r[0], r[1]);
-                        Mma<T>::go(o[c + 1], a, r[2], r[3]);
+                        M::go(o[c], a, r[0], r[1]);
+                        M::go(o[c + 1], a, r[2], r[3]);
                     }
                 }
             }
@@ -577,51 +657,27 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
         // the warps' sums, maxima and sums of powers, [warp][row][DP + 2]
         float *join = reinterpret_cast<float *>(smem);
         constexpr int JR = DP + 2;
+        const float unit = E4M3 && !F::kF32 ? scale_of((uint32_t)v_top) : 1.f;
+        int bad = 0;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             float *row = join + (warp * kFewRows + g + half * 8) * JR;
+            bool fine = l[half] < INFINITY && !isnan(m[half]);
 #pragma unroll
             for (int i = 0; i < ND; ++i) {
                 const int d = F::kF32 ? (i >> 2) * 32 + 8 * t + (i & 3) : E4M3 ? (i >> 1) * 16 + 4 * t + (i & 1) : i * 8 + 2 * t;
-                row[d] = o[i][2 * half];
-                row[d + (F::kF32 ? 4 : E4M3 ? 2 : 1)] = o[i][2 * half + 1];
+                const float x0 = o[i][2 * half] * unit, x1 = o[i][2 * half + 1] * unit;
+                fine = fine && fabsf(x0) < INFINITY && fabsf(x1) < INFINITY;
+                row[d] = x0;
+                row[d + (F::kF32 ? 4 : E4M3 ? 2 : 1)] = x1;
             }
             if (t == 0) { row[DP] = m[half]; row[DP + 1] = l[half]; }
+            bad |= !fine && g + half * 8 < w.rows;
         }
-        __syncthreads();
-
-        // a row's parts -> its sums: parts at src[i * step], n of them, in that order; by 8 values
-        auto joined = [&](const float *src, int64_t step, int n, int c, float *x, float &mm, float &ll) {
-            mm = -INFINITY;
-            for (int i = 0; i < n; ++i) {
-                const float v = src[i * step + DP];
-                mm = isnan(v) || isnan(mm) ? NAN : fmaxf(mm, v);
-            }
-            const float ref = mm == -INFINITY ? 0.f : mm;
-            ll = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.f;
-            for (int i = 0; i < n; ++i) {
-                const float f = ex2(src[i * step + DP] - ref);
-                ll = fmaf(f, src[i * step + DP + 1], ll);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = fmaf(f, src[i * step + c + k], x[k]);
-            }
-        };
         const int chunks = D / 8;
         // rows whose sums are not numbers are done again by the definition, from the cells they may
         // attend to alone: a masked cell's NaN or infinity has met a probability of 0
-        int nan_here = 0;
-        for (int u = threadIdx.x; u < w.rows * chunks; u += kWarps * 32) {
-            float x[8], mm, ll;
-            const int r = u / chunks, c = (u % chunks) * 8;
-            joined(join + r * JR, kFewRows * JR, kWarps, c, x, mm, ll);
-            bool bad = isnan(mm) || isnan(ll);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) bad = bad || isnan(x[i]) || isinf(x[i]);
-            nan_here |= bad;
-        }
-        if (__syncthreads_or(nan_here)) {
+        if (__syncthreads_or(bad)) {
             const int j0 = w.t0 < nA ? w.t0 * F::kTile : max(w.b0, b_al + (w.t0 - nA) * F::kTile);
             const int j1 = w.t1 <= nA ? min(w.a1, w.t1 * F::kTile) : min(w.b1, b_al + (w.t1 - nA) * F::kTile);
             for (int r = warp; r < w.rows; r += kWarps) {
@@ -629,7 +685,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                 const T *q = reinterpret_cast<const T *>(p.q.p) + (int64_t)(w.row0 + rr / p.b.group) * p.q.ts +
                              (int64_t)(w.h * p.b.group + rr % p.b.group) * p.q.hs;
                 float x[8], mm, ll;
-                attend_row<T, E4M3>(p.pool, table, w.h, q, p.q.vec, w.pos + rr / p.b.group, j0, j1, p.b.window, p.b.sinks,
+                attend_row<T, E4M3>(p.pool, p.b.table + w.table0, w.h, q, p.q.vec, w.pos + rr / p.b.group, j0, j1, p.b.window, p.b.sinks,
                                     p.b.scale_log2, x, mm, ll);
                 for (int k = 0; k < kWarps; ++k) {
                     float *row = join + (k * kFewRows + r) * JR;
@@ -642,18 +698,99 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
             }
             __syncthreads();
         }
+        float *wt = join + kWarps * kFewRows * JR;             // (past the joined sums)
+        // The weight of each of n parts of a row, at wt[row * n + i], and the row's maximum and sum of
+        // powers: a thread per row for the block's own parts, a warp per row (parts along the lanes) for a
+        // cut unit's.  src: a row's parts `step` apart.
+        auto done = [&](int r, float mm, float ll, bool last_join) {
+            if (last_join) {
+                const int rr = w.r0 + r;
+                if (p.lse)
+                    p.lse[(int64_t)(w.row0 + rr / p.b.group) * p.b.n_heads + w.h * p.b.group + rr % p.b.group] =
+                        ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.693147180559945f;
+            } else {
+                float *mine = p.w.part + ((int64_t)w.part * kFewRows + r) * JR;
+                mine[DP] = mm;
+                mine[DP + 1] = ll;
+            }
+        };
+        auto weigh_own = [&](bool last_join) {
+            if ((int)threadIdx.x < w.rows) {
+                const int r = threadIdx.x;
+                float v[kWarps], mm = -INFINITY, ll = 0.f;
+                bool nan = false;
+#pragma unroll
+                for (int i = 0; i < kWarps; ++i) {
+                    v[i] = join[(i * kFewRows + r) * JR + DP];
+                    nan = nan || isnan(v[i]);
+                    mm = fmaxf(mm, v[i]);
+                }
+                mm = nan ? NAN : mm;
+                const float ref = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+                for (int i = 0; i < kWarps; ++i) {
+                    v[i] = ex2(v[i] - ref);
+                    ll = fmaf(v[i], join[(i * kFewRows + r) * JR + DP + 1], ll);
+                }
+                const float inv = !last_join ? 1.f : ll == 0.f ? 0.f : 1.f / ll;
+#pragma unroll
+                for (int i = 0; i < kWarps; ++i) wt[r * kWarps + i] = v[i] * inv;
+                done(r, mm, ll, last_join);
+            }
+            __syncthreads();
+        };
+        auto weigh = [&](const float *src, int64_t step, int n) {
+            for (int r = warp; r < w.rows; r += kWarps) {
+                float mm = -INFINITY, ll = 0.f;
+                bool nan = false;
+                for (int i = lane; i < n; i += 32) {
+                    const float v = src[i * step + r * JR + DP];
+                    wt[r * n + i] = v;
+                    nan = nan || isnan(v);
+                    mm = fmaxf(mm, v);
+                }
+#pragma unroll
+                for (int s = 16; s; s >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, s));
+                mm = __any_sync(0xffffffffu, nan) ? NAN : mm;
+                const float ref = mm == -INFINITY ? 0.f : mm;
+                for (int i = lane; i < n; i += 32) {
+                    const float f = ex2(wt[r * n + i] - ref);
+                    wt[r * n + i] = f;
+                    ll = fmaf(f, src[i * step + r * JR + DP + 1], ll);
+                }
+#pragma unroll
+                for (int s = 16; s; s >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, s);
+                const float inv = ll == 0.f ? 0.f : 1.f / ll;
+                for (int i = lane; i < n; i += 32) wt[r * n + i] *= inv;
+                if (lane == 0) done(r, mm, ll, true);
+            }
+            __syncthreads();
+        };
+        // eight of a row's values, weighed and added in the order of the parts
+        auto joined = [&](const float *src, int64_t step, int n, const float *wt, float *x) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) {
+                const float2 *y = reinterpret_cast<const float2 *>(src + i * step);
+                const float2 y0 = y[0], y1 = y[1], y2 = y[2], y3 = y[3];
+                const float f = wt[i];
+                x[0] = fmaf(f, y0.x, x[0]); x[1] = fmaf(f, y0.y, x[1]); x[2] = fmaf(f, y1.x, x[2]); x[3] = fmaf(f, y1.y, x[3]);
+                x[4] = fmaf(f, y2.x, x[4]); x[5] = fmaf(f, y2.y, x[5]); x[6] = fmaf(f, y3.x, x[6]); x[7] = fmaf(f, y3.y, x[7]);
+            }
+        };
         const float *src = join;
         int64_t step = kFewRows * JR;
-        int n = kWarps, stride = JR;
+        int n = kWarps;
         if (w.parts > 1) {
+            weigh_own(false);
             float *mine = p.w.part + (int64_t)w.part * kFewRows * JR;
             for (int u = threadIdx.x; u < w.rows * chunks; u += kWarps * 32) {
-                float x[8], mm, ll;
                 const int r = u / chunks, c = (u % chunks) * 8;
-                joined(join + r * JR, kFewRows * JR, kWarps, c, x, mm, ll);
+                float x[8];
+                joined(src + r * JR + c, step, n, wt + r * n, x);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) mine[r * JR + c + i] = x[i];
-                if (c == 0) { mine[r * JR + DP] = mm; mine[r * JR + DP + 1] = ll; }
+                for (int i = 0; i < 8; i += 2) *reinterpret_cast<float2 *>(mine + r * JR + c + i) = make_float2(x[i], x[i + 1]);
             }
             __threadfence();
             __syncthreads();
@@ -666,18 +803,17 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
             __threadfence();
             src = p.w.part + (int64_t)w.part0 * kFewRows * JR;
             n = w.parts;
+            wt = join;
+            weigh(src, step, n);
+        } else {
+            weigh_own(true);
         }
         for (int u = threadIdx.x; u < w.rows * chunks; u += kWarps * 32) {
-            float x[8], mm, ll;
             const int r = u / chunks, c = (u % chunks) * 8, rr = w.r0 + r;
-            joined(src + r * stride, step, n, c, x, mm, ll);
+            float x[8];
+            joined(src + r * JR + c, step, n, wt + r * n, x);
             const int token = w.row0 + rr / p.b.group, head = w.h * p.b.group + rr % p.b.group;
-            const float inv = ll == 0.f ? 0.f : 1.f / ll;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] *= inv;
             store8(reinterpret_cast<T *>(p.out.p) + token * p.out.ts + head * p.out.hs + c, p.out.vec, x);
-            if (p.lse && c == 0)
-                p.lse[(int64_t)token * p.b.n_heads + head] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.693147180559945f;
         }
         __syncthreads();                                     // the joined sums' memory is the next ring
     }

@@ -375,6 +375,32 @@ def test_scores_at_the_ends_of_the_range(M, ctx):
         t.check()
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_scales_of_all_sizes(M, ctx, dtype, d):
+    """e4m3 rows whose scales differ by up to 2^20 within a sequence, rows of zeros and of the least scale
+    beside large ones, and queries of very small and very large magnitude (f16: as far as it goes)."""
+    lo, hi = (-10, 10) if dtype != "f16" else (-6, 4)
+    t = Batch(M, ctx, [1, 90], [700, 300], [701, 390], 8, 2, d, 16, dtype, "e4m3", seed=9)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for w, middle in ((2, 113), (3, 119)):         # (of K smaller: scores stay within tens)
+        e = torch.randint(lo, hi + 1, t.pools[w].shape, generator=g, device="cuda")
+        t.pools[w].copy_((middle + e).to(torch.uint8))
+        pick = torch.rand(t.pools[w].shape, generator=g, device="cuda")
+        t.pools[w][pick < 0.05] = 0                # least scale, codes of any size
+        t.pools[w - 2].view(torch.uint8)[pick > 0.95] = 0
+    t.check()
+    if dtype != "f16":
+        t.q.mul_(2.0 ** -60)
+        t.check()
+        t.q.mul_(2.0 ** 90)
+        t.pools[2][t.pools[2] > 40] -= 40
+        t.check()
+    else:
+        t.q[..., ::2].mul_(2.0 ** -12)
+        t.check()
+
+
 @pytest.mark.parametrize("dtype,form", [("bf16", "same"), ("bf16", "e4m3"), ("f32", "same")])
 def test_offsets_past_32_bits(M, ctx, dtype, form):
     """Pages at the far end of pools of more than 2^31 values."""
