@@ -10,9 +10,8 @@
 //     own, and a ring of cp.async stages of its own: no barrier in the loop;
 //   - e4m3 codes are widened in registers to f16 (one conversion for two, exact), whatever the rows' type:
 //     bf16 rows of q become f16 ones with their largest magnitude brought to 8 .. 16 by a power of two,
-//     exact down to 2^-18 of it.  A cell's scale of K goes to its score, in fp32.  A cell's scale of
-//     V goes to the value, relative to the largest scale met so far and down to 2^-14 of it (exact:
-//     the codes' least bit is then 2^-23), what is left of it to the probability.
+//     exact down to 2^-18 of it.  A cell's scale of K goes to its score and that of V, relative to the
+//     largest met so far, to its probability, in fp32 (64 products of values saved per step).
 // fp32 rows take the same way with TF32 products: every operand is split in two TF32 halves, a = a_hi + a_lo,
 // and a product is a_hi b_hi + a_hi b_lo + a_lo b_hi (codes are TF32 values as they are: two products).
 // What a row's scores are taken relative to lies 7 below their running maximum and moves only when that
@@ -48,7 +47,8 @@ struct Few {
     static constexpr bool kSharedQ = DP > 128 || kF32 || E4M3;
     static constexpr int kQSteps = kF32 ? DP / 8 : DP / 16;
     static constexpr int kQ = kSharedQ ? kQSteps * 32 * 16 : 0;
-    static constexpr int kSmem = (kRing > kJoin ? kRing : kJoin) + kQ;
+    static constexpr int kFactors = E4M3 ? kWarps * 2 * 32 * 4 : 0;          // a step's scales, as factors
+    static constexpr int kSmem = (kRing > kJoin ? kRing : kJoin) + kQ + kFactors;
     static constexpr int kBlocks = kSmem > 110 * 1024 ? 1 : DP > 128 || kSmem > 74 * 1024 || (kF32 && E4M3 && DP > 64) ? 2 : 3;   // per SM
 };
 
@@ -106,6 +106,12 @@ __device__ __forceinline__ float4 lds16(uint32_t a)
 {
     float4 v;
     asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 lds8(uint32_t a)
+{
+    float2 v;
+    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
     return v;
 }
 __device__ __forceinline__ uint32_t lds4(uint32_t a)
@@ -189,19 +195,6 @@ __device__ __forceinline__ uint32_t widen(uint32_t two)
     return h;
 }
 
-// 2^lo and 2^hi as f16 values, -14 .. 15.
-__device__ __forceinline__ uint32_t half2_pow2(int lo, int hi)
-{
-    return (uint32_t)(lo + 15) << 10 | (uint32_t)(hi + 15) << 26;
-}
-
-__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-
 // Two neighbouring values of a row of q (element offset even; rows may start anywhere).
 template <class T>
 __device__ __forceinline__ uint32_t load2(const T *p, int vec)
@@ -219,6 +212,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
     constexpr int KS = F::kQSteps, NT = F::WK / 8, ND = DP / 8, WK = F::WK;
     extern __shared__ __align__(128) char smem[];
     __shared__ TokItem w;
+    __shared__ float row_factor[kFewRows];                   // bf16 rows on codes
     __shared__ int ends[2];                                  // positions of the first and the last row
     __shared__ int last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -328,7 +322,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
         }
 
         uint32_t qf[F::kSharedQ ? 1 : KS][4];
-        uint4 *q_shared = reinterpret_cast<uint4 *>(smem + F::kSmem - F::kQ);
+        uint4 *q_shared = reinterpret_cast<uint4 *>(smem + F::kSmem - F::kFactors - F::kQ);
         // every fragment of q (shared ones: `all`, or by warp 0 alone)
         auto for_q = [&](bool all, auto fn) {
             if (!F::kSharedQ) {
@@ -341,7 +335,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int r = w.r0 + g + half * 8;
-            const bool on = g + half * 8 < w.rows;
+            const bool on = g + half * 8 < w.rows && (!F::kSharedQ || warp == 0);
             const T *q = reinterpret_cast<const T *>(p.q.p) +
                          (on ? (int64_t)(w.row0 + r / p.b.group) * p.q.ts + (int64_t)(w.h * p.b.group + r % p.b.group) * p.q.hs : 0);
 #pragma unroll
@@ -368,8 +362,8 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
             }
         }
         // scores: products times rowf (and a cell's scale) are powers of two
-        float rowf[2] = {p.b.scale_log2, p.b.scale_log2};
-        if constexpr (E4M3 && std::is_same<T, __nv_bfloat16>::value) {
+        constexpr bool kRowFactor = E4M3 && std::is_same<T, __nv_bfloat16>::value;
+        if constexpr (kRowFactor) {
             uint32_t top[2] = {0, 0};
             auto magnitude = [](uint32_t two) { return max(two & 0x7FFFu, two >> 16 & 0x7FFFu); };
             if (F::kSharedQ) __syncthreads();
@@ -385,7 +379,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                 const uint32_t e = top[i] >> 7;                        // 255: an infinity or a NaN, left as it is
                 const uint32_t f = e == 255u ? 127u : min(257u - e, 253u);
                 up[i] = __uint_as_float(f << 23);
-                rowf[i] *= __uint_as_float((254u - f) << 23);
+                if (warp == 0 && t == 0) row_factor[g + 8 * i] = p.b.scale_log2 * __uint_as_float((254u - f) << 23);
             }
             if (F::kSharedQ) __syncthreads();
             for_q(false, [&](uint32_t *f) {
@@ -410,27 +404,49 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
             }
             asm volatile("cp.async.wait_group %0;" ::"n"(F::kStages - 1) : "memory");
             __syncwarp();
+            const uint32_t qs = su32(smem) + F::kSmem - F::kFactors - F::kQ + lane * 16;
+            const uint32_t factors = su32(smem) + F::kSmem - F::kFactors + warp * 256;
             const uint32_t st = ring + slot * F::kStageAl;
             slot = slot + 1 == F::kStages ? 0 : slot + 1;
             int start, begin, end;
             range(tile, start, begin, end);
             if (start >= end || start + WK <= begin) { __syncwarp(); continue; }
-            const char *sc = smem + (st - su32(smem)) + 2 * WK * F::kRow;
+            if constexpr (E4M3) {
+                // a cell's scales by its lane: K's as a factor of its scores, V's of its probabilities,
+                // relative to the largest scale of V so far
+                const char *sc = smem + (st - su32(smem)) + 2 * WK * F::kRow;
+                const bool in = lane < WK && start + lane >= begin && start + lane < end;
+                const uint32_t yk = in ? *reinterpret_cast<const uint8_t *>(sc + lane) : 0u;
+                const uint32_t yv = in ? *reinterpret_cast<const uint8_t *>(sc + WK + lane) : 0u;
+                if constexpr (!F::kF32) {
+                    const int most = (int)__reduce_max_sync(0xffffffffu, yv == 255u ? 0u : yv);
+                    if (most > v_top) {
+                        const float f = scale_of((uint32_t)max(127 + v_top - most, 0));
+#pragma unroll
+                        for (int i = 0; i < ND; ++i) { o[i][0] *= f; o[i][1] *= f; o[i][2] *= f; o[i][3] *= f; }
+                        v_top = most;
+                    }
+                }
+                float *mine = reinterpret_cast<float *>(smem + F::kSmem - F::kFactors) + warp * 64 + lane;   // of K, then of V
+                mine[0] = scale_of(yk);
+                mine[32] = yv == 255u || F::kF32 ? scale_of(yv) : scale_of((uint32_t)max(127 + (int)yv - v_top, 0));
+                __syncwarp();
+            }
 
             float s[NT][4];
 #pragma unroll
             for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
             if constexpr (F::kF32) {
-#pragma unroll
+#pragma unroll 4
                 for (int i = 0; i < DP / 16; ++i) {            // 16 values of a row: two steps
                     uint32_t hi[2][4], lo[2][4];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const uint4 a = q_shared[(2 * i + e) * 32 + lane];
-                        halves(__uint_as_float(a.x), hi[e][0], lo[e][0]);
-                        halves(__uint_as_float(a.y), hi[e][1], lo[e][1]);
-                        halves(__uint_as_float(a.z), hi[e][2], lo[e][2]);
-                        halves(__uint_as_float(a.w), hi[e][3], lo[e][3]);
+                        const float4 a = lds16(qs + (2 * i + e) * 512);
+                        halves(a.x, hi[e][0], lo[e][0]);
+                        halves(a.y, hi[e][1], lo[e][1]);
+                        halves(a.z, hi[e][2], lo[e][2]);
+                        halves(a.w, hi[e][3], lo[e][3]);
                     }
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
@@ -449,23 +465,24 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
             } else if constexpr (E4M3) {
 #pragma unroll
                 for (int kp = 0; kp < F::kRow / 64; ++kp) {        // four 16-byte chunks of eight rows
-                    uint4 qa[4];
+                    float4 qa[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) qa[i] = q_shared[(kp * 4 + i) * 32 + lane];
+                    for (int i = 0; i < 4; ++i) qa[i] = lds16(qs + (kp * 4 + i) * 512);
+                    uint32_t r[NT][4];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        uint32_t r[4];
-                        ldsm4(st + swz<F::kRow, false>(n * 8 + (lane & 7), (kp * 4 + (lane >> 3)) * 16, false), r);
+                    for (int n = 0; n < NT; ++n)
+                        ldsm4(st + swz<F::kRow, false>(n * 8 + (lane & 7), (kp * 4 + (lane >> 3)) * 16, false), r[n]);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            M::go(s[n], reinterpret_cast<const uint32_t *>(&qa[i]), widen(r[i] & 0xffffu), widen(r[i] >> 16));
-                    }
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            M::go(s[n], reinterpret_cast<const uint32_t *>(&qa[i]), widen(r[n][i] & 0xffffu), widen(r[n][i] >> 16));
                 }
             } else {
 #pragma unroll
                 for (int kp = 0; kp < F::kRow / 64; ++kp) {
-                    uint4 qa[2];
-                    if (F::kSharedQ) { qa[0] = q_shared[2 * kp * 32 + lane]; qa[1] = q_shared[(2 * kp + 1) * 32 + lane]; }
+                    float4 qa[2];
+                    if (F::kSharedQ) { qa[0] = lds16(qs + kp * 1024); qa[1] = lds16(qs + kp * 1024 + 512); }
                     const uint32_t *q0 = F::kSharedQ ? reinterpret_cast<const uint32_t *>(&qa[0]) : qf[F::kSharedQ ? 0 : 2 * kp];
                     const uint32_t *q1 = F::kSharedQ ? reinterpret_cast<const uint32_t *>(&qa[1]) : qf[F::kSharedQ ? 0 : 2 * kp + 1];
 #pragma unroll
@@ -480,6 +497,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
             // scores in powers of two, masked
             const bool open = start >= begin && start + WK <= end && start + WK - 1 <= ends[0] &&
                               (p.b.window == 0 || start > ends[1] - p.b.window);
+            const float rowf[2] = {kRowFactor ? row_factor[g] : p.b.scale_log2, kRowFactor ? row_factor[g + 8] : p.b.scale_log2};
             float top[2] = {-INFINITY, -INFINITY};
             uint32_t seen = 0;                               // not open: a bit per score
             int row_pos[2] = {0, 0};
@@ -491,9 +509,9 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
             for (int n = 0; n < NT; ++n) {
                 float f0 = 1.f, f1 = 1.f;
                 if (E4M3) {
-                    const uint32_t two = *reinterpret_cast<const uint16_t *>(sc + n * 8 + 2 * t);
-                    f0 = scale_of(two & 255u);
-                    f1 = scale_of(two >> 8);
+                    const float2 f = lds8(factors + (n * 8 + 2 * t) * 4);
+                    f0 = f.x;
+                    f1 = f.y;
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -513,8 +531,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                 top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
                 top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2)) * rowf[i];
             }
-            const bool up0 = top[0] > m[0] + 8.f;
-            const bool up1 = top[1] > m[1] + 8.f;
+            const bool up0 = top[0] > m[0] + 15.f, up1 = top[1] > m[1] + 15.f;
             if (__any_sync(0xffffffffu, up0 || up1)) {
                 const float n0 = up0 ? top[0] - 7.f : m[0], n1 = up1 ? top[1] - 7.f : m[1];
                 const float k0 = up0 ? ex2(m[0] - n0) : 1.f, k1 = up1 ? ex2(m[1] - n1) : 1.f;
@@ -538,22 +555,25 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                 l[0] += s[n][0] + s[n][1];
                 l[1] += s[n][2] + s[n][3];
             }
+            if constexpr (E4M3) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float *x = s[n];
+                    const float2 f = lds8(factors + (32 + n * 8 + 2 * t) * 4);
+                    if (open) {
+                        x[0] *= f.x; x[1] *= f.y; x[2] *= f.x; x[3] *= f.y;
+                    } else {                                 // a masked cell's scale may be anything
+                        const uint32_t b = seen >> (4 * n);
+                        x[0] = b & 1 ? x[0] * f.x : 0.f; x[1] = b & 2 ? x[1] * f.y : 0.f;
+                        x[2] = b & 4 ? x[2] * f.x : 0.f; x[3] = b & 8 ? x[3] * f.y : 0.f;
+                    }
+                }
+            }
             const uint32_t vst = st + WK * F::kRow;
             if constexpr (F::kF32) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {                 // eight cells: the step's cells 2t and 2t + 1 are this lane's
                     float *x = s[n];
-                    if (E4M3) {
-                        const uint32_t two = *reinterpret_cast<const uint16_t *>(sc + WK + n * 8 + 2 * t);
-                        const float f0 = scale_of(two & 255u), f1 = scale_of(two >> 8);
-                        if (!open) {                         // a masked cell's scale may be anything
-                            const uint32_t b = seen >> (4 * n);
-                            x[0] = b & 1 ? x[0] * f0 : 0.f; x[1] = b & 2 ? x[1] * f1 : 0.f;
-                            x[2] = b & 4 ? x[2] * f0 : 0.f; x[3] = b & 8 ? x[3] * f1 : 0.f;
-                        } else {
-                            x[0] *= f0; x[1] *= f1; x[2] *= f0; x[3] *= f1;
-                        }
-                    }
                     uint32_t hi[4], lo[4];
                     halves(x[0], hi[0], lo[0]);
                     halves(x[2], hi[1], lo[1]);
@@ -580,47 +600,12 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                     }
                 }
             } else {
-            bool plain = true;                               // no part of a scale goes to a probability
-            if constexpr (E4M3) {
-                uint32_t most = 0;
-#pragma unroll
-                for (int i = 0; i < (WK + 31) / 32; ++i) {
-                    const int k = lane + 32 * i, j = start + k;
-                    const bool in = k < WK && j >= begin && j < end;
-                    const uint32_t y = in ? *reinterpret_cast<const uint8_t *>(sc + WK + k) : 0u;
-                    most = max(most, y == 255u ? 0u : y);
-                    plain = plain && (!in || (y != 255u && (int)y >= v_top - 14));
-                }
-                most = __reduce_max_sync(0xffffffffu, most);
-                if ((int)most > v_top) {
-                    const float f = scale_of((uint32_t)max(127 + v_top - (int)most, 0));
-#pragma unroll
-                    for (int i = 0; i < ND; ++i) { o[i][0] *= f; o[i][1] *= f; o[i][2] *= f; o[i][3] *= f; }
-                    v_top = (int)most;
-                    plain = false;                           // (judged by the scale before)
-                }
-                plain = __all_sync(0xffffffffu, plain);
-            }
 #pragma unroll
             for (int kg = 0; kg < WK / 16; ++kg) {
-                uint32_t a[4], vs[2] = {0, 0};
+                uint32_t a[4];
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
-                    float *x = s[2 * kg + hh];
-                    if (E4M3) {
-                        const uint32_t two = *reinterpret_cast<const uint16_t *>(sc + WK + kg * 16 + hh * 8 + 2 * t);
-                        const int y0 = two & 255u, y1 = two >> 8;
-                        const int e0 = max(-14, min(0, y0 - v_top)), e1 = max(-14, min(0, y1 - v_top));
-                        vs[hh] = half2_pow2(e0, e1);
-                        if (!plain) {
-                            const float f0 = y0 == 255 ? NAN : scale_of((uint32_t)max(0, 127 + y0 - v_top - e0));
-                            const float f1 = y1 == 255 ? NAN : scale_of((uint32_t)max(0, 127 + y1 - v_top - e1));
-                            // (a masked cell's scale may be anything)
-                            const uint32_t b = open ? 15u : seen >> (8 * kg + 4 * hh);
-                            x[0] = b & 1 ? x[0] * f0 : 0.f; x[1] = b & 2 ? x[1] * f1 : 0.f;
-                            x[2] = b & 4 ? x[2] * f0 : 0.f; x[3] = b & 8 ? x[3] * f1 : 0.f;
-                        }
-                    }
+                    const float *x = s[2 * kg + hh];
                     a[2 * hh] = M::pack(x[0], x[1]);
                     a[2 * hh + 1] = M::pack(x[2], x[3]);
                 }
@@ -631,12 +616,9 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                     if (E4M3) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            uint32_t e0 = widen(__byte_perm(r[2 * i], 0, 0x4420)), e1 = widen(__byte_perm(r[2 * i + 1], 0, 0x4420));
-                            uint32_t u0 = widen(__byte_perm(r[2 * i], 0, 0x4431)), u1 = widen(__byte_perm(r[2 * i + 1], 0, 0x4431));
-                            e0 = hmul2(e0, vs[0]); u0 = hmul2(u0, vs[0]);
-                            e1 = hmul2(e1, vs[1]); u1 = hmul2(u1, vs[1]);
-                            M::go(o[2 * (c + i)], a, e0, e1);
-                            M::go(o[2 * (c + i) + 1], a, u0, u1);
+                            const uint32_t r0 = r[2 * i], r1 = r[2 * i + 1];
+                            M::go(o[2 * (c + i)], a, widen(__byte_perm(r0, 0, 0x4420)), widen(__byte_perm(r1, 0, 0x4420)));
+                            M::go(o[2 * (c + i) + 1], a, widen(__byte_perm(r0, 0, 0x4431)), widen(__byte_perm(r1, 0, 0x4431)));
                         }
                     } else {
                         M::go(o[c], a, r[0], r[1]);
