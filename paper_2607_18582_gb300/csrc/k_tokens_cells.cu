@@ -2,16 +2,18 @@
 // dense rows.
 //
 // Both are copies that touch each byte once and are bound by device memory.  A thread takes eight
-// values of a row (16 bytes of a 16-bit type, 8 bytes of codes), the threads of a row are a
-// power-of-two group of a warp, so the row's largest magnitude is a few shuffles away and an e4m3
-// row is quantised in the pass that copies it.  A block takes a tile of tokens of one sequence.
+// values of a row of K and the same of V (16 bytes each of a 16-bit type, 8 bytes of codes), kRows
+// rows at a time: all its loads are on their way before the first is used.  The threads of a row are a
+// power-of-two group of a warp, so the row's largest magnitude is a few shuffles away and an e4m3 row is
+// quantised in the pass that copies it.  A block takes a tile of 16 tokens of one sequence.
 #include "tokens_util.cuh"
 
 namespace mure {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;    // (with 4 rows a thread: 256 threads 3 %, 2 rows 8-11 %, 8 rows 22-48 % slower)
+constexpr int kRows = 4;         // rows of K and of V that a thread has on their way
 
 struct CellParams {
     TokPool pool;
@@ -29,13 +31,106 @@ struct Tile {
 __device__ __forceinline__ Tile tile_of(const TokBatch &b, bool all, TokSeq &sq)
 {
     const int32_t *prefix = all ? b.tile_all : b.tile_new;
-    const int per = all ? kTokTileAll : kTokTileNew;
     Tile t;
-    t.seq = find_prefix(prefix, b.n_seqs, (int)blockIdx.x);
+    // (one tile for each sequence, as in a decoding step: no search)
+    t.seq = !all && b.one_new ? (int)blockIdx.x : find_prefix(prefix, b.n_seqs, (int)blockIdx.x);
     sq = b.seq[t.seq];
-    t.i0 = ((int)blockIdx.x - prefix[t.seq]) * per;
-    t.n = min(per, (all ? sq.kv : sq.n_new) - t.i0);
+    t.i0 = !all && b.one_new ? 0 : ((int)blockIdx.x - __ldg(prefix + t.seq)) * kTokTile;
+    t.n = min(kTokTile, (all ? sq.kv : sq.n_new) - t.i0);
     return t;
+}
+
+// Eight values as they lie in memory.
+template <class T, bool E4M3>
+struct Raw {
+    uint4 w[E4M3 ? 1 : sizeof(T) / 2];
+    uint32_t scale;
+};
+
+template <class T>
+__device__ __forceinline__ void raw_row(Raw<T, false> &r, const T *p, int vec)
+{
+    if (vec) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = reinterpret_cast<const uint4 *>(p)[i];
+    } else {
+        T *t = reinterpret_cast<T *>(r.w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = p[i];
+    }
+}
+
+template <class T, bool E4M3>
+__device__ __forceinline__ void raw_cell(Raw<T, E4M3> &r, const void *pool, const uint8_t *scales, int64_t row, int D, int c)
+{
+    if constexpr (E4M3) {
+        const uint2 u = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(pool) + row * D + c);
+        r.w[0] = make_uint4(u.x, u.y, 0, 0);
+        r.scale = scales[row];
+    } else {
+        raw_row(r, static_cast<const T *>(pool) + row * D + c, 1);
+    }
+}
+
+template <class T, bool E4M3>
+__device__ __forceinline__ void raw_values(const Raw<T, E4M3> &r, float *x)
+{
+    if constexpr (E4M3) {
+        const float s = scale_of(r.scale);
+        const uint32_t u[2] = {r.w[0].x, r.w[0].y};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = e4m3_values((uint16_t)(u[i >> 1] >> (16 * (i & 1))));
+            x[2 * i] = f.x * s;
+            x[2 * i + 1] = f.y * s;
+        }
+    } else {
+        const T *t = reinterpret_cast<const T *>(r.w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = TokType<T>::up(t[i]);
+    }
+}
+
+// One row of a pool from eight values per lane (all lanes of the warp take part in the shuffles).
+template <class T, bool E4M3>
+__device__ __forceinline__ void put_row(const Raw<T, false> &raw, bool on, void *pool, uint8_t *scales, int64_t row, int D, int c, int lanes)
+{
+    if constexpr (!E4M3) {
+        if (on) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(static_cast<T *>(pool) + row * D + c)[i] = raw.w[i];
+        }
+    } else {
+        float x[8];
+        uint32_t a = 0;                                  // the largest magnitude's bits (16-bit types: two at a time)
+        if constexpr (sizeof(T) == 2) {
+            const uint32_t u[4] = {raw.w[0].x, raw.w[0].y, raw.w[0].z, raw.w[0].w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) a = __vmaxu2(a, u[q] & 0x7FFF7FFFu);
+            a = max(a & 0xFFFFu, a >> 16);
+        } else {
+            const uint32_t *u = reinterpret_cast<const uint32_t *>(raw.w);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) a = max(a, u[q] & 0x7FFFFFFFu);
+        }
+        a = on ? a : 0u;
+        for (int s = lanes >> 1; s; s >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, s));
+        if constexpr (sizeof(T) == 2) {
+            const uint16_t h = (uint16_t)a;
+            a = __float_as_uint(TokType<T>::up(*reinterpret_cast<const T *>(&h)));
+        }
+        raw_values(raw, x);
+        const uint32_t byte = scale_byte(a);
+        if (on) {
+            uint32_t w[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                w[q] = e4m3_pair(unscale(x[4 * q], byte), unscale(x[4 * q + 1], byte)) |
+                       e4m3_pair(unscale(x[4 * q + 2], byte), unscale(x[4 * q + 3], byte)) << 16;
+            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(pool) + row * D + c) = byte == 255u ? make_uint2(0, 0) : make_uint2(w[0], w[1]);
+            if (c == 0) scales[row] = (uint8_t)byte;
+        }
+    }
 }
 
 template <class T, bool E4M3>
@@ -43,42 +138,30 @@ __global__ void __launch_bounds__(kThreads) k_tokens_append(CellParams p)
 {
     TokSeq sq;
     const Tile t = tile_of(p.b, false, sq);
-    const int lane = threadIdx.x & (p.lanes - 1), D = p.pool.d, c = lane * 8;
+    const int D = p.pool.d, c = (threadIdx.x & (p.lanes - 1)) * 8;
     const int32_t *table = p.b.table + sq.table0;
-    const int rows = t.n * p.pool.hk * 2;
-    // (all lanes of a warp take part in the shuffles: rows are handed out to whole warps)
-    const int per = kThreads / p.lanes, first = threadIdx.x / p.lanes;
-    for (int r0 = 0; r0 < rows; r0 += per) {
-        const int r = r0 + first;
-        const bool on = r < rows && c < D;
-        const int which = r & 1, h = (r >> 1) % p.pool.hk, i = (r >> 1) / p.pool.hk;
-        float x[8];
-        int64_t row = 0;
-        if (on) {
-            const TokRows &in = which ? p.v : p.k;
-            row = cell_row(p.pool, table, h, sq.pos + t.i0 + i);
-            load8(reinterpret_cast<const T *>(in.p) + (int64_t)(sq.row0 + t.i0 + i) * in.ts + h * in.hs + c, in.vec, x);
+    const int rows = t.n * p.pool.hk, per = kThreads / p.lanes;
+    for (int r0 = threadIdx.x / p.lanes; r0 - (int)(threadIdx.x / p.lanes) < rows; r0 += per * kRows) {
+        Raw<T, false> k[kRows], v[kRows];
+        int64_t row[kRows];
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) {
+            const int r = r0 + u * per, h = r % p.pool.hk, i = r / p.pool.hk;
+            k[u] = Raw<T, false>{};
+            v[u] = Raw<T, false>{};
+            row[u] = -1;
+            if (r < rows && c < D) {
+                row[u] = cell_row(p.pool, table, h, sq.pos + t.i0 + i);
+                const int64_t token = sq.row0 + t.i0 + i;
+                raw_row(k[u], reinterpret_cast<const T *>(p.k.p) + token * p.k.ts + h * p.k.hs + c, p.k.vec);
+                raw_row(v[u], reinterpret_cast<const T *>(p.v.p) + token * p.v.ts + h * p.v.hs + c, p.v.vec);
+            }
         }
-        void *pool = which ? p.pool.v : p.pool.k;
-        if (!E4M3) {
-            if (on) store8(static_cast<T *>(pool) + row * D + c, 1, x);
-        } else {
-            uint32_t a = 0;
-            if (on) {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) a = max(a, __float_as_uint(x[q]) & 0x7FFFFFFFu);
-            }
-            for (int s = p.lanes >> 1; s; s >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, s));
-            const uint32_t byte = scale_byte(a);
-            if (on) {
-                uint32_t w[2];
-#pragma unroll
-                for (int q = 0; q < 2; ++q)
-                    w[q] = byte == 255u ? 0u : e4m3_pair(unscale(x[4 * q], byte), unscale(x[4 * q + 1], byte)) |
-                                                   e4m3_pair(unscale(x[4 * q + 2], byte), unscale(x[4 * q + 3], byte)) << 16;
-                *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(pool) + row * D + c) = make_uint2(w[0], w[1]);
-                if (lane == 0) (which ? p.pool.vs : p.pool.ks)[row] = (uint8_t)byte;
-            }
+        for (int u = 0; u < kRows; ++u) {
+            if (r0 - (int)(threadIdx.x / p.lanes) + u * per >= rows) break;      // (for all threads alike)
+            put_row<T, E4M3>(k[u], row[u] >= 0, p.pool.k, p.pool.ks, row[u], D, c, p.lanes);
+            put_row<T, E4M3>(v[u], row[u] >= 0, p.pool.v, p.pool.vs, row[u], D, c, p.lanes);
         }
     }
 }
@@ -88,20 +171,34 @@ __global__ void __launch_bounds__(kThreads) k_tokens_read(CellParams p)
 {
     TokSeq sq;
     const Tile t = tile_of(p.b, p.part == 0, sq);
-    const int lane = threadIdx.x & (p.lanes - 1), D = p.pool.d, c = lane * 8;
+    const int D = p.pool.d, c = (threadIdx.x & (p.lanes - 1)) * 8;
     if (c >= D) return;
     const int32_t *table = p.b.table + sq.table0;
-    const int rows = t.n * p.pool.hk;
+    const int rows = t.n * p.pool.hk, per = kThreads / p.lanes;
     const int64_t out0 = (p.part == 0 ? sq.cell0 : (int64_t)sq.row0) + t.i0;
     const int cell0 = (p.part == 0 ? 0 : sq.pos) + t.i0;
-    for (int r = threadIdx.x / p.lanes; r < rows; r += kThreads / p.lanes) {
-        const int h = r % p.pool.hk, i = r / p.pool.hk;
-        const int64_t row = cell_row(p.pool, table, h, cell0 + i);
-        float k[8], v[8];
-        cell8<T, E4M3>(p.pool.k, p.pool.ks, row, D, c, k);
-        cell8<T, E4M3>(p.pool.v, p.pool.vs, row, D, c, v);
-        store8(reinterpret_cast<T *>(p.k.p) + (out0 + i) * p.k.ts + h * p.k.hs + c, p.k.vec, k);
-        store8(reinterpret_cast<T *>(p.v.p) + (out0 + i) * p.v.ts + h * p.v.hs + c, p.v.vec, v);
+    for (int r0 = threadIdx.x / p.lanes; r0 < rows; r0 += per * kRows) {
+        Raw<T, E4M3> k[kRows], v[kRows];
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) {
+            const int r = r0 + u * per;
+            if (r >= rows) break;
+            const int64_t row = cell_row(p.pool, table, r % p.pool.hk, cell0 + r / p.pool.hk);
+            raw_cell<T, E4M3>(k[u], p.pool.k, p.pool.ks, row, D, c);
+            raw_cell<T, E4M3>(v[u], p.pool.v, p.pool.vs, row, D, c);
+        }
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) {
+            const int r = r0 + u * per;
+            if (r >= rows) break;
+            const int h = r % p.pool.hk;
+            const int64_t at = out0 + r / p.pool.hk;
+            float x[8], y[8];
+            raw_values(k[u], x);
+            raw_values(v[u], y);
+            store8(reinterpret_cast<T *>(p.k.p) + at * p.k.ts + h * p.k.hs + c, p.k.vec, x);
+            store8(reinterpret_cast<T *>(p.v.p) + at * p.v.ts + h * p.v.hs + c, p.v.vec, y);
+        }
     }
 }
 

@@ -35,7 +35,8 @@ struct Few {
     static constexpr int kElt = E4M3 ? 1 : (int)sizeof(T);
     static constexpr int kRow = DP * kElt;                                   // bytes of a staged row
     static constexpr int kLeast = kF32 ? 8 : 16;
-    static constexpr int kBytes = 4096, kStages = kRow < 128 ? 4 : 2;         // of a step's K or V rows
+    static constexpr int kBytes = kF32 && E4M3 && DP > 128 ? 2048 : 4096;     // of a step's K or V rows
+    static constexpr int kStages = kRow < 128 ? 4 : 2;
     static constexpr int WK = (kBytes / kRow < kLeast) ? kLeast : (kBytes / kRow > 32 ? 32 : kBytes / kRow);   // cells of a warp's step
     static constexpr int kTile = kWarps * WK;
     static constexpr int kScaleBytes = E4M3 ? 2 * WK : 0;
@@ -338,7 +339,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
             const bool on = g + half * 8 < w.rows && (!F::kSharedQ || warp == 0);
             const T *q = reinterpret_cast<const T *>(p.q.p) +
                          (on ? (int64_t)(w.row0 + r / p.b.group) * p.q.ts + (int64_t)(w.h * p.b.group + r % p.b.group) * p.q.hs : 0);
-#pragma unroll
+#pragma unroll(F::kSharedQ ? 4 : KS)
             for (int ks = 0; ks < KS; ++ks) {
                 // the order of a row's values within a step only has to be that of the cells' values
                 uint32_t x0, x1;
@@ -437,7 +438,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
 #pragma unroll
             for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
             if constexpr (F::kF32) {
-#pragma unroll 4
+#pragma unroll(DP > 128 ? 2 : 4)
                 for (int i = 0; i < DP / 16; ++i) {            // 16 values of a row: two steps
                     uint32_t hi[2][4], lo[2][4];
 #pragma unroll

@@ -307,8 +307,8 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
         table.insert(table.end(), ids, ids + pages);
         n_new += nn;
         n_cells += kv;
-        t_new += (nn + kTokTileNew - 1) / kTokTileNew;
-        t_all += (kv + kTokTileAll - 1) / kTokTileAll;
+        t_new += (nn + kTokTile - 1) / kTokTile;
+        t_all += (kv + kTokTile - 1) / kTokTile;
         FAILIF(n_new > INT32_MAX || t_all > INT32_MAX, c, MURE_ERR_UNSUPPORTED, "more than 2^31 - 1 new tokens or tiles of cells");
         tile_new[s + 1] = (int32_t)t_new;
         tile_all[s + 1] = (int32_t)t_all;
@@ -406,6 +406,8 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
     p->wide_pages = reinterpret_cast<int32_t *>(m + o_wp);
     p->n_wide = (int64_t)wide_pages.size();
     v.n_seqs = n;
+    v.one_new = t_new == n;
+    for (int s = 0; s < n && v.one_new; ++s) v.one_new = tile_new[s + 1] - tile_new[s] == 1;
     v.n_heads = b.n_heads;
     v.group = group;
     v.window = b.window;

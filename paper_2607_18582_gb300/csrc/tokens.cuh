@@ -28,15 +28,16 @@ struct TokPool {
 struct TokBatch {
     const TokSeq *seq = nullptr;
     const int32_t *table = nullptr;          // the sequences' pages, one after the other
-    const int32_t *tile_new = nullptr;       // [n_seqs + 1] tiles of kTokTileNew new tokens before a sequence's
-    const int32_t *tile_all = nullptr;       // [n_seqs + 1] the same for kTokTileAll cells
+    const int32_t *tile_new = nullptr;       // [n_seqs + 1] tiles of kTokTile new tokens before a sequence's
+    const int32_t *tile_all = nullptr;       // [n_seqs + 1] the same for its cells
     int n_seqs = 0;
+    int one_new = 0;                         // every sequence has one tile of new tokens
     int n_heads = 0, group = 0;              // query heads; query heads per cached one
     int window = 0, sinks = 0;
     float scale_log2 = 0.f;                  // factor of the scores, times log2(e)
 };
 
-constexpr int kTokTileNew = 16, kTokTileAll = 64;
+constexpr int kTokTile = 16;
 
 // Rows of activations (mure_tokens_rows); vec: every row starts on a 16-byte boundary.
 struct TokRows {

@@ -490,6 +490,7 @@ class Tokens:
         self.n_pages = desc.n_pages
         import torch
         self.torch_dtype, self.torch_device = _torch_dtype(dtype), torch.device("cuda", ctx.device)
+        self.torch_float = torch.float32
         self._keep = keep          # the caller's pools
         ctx._children += 1
 
@@ -584,13 +585,22 @@ def mure_tokens_plan(tokens: Tokens, n_heads: int, new_len, pos, kv_len, page_ta
     return plan
 
 
+def _raw_stream(device):
+    """torch's current stream as an integer (its own short way where it has one: a call takes a token's time)."""
+    global _raw_stream
+    import torch
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+        lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _raw_stream(device)
+
+
 def _enter(ctx, tensors):
     """Where torch's current stream is not the context's: the context's stream waits for what is
     queued on it, and the tensors' memory is kept until the context's stream is done with it."""
+    if _raw_stream(ctx.device) == ctx.stream:
+        return None
     import torch
     cur = torch.cuda.current_stream(ctx.device)
-    if cur.cuda_stream == ctx.stream:
-        return None
     mine = torch.cuda.ExternalStream(ctx.stream, device=ctx.device) if ctx.stream else torch.cuda.default_stream(ctx.device)
     mine.wait_stream(cur)
     for t in tensors:
@@ -633,8 +643,7 @@ def mure_tokens_read(tokens: Tokens, plan: TokensPlan, new: bool = False, out=No
     n = plan.n_new if new else plan.n_cells
     if out is None:
         shape = (n, tokens.n_kv_heads, tokens.head_dim)
-        out = (torch.empty(shape, dtype=tokens.torch_dtype, device=tokens.torch_device),
-               torch.empty(shape, dtype=tokens.torch_dtype, device=tokens.torch_device))
+        out = torch.empty((2, *shape), dtype=tokens.torch_dtype, device=tokens.torch_device).unbind(0)
     kr = _token_rows(out[0], tokens, n, tokens.n_kv_heads, "out[0]")
     vr = _token_rows(out[1], tokens, n, tokens.n_kv_heads, "out[1]")
     st = _enter(ctx, out)
@@ -646,13 +655,12 @@ def mure_tokens_read(tokens: Tokens, plan: TokensPlan, new: bool = False, out=No
 def mure_tokens_attend(tokens: Tokens, plan: TokensPlan, q, out=None, lse: bool = False):
     """Attention of the batch's new tokens q [tokens][n_heads][head_dim] over their sequences' cells:
     out (same shape), with lse=True also the logs of the rows' sums, fp32 [tokens][n_heads]."""
-    import torch
     ctx, n = tokens.ctx, plan.n_new
     qr = _token_rows(q, tokens, n, plan.n_heads, "q")
     if out is None:
-        out = torch.empty((n, plan.n_heads, tokens.head_dim), dtype=tokens.torch_dtype, device=tokens.torch_device)
+        out = q.new_empty((n, plan.n_heads, tokens.head_dim))
     orow = _token_rows(out, tokens, n, plan.n_heads, "out")
-    ls = torch.empty((n, plan.n_heads), dtype=torch.float32, device=tokens.torch_device) if lse else None
+    ls = q.new_empty((n, plan.n_heads), dtype=tokens.torch_float) if lse else None
     st = _enter(ctx, (q, out, ls))
     ctx.check(lib().mure_tokens_attend(tokens.h, plan.h, qr, orow, ls.data_ptr() if lse else None))
     _leave(st)
