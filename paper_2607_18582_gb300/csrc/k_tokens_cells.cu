@@ -6,6 +6,8 @@
 // rows at a time: all its loads are on their way before the first is used.  The threads of a row are a
 // power-of-two group of a warp, so the row's largest magnitude is a few shuffles away and an e4m3 row is
 // quantised in the pass that copies it.  A block takes a tile of 16 tokens of one sequence.
+#include <type_traits>
+
 #include "tokens_util.cuh"
 
 namespace mure {
@@ -202,7 +204,7 @@ __global__ void __launch_bounds__(kThreads) k_tokens_read(CellParams p)
     }
 }
 
-// Whole pages of codes as 16-bit pages, in the order of the list.
+// Whole pages of codes as 16-bit pages, in the order of the list; f16: of half the values.
 template <class T>
 __global__ void __launch_bounds__(kThreads) k_tokens_widen(TokPool p, const int32_t *pages, int64_t rows, int lanes, T *k, T *v)
 {
@@ -214,6 +216,14 @@ __global__ void __launch_bounds__(kThreads) k_tokens_widen(TokPool p, const int3
         float x[8], y[8];
         cell8<T, true>(p.k, p.ks, row, p.d, c, x);
         cell8<T, true>(p.v, p.vs, row, p.d, c, y);
+        if constexpr (std::is_same<T, __half>::value) {
+            // halves: a code may have been rounded up past f16's largest value (65,504 to 65,536)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[i] *= 0.5f;
+                y[i] *= 0.5f;
+            }
+        }
         store8(k + r * p.d + c, 1, x);
         store8(v + r * p.d + c, 1, y);
     }

@@ -3,15 +3,15 @@
 // A sequence's cells are read once per cached head, all query heads of the group as the 16 rows of
 // one mma tile, so the kernel is bound by device memory: 4 D flops per row and cell against
 // 2 D bytes a cell.  What decides is the bytes in flight and an even split:
-//   - the cells of all (sequence, cached head) pairs form one line of tiles, cut into equal
-//     shares, one per resident block; a pair that is cut is joined by the block that finishes
-//     last, in the order of its parts (equal bits whatever the order of arrival);
+//   - the (sequence, cached head) pairs are dealt out whole to the resident blocks, the longest first,
+//     those that do not fit an even share in parts; a pair that is cut is joined by the block that
+//     finishes last, in the order of its parts (equal bits whatever the order of arrival);
 //   - each warp of a block takes a quarter of every tile with a running maximum and sum of its
 //     own, and a ring of cp.async stages of its own: no barrier in the loop;
 //   - e4m3 codes are widened in registers to f16 (one conversion for two, exact), whatever the rows' type:
 //     bf16 rows of q become f16 ones with their largest magnitude brought to 8 .. 16 by a power of two,
 //     exact down to 2^-18 of it.  A cell's scale of K goes to its score and that of V, relative to the
-//     largest met so far, to its probability, in fp32 (64 products of values saved per step).
+//     largest met so far, to its probability, in fp32 (scales far below the largest: in part to the values).
 // fp32 rows take the same way with TF32 products: every operand is split in two TF32 halves, a = a_hi + a_lo,
 // and a product is a_hi b_hi + a_hi b_lo + a_lo b_hi (codes are TF32 values as they are: two products).
 // What a row's scores are taken relative to lies 7 below their running maximum and moves only when that
@@ -48,8 +48,9 @@ struct Few {
     static constexpr bool kSharedQ = DP > 128 || kF32 || E4M3;
     static constexpr int kQSteps = kF32 ? DP / 8 : DP / 16;
     static constexpr int kQ = kSharedQ ? kQSteps * 32 * 16 : 0;
-    static constexpr int kFactors = E4M3 ? kWarps * 2 * 32 * 4 : 0;          // a step's scales, as factors
+    static constexpr int kFactors = E4M3 ? kWarps * 3 * 32 * 4 : 0;          // a step's scales, as factors
     static constexpr int kSmem = (kRing > kJoin ? kRing : kJoin) + kQ + kFactors;
+    static_assert(kSmem >= kMostParts * kFewRows * 4, "a unit's weights of parts do not fit");
     static constexpr int kBlocks = kSmem > 110 * 1024 ? 1 : DP > 128 || kSmem > 74 * 1024 || (kF32 && E4M3 && DP > 64) ? 2 : 3;   // per SM
 };
 
@@ -194,6 +195,13 @@ __device__ __forceinline__ uint32_t widen(uint32_t two)
     uint32_t h;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
     return h;
+}
+
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
 
 // Two neighbouring values of a row of q (element offset even; rows may start anywhere).
@@ -406,12 +414,13 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
             asm volatile("cp.async.wait_group %0;" ::"n"(F::kStages - 1) : "memory");
             __syncwarp();
             const uint32_t qs = su32(smem) + F::kSmem - F::kFactors - F::kQ + lane * 16;
-            const uint32_t factors = su32(smem) + F::kSmem - F::kFactors + warp * 256;
+            const uint32_t factors = su32(smem) + F::kSmem - F::kFactors + warp * 384;
             const uint32_t st = ring + slot * F::kStageAl;
             slot = slot + 1 == F::kStages ? 0 : slot + 1;
             int start, begin, end;
             range(tile, start, begin, end);
             if (start >= end || start + WK <= begin) { __syncwarp(); continue; }
+            bool split = false;
             if constexpr (E4M3) {
                 // a cell's scales by its lane: K's as a factor of its scores, V's of its probabilities,
                 // relative to the largest scale of V so far
@@ -428,9 +437,16 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                         v_top = most;
                     }
                 }
-                float *mine = reinterpret_cast<float *>(smem + F::kSmem - F::kFactors) + warp * 64 + lane;   // of K, then of V
+                float *mine = reinterpret_cast<float *>(smem + F::kSmem - F::kFactors) + warp * 96 + lane;   // of K, of V (to the
+                // probability, to the value)
+                // (a scale below 2^-7 of the largest: 2^-14 .. 1 of it goes to the values instead, so that the
+                // probability keeps its bits in f16)
+                const int low = F::kF32 || !in || yv == 255u || yv == 0u ? 0 : (int)yv - v_top;
+                split = !F::kF32 && __any_sync(0xffffffffu, low < -7);
+                const int to_value = split ? max(low, -14) : 0;
                 mine[0] = scale_of(yk);
-                mine[32] = yv == 255u || F::kF32 ? scale_of(yv) : scale_of((uint32_t)max(127 + (int)yv - v_top, 0));
+                mine[32] = yv == 255u || F::kF32 ? scale_of(yv) : scale_of((uint32_t)max(127 + (int)yv - v_top - to_value, 0));
+                if (split) mine[64] = __uint_as_float((uint32_t)(15 + to_value) << 10);   // 2^to_value in f16
                 __syncwarp();
             }
 
@@ -601,32 +617,46 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                     }
                 }
             } else {
+            auto products = [&](auto with_split) {
+                constexpr bool kSplit = decltype(with_split)::value;
 #pragma unroll
-            for (int kg = 0; kg < WK / 16; ++kg) {
-                uint32_t a[4];
+                for (int kg = 0; kg < WK / 16; ++kg) {
+                    uint32_t a[4], vs[2] = {0, 0};
 #pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const float *x = s[2 * kg + hh];
-                    a[2 * hh] = M::pack(x[0], x[1]);
-                    a[2 * hh + 1] = M::pack(x[2], x[3]);
-                }
-#pragma unroll
-                for (int c = 0; c < F::kRow / 16; c += 2) {
-                    uint32_t r[4];
-                    ldsm4t(vst + swz<F::kRow, false>(kg * 16 + (lane & 15), (c + (lane >> 4)) * 16, true), r);
-                    if (E4M3) {
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const uint32_t r0 = r[2 * i], r1 = r[2 * i + 1];
-                            M::go(o[2 * (c + i)], a, widen(__byte_perm(r0, 0, 0x4420)), widen(__byte_perm(r1, 0, 0x4420)));
-                            M::go(o[2 * (c + i) + 1], a, widen(__byte_perm(r0, 0, 0x4431)), widen(__byte_perm(r1, 0, 0x4431)));
+                    for (int hh = 0; hh < 2; ++hh) {
+                        const float *x = s[2 * kg + hh];
+                        a[2 * hh] = M::pack(x[0], x[1]);
+                        a[2 * hh + 1] = M::pack(x[2], x[3]);
+                        if (kSplit) {
+                            const float2 f = lds8(factors + (64 + kg * 16 + hh * 8 + 2 * t) * 4);
+                            vs[hh] = __float_as_uint(f.x) | __float_as_uint(f.y) << 16;
                         }
-                    } else {
-                        M::go(o[c], a, r[0], r[1]);
-                        M::go(o[c + 1], a, r[2], r[3]);
+                    }
+#pragma unroll
+                    for (int c = 0; c < F::kRow / 16; c += 2) {
+                        uint32_t r[4];
+                        ldsm4t(vst + swz<F::kRow, false>(kg * 16 + (lane & 15), (c + (lane >> 4)) * 16, true), r);
+                        if (E4M3) {
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                uint32_t e0 = widen(__byte_perm(r[2 * i], 0, 0x4420)), e1 = widen(__byte_perm(r[2 * i + 1], 0, 0x4420));
+                                uint32_t u0 = widen(__byte_perm(r[2 * i], 0, 0x4431)), u1 = widen(__byte_perm(r[2 * i + 1], 0, 0x4431));
+                                if (kSplit) {
+                                    e0 = hmul2(e0, vs[0]); u0 = hmul2(u0, vs[0]);
+                                    e1 = hmul2(e1, vs[1]); u1 = hmul2(u1, vs[1]);
+                                }
+                                M::go(o[2 * (c + i)], a, e0, e1);
+                                M::go(o[2 * (c + i) + 1], a, u0, u1);
+                            }
+                        } else {
+                            M::go(o[c], a, r[0], r[1]);
+                            M::go(o[c + 1], a, r[2], r[3]);
+                        }
                     }
                 }
-            }
+            };
+            if (E4M3 && split) products(std::true_type{});
+            else products(std::false_type{});
             }
             __syncwarp();
         }

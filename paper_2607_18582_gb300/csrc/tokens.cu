@@ -105,6 +105,7 @@ struct Shape {
     int tile;      // cells
     int align;     // of the first tile past the sinks
     int blocks;    // that run at a time
+    int least;     // tiles of a part, at least
 };
 
 void add_units(std::vector<Unit> &units, const TokSeq &q, int seq, int hk, int group, int window, int sinks, const Shape &sh)
@@ -130,68 +131,26 @@ void add_units(std::vector<Unit> &units, const TokSeq &q, int seq, int hk, int g
         }
 }
 
-// The units' tiles as one line, cut into equal shares, one per block that runs at a time; a unit that
-// is cut gets a slot for every part's result.
+// A kernel's pieces, block by block.
 struct Shares {
     std::vector<TokItem> items, cut;   // cut: the first part of every cut unit
     std::vector<int32_t> first;
     int parts = 0;
 };
 
-Shares share(const std::vector<Unit> &units, const Shape &sh)
-{
-    Shares r;
-    int64_t total = 0;
-    for (const Unit &u : units) total += std::max(u.tiles, 1);     // (rows without cells still get zeros)
-    const int64_t blocks = std::min<int64_t>(total, sh.blocks);
-    r.first.push_back(0);
-    int64_t at = 0;                                                 // of the line
-    int block = 0;
-    for (const Unit &u : units) {
-        const int64_t n = std::max(u.tiles, 1);
-        const size_t i0 = r.items.size();
-        for (int64_t t = 0; t < n;) {
-            while (at >= total * (block + 1) / blocks) {
-                r.first.push_back((int32_t)r.items.size());
-                ++block;
-            }
-            const int64_t take = std::min(n - t, total * (block + 1) / blocks - at);
-            TokItem w = u.item;
-            w.t0 = (int)t;
-            w.t1 = (int)std::min<int64_t>(t + take, u.tiles);
-            w.parts = 1;
-            r.items.push_back(w);
-            t += take;
-            at += take;
-        }
-        const int parts = (int)(r.items.size() - i0);
-        if (parts > 1) {
-            for (int k = 0; k < parts; ++k) {
-                TokItem &w = r.items[i0 + k];
-                w.part0 = r.parts; w.part = r.parts + k; w.parts = parts; w.unit = (int)r.cut.size();
-            }
-            r.parts += parts;
-            r.cut.push_back(r.items[i0]);
-        }
-    }
-    r.first.push_back((int32_t)r.items.size());
-    if (units.empty()) r.first.assign(1, 0);
-    return r;
-}
-
-// The same for the kernel for chunks, whose pieces read the same cells again for every 256 rows: whole
-// units, the longest first, each to the block with the least work, while they fit its share; the units
-// that are left are cut to fill the blocks up.  Units of one sequence have about one length, so
-// blocks that work at a time read the same cells (a batch whose cells exceed the L2 cache: 880 MB
-// from device memory where shares were cut along the line).  A unit that is cut writes and
-// reads its sums once more, so few are.
+// Whole units, the longest first, each to the block with the least work, while they fit its share; the
+// units that are left are cut to fill the blocks up.  Units of one sequence have about one length, so
+// blocks that work at a time read the same cells (chunks of a batch whose cells exceed the L2 cache:
+// 880 MB from device memory where shares were cut along the line).  A unit that is cut writes and
+// reads its sums once more and starts twice, so few are: one that is little longer than a share and
+// has a block to itself stays whole.
 Shares pack(const std::vector<Unit> &units, const Shape &sh)
 {
     Shares r;
     r.first.push_back(0);
     if (units.empty()) return r;
     // in tiles: a tile of one half (up to 128 rows) takes 0.6 of the time, a unit's beginning and end about 3
-    constexpr double kStart = 3.0;
+    constexpr double kStart = 3.0, kWhole = 1.3;
     auto tile_cost = [&](const Unit &u) { return u.item.rows > sh.rows / 2 ? 1.0 : 0.6; };
     auto cost = [&](const Unit &u) { return u.tiles * tile_cost(u) + kStart; };
     std::vector<int> order(units.size());
@@ -209,22 +168,23 @@ Shares pack(const std::vector<Unit> &units, const Shape &sh)
     for (int i : order) {
         const Unit &u = units[i];
         const Load l = least.top();
-        if (l.first + cost(u) > share) { left.push_back(i); continue; }
+        if (l.first + cost(u) > (l.first == 0 ? share * kWhole : share)) { left.push_back(i); continue; }
         least.pop();
         least.push({l.first + cost(u), l.second});
         TokItem w = u.item;
         w.t0 = 0; w.t1 = u.tiles; w.parts = 1;
         mine[l.second].push_back(w);
     }
-    constexpr int kLeast = 4;                                       // tiles of a part, at least
+    const double fill = share + kStart;                             // (a part of a unit starts once more)
     for (int i : left) {
         const Unit &u = units[i];
+        const int least_tiles = std::max(sh.least, (u.tiles + kMostParts - 1) / kMostParts);
         std::vector<std::pair<int, TokItem>> parts;
         for (int t = 0; t < u.tiles || (u.tiles == 0 && t == 0);) {
             const Load l = least.top();
             least.pop();
-            int take = std::max((int)((share - l.first - kStart) / tile_cost(u)), kLeast);
-            if (u.tiles - t - take < kLeast) take = u.tiles - t;
+            int take = std::max((int)((fill - l.first - kStart) / tile_cost(u)), least_tiles);
+            if (u.tiles - t - take < sh.least) take = u.tiles - t;
             TokItem w = u.item;
             w.t0 = t; w.t1 = t + take;
             parts.push_back({l.second, w});
@@ -338,8 +298,8 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
     const int group = b.n_heads / d.n_kv_heads;
     const bool wide = d.form == MURE_FORM_E4M3;
     const FewShape fshape = mure::few_shape(d.dtype, d.form, d.head_dim);
-    const Shape few_shape{kFewRows, fshape.tile, 16, fshape.blocks};
-    const Shape chunk_shape{kChunkRows, kChunkTile, chunk_box(d.page_size), chunk_blocks()};
+    const Shape few_shape{kFewRows, fshape.tile, 16, fshape.blocks, 2};
+    const Shape chunk_shape{kChunkRows, kChunkTile, chunk_box(d.page_size), chunk_blocks(), 4};
     std::vector<Unit> few, chunk;
     std::vector<int32_t> wide_table, wide_pages;
     std::unordered_map<int32_t, int32_t> wide_of;
@@ -363,7 +323,7 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
             wide_table[q.table0 + i] = at.first->second;
         }
     }
-    const Shares fs = share(few, few_shape), cs = pack(chunk, chunk_shape);
+    const Shares fs = pack(few, few_shape), cs = pack(chunk, chunk_shape);
     FAILIF(fs.items.size() + cs.items.size() > ((size_t)1 << 28), c, MURE_ERR_UNSUPPORTED, "more than 2^28 pieces of work");
 
     Image im;
@@ -628,7 +588,7 @@ mure_status mure_tokens_attend(mure_tokens *t, mure_tokens_plan *p, const mure_t
                 c->launches += launch_tokens_widen(pool_of(t), d.dtype, p->wide_pages, p->n_wide, pool.k, pool.v, c->stream);
             }
             c->launches += launch_tokens_chunk(pool, b, p->chunk, d.dtype, qr, orow, lse, wide ? p->n_wide : d.n_pages,
-                                               wide ? p->map_k : t->map_k, wide ? p->map_v : t->map_v, c->err_dev, c->wait_limit,
+                                               wide ? p->map_k : t->map_k, wide ? p->map_v : t->map_v, wide, c->err_dev, c->wait_limit,
                                                c->stream);
         }
         check_launch(c);

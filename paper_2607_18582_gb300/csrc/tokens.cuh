@@ -70,6 +70,7 @@ struct TokWork {
 
 // Rows of a piece and cells of a tile of the kernel for few rows.
 constexpr int kFewRows = 16;
+constexpr int kMostParts = 512;       // of a unit
 struct FewShape {
     int tile, blocks;                 // cells of a tile; blocks that run at a time
 };
@@ -91,8 +92,10 @@ int chunk_box(int page_size);         // cells of a box its copies take (and its
 int64_t chunk_part_floats(int d);
 bool chunk_map(CUtensorMap &map, void *pool, int dtype, int hk, int d, int page_size, int64_t n_pages);
 int launch_tokens_chunk(const TokPool &pool, const TokBatch &b, const TokChunk &c, int dtype, TokRows q, TokRows out, float *lse,
-                        int64_t n_pages, const CUtensorMap &map_k, const CUtensorMap &map_v, int *err, int64_t spin, cudaStream_t s);
-// E4M3 pages pages[0 .. n_list) as pages 0 .. n_list - 1 of 16-bit pools k and v.
+                        int64_t n_pages, const CUtensorMap &map_k, const CUtensorMap &map_v, bool widened, int *err, int64_t spin,
+                        cudaStream_t s);
+// E4M3 pages pages[0 .. n_list) as pages 0 .. n_list - 1 of 16-bit pools k and v (f16: of half the values),
+// which launch_tokens_chunk takes as `widened`.
 int launch_tokens_widen(const TokPool &pool, int dtype, const int32_t *pages, int64_t n_list, void *k, void *v, cudaStream_t s);
 
 int launch_tokens_append(const TokPool &pool, const TokBatch &b, int dtype, int form, TokRows k, TokRows v, int64_t tiles,

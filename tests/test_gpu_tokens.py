@@ -401,6 +401,18 @@ def test_scales_of_all_sizes(M, ctx, dtype, d):
         t.check()
 
 
+@pytest.mark.parametrize("new", [1, 100])
+def test_largest_f16_values_as_codes(M, ctx, new):
+    """f16 values whose nearest code stands for 65,536: attention takes them as finite."""
+    t = Batch(M, ctx, [new], [60], [60 + new], 2, 1, 64, 16, "f16", "e4m3")
+    big = torch.full((60, 1, 64), 65504.0, device="cuda", dtype=torch.float16)
+    big[::2] = -60000.0
+    plan = M.mure_tokens_plan(t.cache, 2, [60], [0], [60], t.table)
+    M.mure_tokens_append(t.cache, plan, big * 2.0 ** -20, big)
+    out, _ = t.check()
+    assert bool(torch.isfinite(out).all())
+
+
 @pytest.mark.parametrize("dtype,form", [("bf16", "same"), ("bf16", "e4m3"), ("f32", "same")])
 def test_offsets_past_32_bits(M, ctx, dtype, form):
     """Pages at the far end of pools of more than 2^31 values."""
