@@ -14,8 +14,8 @@
 //   9, 10     copy K and V tiles by tensor maps, a box per page (or 128 cells of a larger page).
 // What a row's scores are taken relative to lies 7 below their running maximum and moves only when that
 // grows by more than 8 (in powers of two; f16 holds powers up to 2^15, and those down to 2^-21 of the
-// largest keep all its bits), so O is hardly ever rescaled; where it is, S's arrival has shown that
-// every earlier product is done.  Whole units of work go to the CTAs, the longest first; the ones that
+// largest keep all its bits), so O is hardly ever rescaled; where it is, S's arrival (or, where P lies
+// beside S, a barrier of the product's own) has shown that every earlier product is done.  Whole units of work go to the CTAs, the longest first; the ones that
 // do not fit an even share are cut along the cells and joined by a second kernel in the order of
 // their parts.
 // Every wait is bounded, as in the GEMM kernel.
@@ -39,6 +39,11 @@ struct Chunk {
     static constexpr uint32_t kQ = 2 * kPanels * kPanel;            // two row tiles
     static constexpr uint32_t kStage = kPanels * kPanel;            // a K or V tile
     static constexpr int kStages = DP == 64 ? 8 : 4;
+    // Tensor memory: S of both row tiles in columns 0 .. 255, O from 256.  P lies over half of S, or for
+    // up to 64 values, where O leaves room, beside it: the next scores then need not wait for P V.
+    static constexpr bool kApart = DP == 64;
+    static __device__ __forceinline__ uint32_t col_p(int h) { return kApart ? 384 + h * 64 : h * 128 + 64; }
+    static __device__ __forceinline__ uint32_t col_o(int h) { return 256 + h * DP; }
     static constexpr uint32_t kSmem = kQ + kStages * kStage + 1024; // (+ room to align to 1024)
 };
 
@@ -177,7 +182,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
     using C = Chunk<DP>;
     extern __shared__ char smem_raw[];
     // stages 0 .. kStages / 2 - 1 hold K tiles, the others V tiles
-    __shared__ __align__(8) uint64_t bar_full[C::kStages], bar_empty[C::kStages], bar_q[2], bar_s[2], bar_p[2][2], bar_o[2], bar_turn[2], bar_drain[2];
+    __shared__ __align__(8) uint64_t bar_full[C::kStages], bar_empty[C::kStages], bar_q[2], bar_s[2], bar_p[2][2], bar_o[2], bar_pv[2], bar_turn[2], bar_drain[2];
     __shared__ uint32_t tmem_sh;
     __shared__ WaitCtl ctl_sh;
     __shared__ TokItem item_sh[12];           // each warp's piece of work
@@ -205,6 +210,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
             mbar_init(smem_u32(&bar_p[h][0]), 4);
             mbar_init(smem_u32(&bar_p[h][1]), 4);
             mbar_init(smem_u32(&bar_o[h]), 1);
+            mbar_init(smem_u32(&bar_pv[h]), 1);
             mbar_init(smem_u32(&bar_turn[h]), 1);
             mbar_init(smem_u32(&bar_drain[h]), 1);
         }
@@ -227,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
         // ------------------------------------------------------------------ softmax --
         const int h = warp >> 2, r = threadIdx.x & 127;              // row tile, row of it
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tS = tmem + lanes + h * 128, tP = tS + 64, tO = tmem + lanes + 256 + h * 128;
+        const uint32_t tS = tmem + lanes + h * 128, tP = tmem + lanes + C::col_p(h), tO = tmem + lanes + C::col_o(h);
         const uint32_t qs = q_smem + h * C::kPanels * kPanel;
         uint32_t n_s = 0, n_o = 0;                                   // phases waited for
         bool ok = true;
@@ -278,25 +284,36 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 // a cell of the tile a row may attend to: i <= last and (i >= first or i < sink)
                 const int last = min(tc.end - 1, at) - tc.start, sink = p.b.sinks - tc.start;
                 const int first = p.b.window ? at - p.b.window + 1 - tc.start : 0;
-                auto mask = [&](uint32_t *x, int i0, int n) {
+                auto mask = [&](uint32_t *x, int i0) {               // 32 cells: a bit each
                     if (open) return;
+                    auto below = [&](int n) { return n <= i0 ? 0u : n >= i0 + 32 ? ~0u : (1u << (n - i0)) - 1u; };
+                    const uint32_t bits = below(last + 1) & (~below(first) | below(sink));
 #pragma unroll
-                    for (int i = 0; i < n; ++i)
-                        if (i0 + i > last || (i0 + i < first && i0 + i >= sink)) x[i] = 0xFF800000u;
+                    for (int i = 0; i < 32; ++i) x[i] = bits & (1u << i) ? x[i] : 0xFF800000u;
                 };
+                // short: at most 64 cells take part (sinks, ends)
+                auto softmax = [&](auto of_short) {
+                constexpr bool kShort = decltype(of_short)::value;
                 // The maximum of the scores; those of the second 64 cells stay in registers.
                 float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 uint32_t s[64];
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
+                    if (c == 1 && kShort) continue;
                     tmem_ld32(tS + c * 64, s);
                     tmem_ld32(tS + c * 64 + 32, s + 32);
                     tmem_wait_ld();
-                    mask(s, c * 64, 64);
+                    mask(s, c * 64);
+                    mask(s + 32, c * 64 + 32);
 #pragma unroll
                     for (int i = 0; i < 64; ++i) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(s[i]));
                 }
                 const float mt = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.b.scale_log2;
+                if (C::kApart && t > t0) {                           // the product before has read P and added to O
+                    ok = warp_wait_phase(smem_u32(&bar_pv[h]), (n_s - 2) & 1, ctl);
+                    if (!ok) return;
+                    fence_after();
+                }
                 const bool up = mt > m + 15.f;
                 if (__any_sync(0xffffffffu, up)) {
                     const float mn = up ? mt - 7.f : m, keep = up ? ex2(m - mn) : 1.f;
@@ -333,10 +350,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 // fetched once more.  The products with all but cells 32 .. 63 start as soon as those are there.
                 uint32_t x[32];
                 tmem_ld32(tS, x);
-                powers(s, tP + 32);
-                powers(s + 32, tP + 48);
+                if (!kShort) {
+                    powers(s, tP + 32);
+                    powers(s + 32, tP + 48);
+                }
                 tmem_wait_ld();
-                mask(x, 0, 32);
+                mask(x, 0);
                 powers(x, tP);
                 tmem_ld32(tS + 32, x);
                 tmem_wait_st();
@@ -344,13 +363,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&bar_p[h][1]));
                 tmem_wait_ld();
-                mask(x, 32, 32);
+                mask(x, 32);
                 powers(x, tP + 16);
                 l += unpack2(sum).x + unpack2(sum).y;
                 tmem_wait_st();
                 fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&bar_p[h][0]));
+                };
+                // (with D = 128 the second body's registers cost more than the short tiles: 1,170 -> 1,207 us)
+                if (DP == 64 && tc.end - tc.start <= 64) softmax(std::integral_constant<bool, DP == 64>{});
+                else softmax(std::false_type{});
+                if (!ok) break;
             }
             if (!ok) break;
             bool have = t1 > t0;                                     // (no cells: zeros)
@@ -471,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
         const int h = warp == 8 ? 0 : 1;
         uint32_t n_q = 0, n_p = 0, n_turn = 0, n_k = 0, n_v = 0;     // phases; K and V tiles taken
         const uint32_t id_s = idesc_16<T>(kCells, false), id_o = idesc_16<T>((D + 15) & ~15, true);
-        const uint32_t tS = tmem + h * 128, tP = tS + 64, tO = tmem + 256 + h * 128;
+        const uint32_t tS = tmem + h * 128, tP = tmem + C::col_p(h), tO = tmem + C::col_o(h);
         const int ks_q = (D + 15) / 16;
         const uint64_t qd = sw128_desc(q_smem + h * C::kPanels * kPanel);
         bool ok = true;
@@ -546,14 +570,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 if (!ok) break;
                 ++n_p;
                 fence_after();
+                if (C::kApart && more) {
+                    ok = warp_wait_phase(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
+                    if (!ok) break;
+                    fence_after();
+                    scores(n_k % NS, false);
+                    ++n_k;
+                }
                 if (elect_one()) {                                   // cells 32 .. 63
                     if (ks_v > 2) product(2, 1);
+                    if (C::kApart && rows > 128) mbar_arrive(smem_u32(&bar_turn[1 - h]));
                     if (ks_v > 3) product(3, 1);
                     mma_commit(smem_u32(&bar_empty[v_stage]));
+                    if (C::kApart) mma_commit(smem_u32(&bar_pv[h]));
                     if (!more) mma_commit(smem_u32(&bar_o[h]));
                 }
                 __syncwarp();
-                if (more) {
+                if (C::kApart) {
+                } else if (more) {
                     ok = warp_wait_phase(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
                     if (!ok) break;
                     fence_after();
