@@ -463,8 +463,9 @@ void mure_tokens_plan_free(mure_tokens_plan *plan);
 
 /* Rows of activations: element (token, head, i) of a batch's packed tokens (the new
  * tokens of sequence 0, then those of sequence 1, ...) is at
- * p[token * token_stride + head * head_stride + i].  Strides count elements; rows need no
- * more than their type's alignment (16-byte aligned rows are copied faster). */
+ * p[token * token_stride + head * head_stride + i].  Strides count elements, 0..2^40; rows
+ * need no more than their type's alignment (16-byte aligned rows are copied faster).
+ * Outputs must not overlap inputs; an output's rows must not overlap one another. */
 typedef struct {
     void *p;                            /* device; may be NULL where the batch has no such rows */
     int64_t token_stride, head_stride;
@@ -485,15 +486,20 @@ mure_status mure_tokens_read(mure_tokens *tokens, mure_tokens_plan *plan, int32_
  * over the cells each may attend to, sums held in fp32; a token that may attend to none
  * gets zeros.  lse (nullable, device fp32 [tokens][n_heads], dense): log of the sum of
  * exp(scale q k), -inf where there are no cells.  16-bit types: the probabilities are
- * rounded to 16 bits before their product with v.  fp32: products and sums have fp32
- * accuracy.  Cells that a token may not attend to never reach its output, whatever they
- * hold.  Equal calls give equal bits.  Errors: INVALID_ARG (as above), CUDA. */
+ * rounded to 16 bits before their product with v; on e4m3 cells a value of magnitude
+ * below 2^-20 of the largest that the batch's row meets may lose bits with a small
+ * probability.  fp32: products and sums have fp32 accuracy.  Cells that a token may not
+ * attend to never reach its output, whatever they hold; where a cell that it may attend to
+ * holds a NaN its output is NaN.  Equal calls give equal bits; the same row in another
+ * batch may differ in its last ones (the split of its cells differs).  Errors:
+ * INVALID_ARG (as above), CUDA. */
 mure_status mure_tokens_attend(mure_tokens *tokens, mure_tokens_plan *plan, const mure_tokens_rows *q,
                                const mure_tokens_rows *out, float *lse);
 
 /* Wait for everything queued on the context's stream.  Errors: TIMEOUT (a device-side
- * wait of a token call gave up; the outputs of the token calls since the last
- * synchronisation are undefined, the context stays usable), CUDA. */
+ * wait of a token call gave up: see mure_set_wait_limit; the outputs of the token calls
+ * since the last synchronisation are undefined, the context stays usable.  A
+ * synchronous call of the context that comes first reports it instead), CUDA. */
 mure_status mure_synchronize(mure_ctx *ctx);
 
 #ifdef __cplusplus

@@ -164,6 +164,22 @@ template <> __device__ __forceinline__ uint32_t narrow2<__half>(float lo, float 
     return r;
 }
 
+// warp_wait_phase, for waits that are shorter than the hardware suspends a waiting thread: the first look
+// does not suspend, so that a limit below kLook cycles (a test of what follows an expired wait) expires.
+constexpr int kLook = 64;
+__device__ __forceinline__ bool warp_wait(uint32_t a, uint32_t parity, volatile WaitCtl *ctl)
+{
+    uint32_t there;
+    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(there) : "r"(a), "r"(parity) : "memory");
+    bool ok = there != 0;
+    if (!ok) {
+        if (ctl->limit < kLook) ctl->abort = 1;
+        else ok = wait_phase(a, parity, ctl);
+    }
+    return __all_sync(0xffffffffu, ok);
+}
+
 // The tiles of a piece: cells [start, start + kCells), of which those below end take part (cells
 // before the first one of b0 .. are before every row's window).
 struct TileCells {
@@ -277,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 const TileCells tc = tile_cells(w, t, p.box);
                 const bool open = tc.start + kCells <= tc.end && tc.start + kCells - 1 <= lo &&
                                   (p.b.window == 0 || tc.start > hi - p.b.window);
-                ok = warp_wait_phase(smem_u32(&bar_s[h]), n_s & 1, ctl);
+                ok = warp_wait(smem_u32(&bar_s[h]), n_s & 1, ctl);
                 if (!ok) break;
                 ++n_s;
                 fence_after();
@@ -310,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 }
                 const float mt = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.b.scale_log2;
                 if (C::kApart && t > t0) {                           // the product before has read P and added to O
-                    ok = warp_wait_phase(smem_u32(&bar_pv[h]), (n_s - 2) & 1, ctl);
+                    ok = warp_wait(smem_u32(&bar_pv[h]), (n_s - 2) & 1, ctl);
                     if (!ok) return;
                     fence_after();
                 }
@@ -379,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
             if (!ok) break;
             bool have = t1 > t0;                                     // (no cells: zeros)
             if (have) {
-                ok = warp_wait_phase(smem_u32(&bar_o[h]), n_o & 1, ctl);
+                ok = warp_wait(smem_u32(&bar_o[h]), n_o & 1, ctl);
                 if (!ok) break;
                 ++n_o;
                 fence_after();
@@ -528,16 +544,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 // no rows here: the stages go by one at a time (a barrier's parity names a phase only to
                 // a waiter that is at most one behind)
                 for (int t = t0; t < t1 && ok; ++t, ++n_k, ++n_v) {
-                    ok = warp_wait_phase(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
+                    ok = warp_wait(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
                     if (ok && lane == 0) mbar_arrive(smem_u32(&bar_empty[n_k % NS]));
-                    ok = ok && warp_wait_phase(smem_u32(&bar_full[NS + n_v % NS]), (n_v / NS) & 1, ctl);
+                    ok = ok && warp_wait(smem_u32(&bar_full[NS + n_v % NS]), (n_v / NS) & 1, ctl);
                     if (ok && lane == 0) mbar_arrive(smem_u32(&bar_empty[NS + n_v % NS]));
                 }
                 continue;
             }
-            ok = warp_wait_phase(smem_u32(&bar_q[h]), n_q++ & 1, ctl);
+            ok = warp_wait(smem_u32(&bar_q[h]), n_q++ & 1, ctl);
             if (!ok || t1 <= t0) continue;                           // (rows without cells: their Q is not read)
-            ok = warp_wait_phase(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
+            ok = warp_wait(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
             if (!ok) break;
             fence_after();
             scores(n_k % NS, false);
@@ -549,9 +565,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 const bool more = t + 1 < t1;
                 const uint64_t b = mn_desc(ring + v_stage * C::kStage);
                 // (turn n of warp 8 follows turn n - 1 of warp 11, turn n of warp 11 turn n of warp 8)
-                ok = warp_wait_phase(smem_u32(&bar_full[v_stage]), (n_v / NS) & 1, ctl) &&
-                     warp_wait_phase(smem_u32(&bar_p[h][1]), n_p & 1, ctl) &&
-                     (rows <= 128 || (h == 0 && n_turn == 0) || warp_wait_phase(smem_u32(&bar_turn[h]), (n_turn - (h == 0)) & 1, ctl));
+                ok = warp_wait(smem_u32(&bar_full[v_stage]), (n_v / NS) & 1, ctl) &&
+                     warp_wait(smem_u32(&bar_p[h][1]), n_p & 1, ctl) &&
+                     (rows <= 128 || (h == 0 && n_turn == 0) || warp_wait(smem_u32(&bar_turn[h]), (n_turn - (h == 0)) & 1, ctl));
                 if (!ok) break;
                 fence_after();
                 auto product = [&](int ks, uint32_t acc) { mma_ts(tO, tP + ks * 8, b + (uint64_t)(ks * (2048 >> 4)), id_o, acc); };
@@ -566,12 +582,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                     }
                 }
                 __syncwarp();
-                ok = warp_wait_phase(smem_u32(&bar_p[h][0]), n_p & 1, ctl);
+                ok = warp_wait(smem_u32(&bar_p[h][0]), n_p & 1, ctl);
                 if (!ok) break;
                 ++n_p;
                 fence_after();
                 if (C::kApart && more) {
-                    ok = warp_wait_phase(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
+                    ok = warp_wait(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
                     if (!ok) break;
                     fence_after();
                     scores(n_k % NS, false);
@@ -588,7 +604,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 __syncwarp();
                 if (C::kApart) {
                 } else if (more) {
-                    ok = warp_wait_phase(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
+                    ok = warp_wait(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
                     if (!ok) break;
                     fence_after();
                     scores(n_k % NS, rows > 128);
@@ -629,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 const int start = tile_cells(w, t, p.box).start;
                 const uint32_t s = which * NS + load % NS, bar = smem_u32(&bar_full[s]);
                 if (load >= NS) {
-                    ok = warp_wait_phase(smem_u32(&bar_empty[s]), (load / NS - 1) & 1, ctl);
+                    ok = warp_wait(smem_u32(&bar_empty[s]), (load / NS - 1) & 1, ctl);
                     if (!ok) break;
                 }
                 __syncwarp();

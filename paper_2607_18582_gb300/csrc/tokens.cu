@@ -6,7 +6,6 @@
 // layers' calls of a step share it.
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 #include <cstring>
 #include <memory>
 #include <numeric>
@@ -48,7 +47,7 @@ namespace {
 
 // E4M3 rows of a sequence and head up to which the kernel for few rows takes them.
 constexpr int kFewRowsWide = 64;
-constexpr int64_t kMostPos = int64_t(1) << 30;
+constexpr int64_t kMostPos = int64_t(1) << 30, kMostStride = int64_t(1) << 40, kMostUnits = int64_t(1) << 24;
 
 int elt_bytes(int dtype) { return dtype == MURE_F32 ? 4 : 2; }
 
@@ -308,8 +307,10 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
         const int64_t rows = (int64_t)q.n_new * group;
         FAILIF(rows > kMostPos, c, MURE_ERR_UNSUPPORTED, "sequence %d: more than 2^30 rows", s);
         const bool as_chunk = d.dtype != MURE_F32 && d.head_dim <= kChunkDim && rows > (wide ? kFewRowsWide : kFewRows);
-        add_units(as_chunk ? chunk : few, q, s, d.n_kv_heads, group, b.window, b.sinks, as_chunk ? chunk_shape : few_shape);
-        FAILIF(few.size() + chunk.size() > ((size_t)1 << 27), c, MURE_ERR_UNSUPPORTED, "more than 2^27 pieces of work");
+        const Shape &sh = as_chunk ? chunk_shape : few_shape;
+        FAILIF((int64_t)(few.size() + chunk.size()) + (rows + sh.rows - 1) / sh.rows * d.n_kv_heads > kMostUnits, c,
+               MURE_ERR_UNSUPPORTED, "more than 2^24 pieces of work");
+        add_units(as_chunk ? chunk : few, q, s, d.n_kv_heads, group, b.window, b.sinks, sh);
         if (!as_chunk || !wide) continue;
         // the pages that any of its rows reads
         wide_table.resize(table.size(), 0);
@@ -324,7 +325,6 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
         }
     }
     const Shares fs = pack(few, few_shape), cs = pack(chunk, chunk_shape);
-    FAILIF(fs.items.size() + cs.items.size() > ((size_t)1 << 28), c, MURE_ERR_UNSUPPORTED, "more than 2^28 pieces of work");
 
     Image im;
     const size_t o_seq = im.add(seq), o_table = im.add(table), o_new = im.add(tile_new), o_all = im.add(tile_all);
@@ -402,6 +402,8 @@ TokRows check_rows(mure_ctx *c, const mure_tokens_rows *r, const mure_tokens_des
     FAILIF(!r || !r->p, c, MURE_ERR_INVALID_ARG, "NULL %s", name);
     FAILIF((uintptr_t)r->p % e != 0, c, MURE_ERR_INVALID_ARG, "%s is not aligned to its type", name);
     o.p = static_cast<char *>(r->p);
+    FAILIF(r->token_stride < 0 || r->head_stride < 0 || r->token_stride > kMostStride || r->head_stride > kMostStride, c,
+           MURE_ERR_INVALID_ARG, "a stride of %s is not in 0..2^40", name);
     o.ts = r->token_stride;
     o.hs = r->head_stride;
     const int per = 16 / e;
@@ -413,7 +415,7 @@ TokRows check_rows(mure_ctx *c, const mure_tokens_rows *r, const mure_tokens_des
 void check_apart(mure_ctx *c, const TokRows &r, const mure_tokens_desc &d, int64_t rows, int heads, const char *name)
 {
     if (rows == 0) return;
-    const int64_t ts = std::llabs(r.ts), hs = std::llabs(r.hs), D = d.head_dim;
+    const int64_t ts = r.ts, hs = r.hs, D = d.head_dim;
     const bool ok = (heads == 1 || rows == 1) ? (heads == 1 || hs >= D) && (rows == 1 || ts >= D)
                                               : (hs >= D && ts >= hs * (heads - 1) + D) || (ts >= D && hs >= ts * (rows - 1) + D);
     FAILIF(!ok, c, MURE_ERR_INVALID_ARG, "rows of %s overlap", name);

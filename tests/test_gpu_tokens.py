@@ -579,6 +579,8 @@ def test_call_refusals(M, ctx):
     assert L.mure_tokens_read(t.cache.h, t.plan.h, 2, r(good), r(good)) == 1
     assert L.mure_tokens_attend(t.cache.h, t.plan.h, r(null), r(orow), None) == 1
     assert L.mure_tokens_attend(t.cache.h, t.plan.h, r(qrow), r(same), None) == 1
+    for bad in ((-256, 64), (256, -64), (2 ** 41, 64)):
+        assert L.mure_tokens_attend(t.cache.h, t.plan.h, r(rows(t.q.data_ptr(), *bad)), r(orow), None) == 1
     assert L.mure_tokens_attend(t.cache.h, t.plan.h, r(qrow), r(orow), out.data_ptr() + 2) == 1
     # another geometry's plan, another context's plan
     u = Batch(M, ctx, [2], [14], [16], 4, 2, 64, 8, "bf16", "same")
