@@ -393,12 +393,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 if (!ok) break;
             }
             if (!ok) break;
+            // the next piece's row of Q, to be at hand when this one's rows are out (not in registers: with
+            // 64 of them kept for it the rest spills)
+            const TokItem *after = p.w.items + min(it + 1, it1 - 1);
+            const int next_r0 = __ldg(&after->r0) + h * 128 + r, next_rows = __ldg(&after->rows);
+            const int next_row0 = __ldg(&after->row0), next_h = __ldg(&after->h);
             bool have = t1 > t0;                                     // (no cells: zeros)
             if (have) {
                 ok = warp_wait(smem_u32(&bar_o[h]), n_o & 1, ctl);
                 if (!ok) break;
                 ++n_o;
                 fence_after();
+            }
+            if (it + 1 < it1 && h * 128 + r < next_rows) {
+                const T *q = reinterpret_cast<const T *>(p.q.p) + (next_row0 + next_r0 / p.b.group) * p.q.ts +
+                             (next_h * p.b.group + next_r0 % p.b.group) * p.q.hs;
+                asm volatile("prefetch.global.L1 [%0];" ::"l"(q));
+                if (D > 64) asm volatile("prefetch.global.L1 [%0];" ::"l"(q + 64));
             }
             const int parts = w.parts, part = w.part;
             const int token = w.row0 + row / p.b.group, head = w.h * p.b.group + row % p.b.group;

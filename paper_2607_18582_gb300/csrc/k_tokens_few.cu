@@ -138,19 +138,20 @@ __device__ __forceinline__ void mma_tf32(float *c, const uint32_t *a, uint32_t b
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// c += a b, the operands in halves (b exact in TF32: EXACT); b0, b1 as fp32.
+// c += a_hi b_hi, x += the products with a low half (two accumulators: a product waits for the one before it
+// on the same); b0, b1 as fp32 (EXACT: they are TF32 values).
 template <bool EXACT>
-__device__ __forceinline__ void mma_f32(float *c, const uint32_t *hi, const uint32_t *lo, float b0, float b1)
+__device__ __forceinline__ void mma_f32(float *c, float *x, const uint32_t *hi, const uint32_t *lo, float b0, float b1)
 {
     if (EXACT) {
-        mma_tf32(c, lo, __float_as_uint(b0), __float_as_uint(b1));
+        mma_tf32(x, lo, __float_as_uint(b0), __float_as_uint(b1));
         mma_tf32(c, hi, __float_as_uint(b0), __float_as_uint(b1));
     } else {
         uint32_t h0, l0, h1, l1;
         halves(b0, h0, l0);
         halves(b1, h1, l1);
-        mma_tf32(c, lo, h0, h1);
-        mma_tf32(c, hi, l0, l1);
+        mma_tf32(x, lo, h0, h1);
+        mma_tf32(x, hi, l0, l1);
         mma_tf32(c, hi, h0, h1);
     }
 }
@@ -454,6 +455,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
 #pragma unroll
             for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
             if constexpr (F::kF32) {
+                float sx[NT][4] = {};
 #pragma unroll(DP > 128 ? 2 : 4)
                 for (int i = 0; i < DP / 16; ++i) {            // 16 values of a row: two steps
                     uint32_t hi[2][4], lo[2][4];
@@ -475,10 +477,14 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                         } else {
                             b = lds16(st + swz<F::kRow, true>(n * 8 + g, (4 * i + t) * 16, false));
                         }
-                        mma_f32<E4M3>(s[n], hi[0], lo[0], b.x, b.y);
-                        mma_f32<E4M3>(s[n], hi[1], lo[1], b.z, b.w);
+                        mma_f32<E4M3>(s[n], sx[n], hi[0], lo[0], b.x, b.y);
+                        mma_f32<E4M3>(s[n], sx[n], hi[1], lo[1], b.z, b.w);
                     }
                 }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[n][i] += sx[n][i];
             } else if constexpr (E4M3) {
 #pragma unroll
                 for (int kp = 0; kp < F::kRow / 64; ++kp) {        // four 16-byte chunks of eight rows
@@ -610,10 +616,21 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                             b0 = lds16(vst + swz<F::kRow, true>(n * 8 + 2 * t, (8 * J + g) * 16, true));
                             b1 = lds16(vst + swz<F::kRow, true>(n * 8 + 2 * t + 1, (8 * J + g) * 16, true));
                         }
-                        mma_f32<E4M3>(o[4 * J], hi, lo, b0.x, b1.x);
-                        mma_f32<E4M3>(o[4 * J + 1], hi, lo, b0.y, b1.y);
-                        mma_f32<E4M3>(o[4 * J + 2], hi, lo, b0.z, b1.z);
-                        mma_f32<E4M3>(o[4 * J + 3], hi, lo, b0.w, b1.w);
+                        const float c0[4] = {b0.x, b0.y, b0.z, b0.w}, c1[4] = {b1.x, b1.y, b1.z, b1.w};
+                        uint32_t h0[4], l0[4], h1[4], l1[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            halves(c0[i], h0[i], l0[i]);
+                            halves(c1[i], h1[i], l1[i]);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mma_tf32(o[4 * J + i], lo, h0[i], h1[i]);
+                        if (!E4M3) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) mma_tf32(o[4 * J + i], hi, l0[i], l1[i]);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mma_tf32(o[4 * J + i], hi, h0[i], h1[i]);
                     }
                 }
             } else {
