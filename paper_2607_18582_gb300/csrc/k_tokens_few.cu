@@ -35,7 +35,7 @@ struct Few {
     static constexpr int kElt = E4M3 ? 1 : (int)sizeof(T);
     static constexpr int kRow = DP * kElt;                                   // bytes of a staged row
     static constexpr int kLeast = kF32 ? 8 : 16;
-    static constexpr int kBytes = kF32 && E4M3 && DP > 128 ? 2048 : 4096;     // of a step's K or V rows
+    static constexpr int kBytes = kF32 && E4M3 && DP > 64 ? 2048 : 4096;     // of a step's K or V rows
     static constexpr int kStages = kRow < 128 ? 4 : 2;
     static constexpr int WK = (kBytes / kRow < kLeast) ? kLeast : (kBytes / kRow > 32 ? 32 : kBytes / kRow);   // cells of a warp's step
     static constexpr int kTile = kWarps * WK;
@@ -51,7 +51,7 @@ struct Few {
     static constexpr int kFactors = E4M3 ? kWarps * 3 * 32 * 4 : 0;          // a step's scales, as factors
     static constexpr int kSmem = (kRing > kJoin ? kRing : kJoin) + kQ + kFactors;
     static_assert(kSmem >= kMostParts * kFewRows * 4, "a unit's weights of parts do not fit");
-    static constexpr int kBlocks = kSmem > 110 * 1024 ? 1 : DP > 128 || kSmem > 74 * 1024 || (kF32 && E4M3 && DP > 64) ? 2 : 3;   // per SM
+    static constexpr int kBlocks = kSmem > 110 * 1024 ? 1 : DP > 128 || kSmem > 74 * 1024 || (kF32 && DP > 64) ? 2 : 3;   // per SM
 };
 
 struct FewParams {
@@ -123,8 +123,8 @@ __device__ __forceinline__ uint32_t lds4(uint32_t a)
     return v;
 }
 
-// TF32 halves: the high one rounded to the nearest, the low one the exact remainder (the product reads its
-// upper bits).
+// TF32 halves: the high one rounded to the nearest, the low one the exact remainder, of which the product
+// reads the upper 19 bits (a NaN stays one in the remainder, whatever becomes of its bits in the high half).
 __device__ __forceinline__ void halves(float x, uint32_t &hi, uint32_t &lo)
 {
     hi = (__float_as_uint(x) + 0x1000u) & 0xFFFFE000u;
@@ -594,43 +594,59 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
             }
             const uint32_t vst = st + WK * F::kRow;
             if constexpr (F::kF32) {
+                uint32_t hi[NT][4], lo[NT][4];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {                 // eight cells: the step's cells 2t and 2t + 1 are this lane's
-                    float *x = s[n];
-                    uint32_t hi[4], lo[4];
-                    halves(x[0], hi[0], lo[0]);
-                    halves(x[2], hi[1], lo[1]);
-                    halves(x[1], hi[2], lo[2]);
-                    halves(x[3], hi[3], lo[3]);
+                    halves(s[n][0], hi[n][0], lo[n][0]);
+                    halves(s[n][2], hi[n][1], lo[n][1]);
+                    halves(s[n][1], hi[n][2], lo[n][2]);
+                    halves(s[n][3], hi[n][3], lo[n][3]);
+                }
+                // 32 values of a row at a time: lane group g has 4g .. 4g + 3
+                constexpr int VW = 4;
 #pragma unroll
-                    for (int J = 0; J < DP / 32; ++J) {        // 32 values of a row: lane group g has 4g .. 4g + 3
-                        float4 b0, b1;
-                        if (E4M3) {
-                            const uint32_t c0 = lds4(vst + swz<F::kRow, false>(n * 8 + 2 * t, (2 * J + g / 4) * 16, true) + g % 4 * 4);
-                            const uint32_t c1 = lds4(vst + swz<F::kRow, false>(n * 8 + 2 * t + 1, (2 * J + g / 4) * 16, true) + g % 4 * 4);
-                            const float2 u0 = e4m3_values((uint16_t)c0), v0 = e4m3_values((uint16_t)(c0 >> 16));
-                            const float2 u1 = e4m3_values((uint16_t)c1), v1 = e4m3_values((uint16_t)(c1 >> 16));
-                            b0 = make_float4(u0.x, u0.y, v0.x, v0.y);
-                            b1 = make_float4(u1.x, u1.y, v1.x, v1.y);
-                        } else {
-                            b0 = lds16(vst + swz<F::kRow, true>(n * 8 + 2 * t, (8 * J + g) * 16, true));
-                            b1 = lds16(vst + swz<F::kRow, true>(n * 8 + 2 * t + 1, (8 * J + g) * 16, true));
+                for (int J = 0; J < DP / 8; J += VW) {
+                    // A step's products in accumulators of their own, added to the sums by rounded fp32
+                    // additions: the tensor cores' truncate, and a long axis has thousands of them
+                    // (of 256 values: straight into the sums, registers are short)
+                    constexpr bool kStraight = DP > 128;
+                    float d[VW][4] = {};
+                    auto sum = [&](int i) -> float * { return kStraight ? o[J + i] : d[i]; };
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        float c[2][4];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int row = n * 8 + 2 * t + e;
+                            if (E4M3) {
+                                const uint32_t u = lds4(vst + swz<F::kRow, false>(row, (J / 4 * 2 + g / 4) * 16, true) + g % 4 * 4);
+                                const float2 x = e4m3_values((uint16_t)u), y = e4m3_values((uint16_t)(u >> 16));
+                                c[e][0] = x.x; c[e][1] = x.y; c[e][2] = y.x; c[e][3] = y.y;
+                            } else {
+                                const float4 x = lds16(vst + swz<F::kRow, true>(row, (J / 4 * 8 + g) * 16, true));
+                                c[e][0] = x.x; c[e][1] = x.y; c[e][2] = x.z; c[e][3] = x.w;
+                            }
                         }
-                        const float c0[4] = {b0.x, b0.y, b0.z, b0.w}, c1[4] = {b1.x, b1.y, b1.z, b1.w};
-                        uint32_t h0[4], l0[4], h1[4], l1[4];
+                        uint32_t h0[VW], l0[VW], h1[VW], l1[VW];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            halves(c0[i], h0[i], l0[i]);
-                            halves(c1[i], h1[i], l1[i]);
+                        for (int i = 0; i < VW; ++i) {
+                            halves(c[0][i], h0[i], l0[i]);
+                            halves(c[1][i], h1[i], l1[i]);
                         }
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) mma_tf32(o[4 * J + i], lo, h0[i], h1[i]);
+                        for (int i = 0; i < VW; ++i) mma_tf32(sum(i), lo[n], h0[i], h1[i]);
                         if (!E4M3) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) mma_tf32(o[4 * J + i], hi, l0[i], l1[i]);
+                            for (int i = 0; i < VW; ++i) mma_tf32(sum(i), hi[n], l0[i], l1[i]);
                         }
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) mma_tf32(o[4 * J + i], hi, h0[i], h1[i]);
+                        for (int i = 0; i < VW; ++i) mma_tf32(sum(i), hi[n], h0[i], h1[i]);
+                    }
+                    if (!kStraight) {
+#pragma unroll
+                        for (int i = 0; i < VW; ++i)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) o[J + i][k] += d[i][k];
                     }
                 }
             } else {

@@ -354,6 +354,9 @@ def test_masked_cells_never_reach_an_output(M, ctx, new, past, window, sinks, dt
             t.pools[2 + w][page, 0, slot] = 255
         else:
             t.pools[w][page, 0, slot] = val
+            if dtype == "f32":                     # (the bits that the GPU's own arithmetic gives)
+                t.pools[w].view(torch.int32)[page, 0, slot, ::2] = 0x7FFFFFFF
+                t.pools[w].view(torch.int32)[page, 0, slot, 1::2] = -1
         out, _ = t.check()
         bad = torch.isnan(out).any(-1)
         row0 = sum(new[:b])
