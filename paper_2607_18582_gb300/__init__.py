@@ -3,7 +3,7 @@
 The method: Ghanbari, Greenman, Tavakkol, Ahmed, "Provably Lossless Acceleration of
 DNN Mutation Testing via Memoization" (PACMSE/ISSTA 2026), Algorithm 1.
 
-  mure            ctypes binding of the CUDA library (include/mure.h)
+  mure            ctypes binding of the CUDA library (include/mure.h): mutation testing, token caches
   workloads       seeded synthetic networks, inputs and mutant tables
   build           nvcc build of the library
 """

@@ -45,8 +45,12 @@ struct mure_tokens_plan {
 
 namespace {
 
-// E4M3 rows of a sequence and head up to which the kernel for few rows takes them.
-constexpr int kFewRowsWide = 64;
+// Rows of a sequence and cached head up to which the kernel for few rows takes them; it reads the cells
+// again for every 16.  16 sequences of 4,000 cells, 8 heads (few rows / chunk, us): 128 values, 32 rows
+// 70 / 58; 64 values, 32 rows 45 / 50, 64 rows 70 / 51; codes, whose pages a chunk's kernel wants
+// widened first, 128 values, 64 rows 126 / 137, 128 rows 225 / 138, 64 values 90 / 92 and 164 / 93.
+int few_rows_up_to(bool codes, int d) { return codes ? 64 : d <= 64 ? 32 : 16; }
+
 constexpr int64_t kMostPos = int64_t(1) << 30, kMostStride = int64_t(1) << 40, kMostUnits = int64_t(1) << 24;
 
 int elt_bytes(int dtype) { return dtype == MURE_F32 ? 4 : 2; }
@@ -157,7 +161,9 @@ Shares pack(const std::vector<Unit> &units, const Shape &sh)
     std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return cost(units[a]) > cost(units[b]); });
     double total = 0;
     for (const Unit &u : units) total += cost(u);
-    const int blocks = (int)std::min<double>(sh.blocks, std::max(1.0, std::ceil(total / (kStart + 1))));
+    int64_t most = 0;                                               // parts of the least size
+    for (const Unit &u : units) most += std::max(1, u.tiles / sh.least);
+    const int blocks = (int)std::min<int64_t>(sh.blocks, most);
     const double share = total / blocks * 1.02;
     using Load = std::pair<double, int>;                            // work so far, block
     std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
@@ -306,7 +312,7 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
         const TokSeq &q = seq[s];
         const int64_t rows = (int64_t)q.n_new * group;
         FAILIF(rows > kMostPos, c, MURE_ERR_UNSUPPORTED, "sequence %d: more than 2^30 rows", s);
-        const bool as_chunk = d.dtype != MURE_F32 && d.head_dim <= kChunkDim && rows > (wide ? kFewRowsWide : kFewRows);
+        const bool as_chunk = d.dtype != MURE_F32 && d.head_dim <= kChunkDim && rows > few_rows_up_to(wide, d.head_dim);
         const Shape &sh = as_chunk ? chunk_shape : few_shape;
         FAILIF((int64_t)(few.size() + chunk.size()) + (rows + sh.rows - 1) / sh.rows * d.n_kv_heads > kMostUnits, c,
                MURE_ERR_UNSUPPORTED, "more than 2^24 pieces of work");
