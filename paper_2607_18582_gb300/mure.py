@@ -490,7 +490,6 @@ class Tokens:
         self.n_pages = desc.n_pages
         import torch
         self.torch_dtype, self.torch_device = _torch_dtype(dtype), torch.device("cuda", ctx.device)
-        self.torch_float = torch.float32
         self._keep = keep          # the caller's pools
         ctx._children += 1
 
@@ -586,7 +585,7 @@ def mure_tokens_plan(tokens: Tokens, n_heads: int, new_len, pos, kv_len, page_ta
 
 
 def _raw_stream(device):
-    """torch's current stream as an integer (its own short way where it has one: a call takes a token's time)."""
+    """torch's current stream as an integer (by its own short way where it has one)."""
     global _raw_stream
     import torch
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
@@ -639,13 +638,15 @@ def mure_tokens_read(tokens: Tokens, plan: TokensPlan, new: bool = False, out=No
     """(k, v) [cells][n_kv_heads][head_dim] of all the batch's cells, sequence after sequence (new: of
     its new tokens' cells)."""
     import torch
-    ctx = tokens.ctx
+    ctx, heads, dim = tokens.ctx, tokens.n_kv_heads, tokens.head_dim
     n = plan.n_new if new else plan.n_cells
     if out is None:
-        shape = (n, tokens.n_kv_heads, tokens.head_dim)
-        out = torch.empty((2, *shape), dtype=tokens.torch_dtype, device=tokens.torch_device).unbind(0)
-    kr = _token_rows(out[0], tokens, n, tokens.n_kv_heads, "out[0]")
-    vr = _token_rows(out[1], tokens, n, tokens.n_kv_heads, "out[1]")
+        out = (torch.empty((n, heads, dim), dtype=tokens.torch_dtype, device=tokens.torch_device),
+               torch.empty((n, heads, dim), dtype=tokens.torch_dtype, device=tokens.torch_device))
+        kr, vr = (_TokensRows(x.data_ptr(), heads * dim, dim) for x in out)
+    else:
+        kr = _token_rows(out[0], tokens, n, heads, "out[0]")
+        vr = _token_rows(out[1], tokens, n, heads, "out[1]")
     st = _enter(ctx, out)
     ctx.check(lib().mure_tokens_read(tokens.h, plan.h, 1 if new else 0, kr, vr))
     _leave(st)
@@ -655,12 +656,15 @@ def mure_tokens_read(tokens: Tokens, plan: TokensPlan, new: bool = False, out=No
 def mure_tokens_attend(tokens: Tokens, plan: TokensPlan, q, out=None, lse: bool = False):
     """Attention of the batch's new tokens q [tokens][n_heads][head_dim] over their sequences' cells:
     out (same shape), with lse=True also the logs of the rows' sums, fp32 [tokens][n_heads]."""
+    import torch
     ctx, n = tokens.ctx, plan.n_new
     qr = _token_rows(q, tokens, n, plan.n_heads, "q")
     if out is None:
-        out = q.new_empty((n, plan.n_heads, tokens.head_dim))
-    orow = _token_rows(out, tokens, n, plan.n_heads, "out")
-    ls = q.new_empty((n, plan.n_heads), dtype=tokens.torch_float) if lse else None
+        out = torch.empty((n, plan.n_heads, tokens.head_dim), dtype=tokens.torch_dtype, device=tokens.torch_device)
+        orow = _TokensRows(out.data_ptr(), plan.n_heads * tokens.head_dim, tokens.head_dim)
+    else:
+        orow = _token_rows(out, tokens, n, plan.n_heads, "out")
+    ls = torch.empty((n, plan.n_heads), dtype=torch.float32, device=tokens.torch_device) if lse else None
     st = _enter(ctx, (q, out, ls))
     ctx.check(lib().mure_tokens_attend(tokens.h, plan.h, qr, orow, ls.data_ptr() if lse else None))
     _leave(st)
