@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                     }
                 }
                 __syncwarp();
-#pragma unroll 4
+#pragma unroll 8
                 for (int i = 0; i < 32; i += kPer) {
                     const int64_t off = __shfl_sync(0xffffffffu, out_at, i + lane / kLanes);
                     const uint4 v = ld_shared16(qs + (chunk >> 3) * kPanel + sw128_off((r & ~31) + i + lane / kLanes, chunk & 7));

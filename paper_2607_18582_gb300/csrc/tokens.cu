@@ -85,15 +85,16 @@ TokPool pool_of(const mure_tokens *t)
     return p;
 }
 
-// The tables' memory: at least `bytes`, and some more where it grows (the next steps' do).
+// At least `bytes` of device memory, and up to 16 MiB more where it grows (the next steps' tables do).
 void reserve(mure_ctx *c, void *&mem, size_t &have, size_t bytes)
 {
     if (bytes <= have) return;
     dfree(c, mem);
     mem = nullptr;
     have = 0;
-    mem = dalloc(c, bytes + bytes / 4);
-    have = bytes + bytes / 4;
+    const size_t room = bytes + std::min<size_t>(bytes / 4, 16 << 20);
+    mem = dalloc(c, room);
+    have = room;
 }
 
 // Rows [r0, r0 + rows) of sequence s and head h and the tiles of the cells that they may attend to.
@@ -111,15 +112,15 @@ struct Shape {
     int least;     // tiles of a part, at least
 };
 
-void add_units(std::vector<Unit> &units, const TokSeq &q, int seq, int hk, int group, int window, int sinks, const Shape &sh)
+void add_units(std::vector<Unit> &units, const TokSeq &q, int hk, int group, int window, int sinks, const Shape &sh)
 {
     const int64_t n_rows = (int64_t)q.n_new * group;
     for (int h = 0; h < hk; ++h)
         for (int64_t r0 = 0; r0 < n_rows; r0 += sh.rows) {
             Unit u{};
             TokItem &w = u.item;
-            w.seq = seq; w.h = h; w.r0 = (int)r0; w.rows = (int)std::min<int64_t>(sh.rows, n_rows - r0);
-            w.pos = q.pos; w.row0 = q.row0; w.kv = q.kv; w.n_rows = (int)n_rows; w.table0 = q.table0;
+            w.h = h; w.r0 = (int)r0; w.rows = (int)std::min<int64_t>(sh.rows, n_rows - r0);
+            w.pos = q.pos; w.row0 = q.row0; w.table0 = q.table0;
             const int lo = q.pos + (int)(r0 / group), hi = q.pos + (int)((r0 + w.rows - 1) / group);
             const int end = std::min(q.kv, hi + 1);
             w.b1 = end;
@@ -316,7 +317,7 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
         const Shape &sh = as_chunk ? chunk_shape : few_shape;
         FAILIF((int64_t)(few.size() + chunk.size()) + (rows + sh.rows - 1) / sh.rows * d.n_kv_heads > kMostUnits, c,
                MURE_ERR_UNSUPPORTED, "more than 2^24 pieces of work");
-        add_units(as_chunk ? chunk : few, q, s, d.n_kv_heads, group, b.window, b.sinks, sh);
+        add_units(as_chunk ? chunk : few, q, d.n_kv_heads, group, b.window, b.sinks, sh);
         if (!as_chunk || !wide) continue;
         // the pages that any of its rows reads
         wide_table.resize(table.size(), 0);

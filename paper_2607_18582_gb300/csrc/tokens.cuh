@@ -51,12 +51,13 @@ struct TokRows {
 // that any of them may attend to: first those of a0 .. a1 - 1 (the sinks, where they lie
 // apart), then those of b0 .. b1 - 1, tiles from b0 rounded down to the kernel's alignment.
 struct TokItem {
-    int32_t seq, h, r0, rows;
-    int32_t pos, row0, kv, n_rows;    // the sequence's, and its rows n_new * group
-    int32_t a1, b0, b1, t0;           // (a0 is 0)
-    int32_t t1, part, part0, parts;   // parts > 1: partial result `part` of part0 .. part0 + parts - 1
+    int32_t h, r0, rows;
+    int32_t pos, row0;                // of the sequence's first new token
+    int32_t a1, b0, b1;               // (a0 is 0)
+    int32_t t0, t1;
+    int32_t part, part0, parts;       // parts > 1: partial result `part` of part0 .. part0 + parts - 1
+    int32_t unit;                     // parts > 1: the counter of the rows' finished parts
     int64_t table0;
-    int32_t unit, reserved;           // parts > 1: the counter of the rows' finished parts
 };
 
 // The pieces, block by block, and room for partial results.
