@@ -20,11 +20,11 @@
 // their parts.
 // Every wait is bounded, as in the GEMM kernel.
 //
-// Measured (GB300): 8,192 new tokens over 16,384 cells, 32 heads of 128 bf16 values on 8: 1,155 us, 1,430
-// TFLOP/s (0.76 of cuBLAS's burst, 0.84 of its sustained rate); a 256 x 128 tile takes 2,750 cycles, the
-// tensor pipe is busy for 2,270.  Twelve ragged chunks of 90 to 700 tokens over up to 6,000 cells: 258 us
+// Measured (GB300): 8,192 new tokens over 16,384 cells, 32 heads of 128 bf16 values on 8: 1,155 to 1,184 us,
+// 1,390 to 1,430 TFLOP/s (0.74 to 0.76 of cuBLAS's burst rate); a 256 x 128 tile takes 2,750 cycles, the
+// tensor pipe is busy for 2,270.  Twelve ragged chunks of 90 to 700 tokens over up to 6,000 cells: 260 us
 // (pieces of a few dozen tiles, 12,000 cycles of beginning and end each).  Chunks within a window
-// (64 values): 72 us, bound by the softmax's latency, 1,800 cycles per tile of which 1,024 exponentials.
+// (64 values): 73 us, bound by the softmax's latency, 1,800 cycles per tile of which 1,024 exponentials.
 #include <type_traits>
 
 #include "simt_tile.cuh"

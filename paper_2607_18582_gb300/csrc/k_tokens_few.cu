@@ -18,11 +18,11 @@
 // grows by more than 8 (in powers of two): the sums then need no rescaling in nearly all steps. Powers
 // reach 2^15, which f16 holds, and those down to 2^-21 of the largest keep all its bits.
 //
-// Measured (GB300): two sequences of 100,000 and 131,000 cells, 8 cached heads of 128 bf16 values: 154 us,
-// 6.4 TB/s.  64 sequences of 500 to 12,000 e4m3 cells, the same heads: 174 us, 4.9 TB/s: bound by its
+// Measured (GB300): two sequences of 100,000 and 131,000 cells, 8 cached heads of 128 bf16 values: 153 us,
+// 6.4 TB/s.  64 sequences of 500 to 12,000 e4m3 cells, the same heads: 172 us, 5.0 TB/s: bound by its
 // instructions there (920 per warp and 32 cells, of which 128 widen codes; the issue slots are 47 %
 // busy at three blocks per SM).  96 sequences of f16 cells within a window of 1,024: 26 us, 3.9 TB/s, a unit
-// of ten tiles per block.  fp32 chunks (6 sequences, 12 heads of 64): 137 us, the mma pipe 45 % busy.
+// of ten tiles per block.  fp32 chunks (6 sequences, 12 heads of 64): 128 us, the mma pipe 43 % busy.
 #include <type_traits>
 
 #include "tokens_util.cuh"
