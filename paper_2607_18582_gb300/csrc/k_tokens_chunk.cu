@@ -266,31 +266,36 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
             const int r0 = w.r0 + h * 128, t0 = w.t0, t1 = w.t1, pos = w.pos;
             const int row = r0 + r;
             const bool real = h * 128 + r < rows;
+            const bool have = t1 > t0;                               // (no cells: zeros, no products)
             // Q into the K-major swizzled tile (all products with the last one have finished), the lanes
-            // of a warp along the rows: kLanes 16-byte chunks of one row, the next rows beside it
+            // of a warp along the rows: kLanes 16-byte chunks of one row, the next rows beside it.  Rows without
+            // cells leave Q and its barrier alone: every arrival is then followed by a wait for this piece's first
+            // scores, so that the issuing warp is never more than one phase behind (a parity names no more).
             constexpr int kLanes = DP / 8, kPer = 32 / kLanes;
             const int chunk = lane % kLanes;
-            const int64_t q_at = real ? (w.row0 + row / p.b.group) * p.q.ts + (w.h * p.b.group + row % p.b.group) * p.q.hs : -1;
-            uint4 v[kLanes];
+            if (have) {
+                const int64_t q_at = real ? (w.row0 + row / p.b.group) * p.q.ts + (w.h * p.b.group + row % p.b.group) * p.q.hs : -1;
+                uint4 v[kLanes];
 #pragma unroll
-            for (int i = 0; i < kLanes; ++i) {                       // (all on their way before the first is stored)
-                const int64_t off = __shfl_sync(0xffffffffu, q_at, i * kPer + lane / kLanes);
-                v[i] = make_uint4(0, 0, 0, 0);
-                if (off < 0 || chunk * 8 >= D) continue;
-                const T *q = reinterpret_cast<const T *>(p.q.p) + off + chunk * 8;
-                if (p.q.vec) v[i] = __ldg(reinterpret_cast<const uint4 *>(q));
-                else {
-                    const uint16_t *u = reinterpret_cast<const uint16_t *>(q);
-                    v[i].x = u[0] | (uint32_t)u[1] << 16; v[i].y = u[2] | (uint32_t)u[3] << 16;
-                    v[i].z = u[4] | (uint32_t)u[5] << 16; v[i].w = u[6] | (uint32_t)u[7] << 16;
+                for (int i = 0; i < kLanes; ++i) {                   // (all on their way before the first is stored)
+                    const int64_t off = __shfl_sync(0xffffffffu, q_at, i * kPer + lane / kLanes);
+                    v[i] = make_uint4(0, 0, 0, 0);
+                    if (off < 0 || chunk * 8 >= D) continue;
+                    const T *q = reinterpret_cast<const T *>(p.q.p) + off + chunk * 8;
+                    if (p.q.vec) v[i] = __ldg(reinterpret_cast<const uint4 *>(q));
+                    else {
+                        const uint16_t *u = reinterpret_cast<const uint16_t *>(q);
+                        v[i].x = u[0] | (uint32_t)u[1] << 16; v[i].y = u[2] | (uint32_t)u[3] << 16;
+                        v[i].z = u[4] | (uint32_t)u[5] << 16; v[i].w = u[6] | (uint32_t)u[7] << 16;
+                    }
                 }
-            }
 #pragma unroll
-            for (int i = 0; i < kLanes; ++i)
-                st_shared16(qs + (chunk >> 3) * kPanel + sw128_off((r & ~31) + i * kPer + lane / kLanes, chunk & 7), v[i]);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bar_q[h]));
+                for (int i = 0; i < kLanes; ++i)
+                    st_shared16(qs + (chunk >> 3) * kPanel + sw128_off((r & ~31) + i * kPer + lane / kLanes, chunk & 7), v[i]);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bar_q[h]));
+            }
 
             const int at = pos + row / p.b.group;                                  // the row's position
             const int lo = pos + r0 / p.b.group, hi = pos + (r0 + 127) / p.b.group;
@@ -404,7 +409,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
             const TokItem *after = p.w.items + min(it + 1, it1 - 1);
             const int next_r0 = __ldg(&after->r0) + h * 128 + r, next_rows = __ldg(&after->rows);
             const int next_row0 = __ldg(&after->row0), next_h = __ldg(&after->h);
-            bool have = t1 > t0;                                     // (no cells: zeros)
             if (have) {
                 ok = warp_wait(smem_u32(&bar_o[h]), n_o & 1, ctl);
                 if (!ok) break;
@@ -568,8 +572,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 }
                 continue;
             }
+            if (t1 <= t0) continue;                                  // (rows without cells: no Q, no products)
             ok = warp_wait(smem_u32(&bar_q[h]), n_q++ & 1, ctl);
-            if (!ok || t1 <= t0) continue;                           // (rows without cells: their Q is not read)
+            if (!ok) break;
             ok = warp_wait(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
             if (!ok) break;
             fence_after();
