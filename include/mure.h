@@ -488,9 +488,10 @@ mure_status mure_tokens_read(mure_tokens *tokens, mure_tokens_plan *plan, int32_
  * over the cells each may attend to, sums held in fp32; a token that may attend to none
  * gets zeros.  lse (nullable, device fp32 [tokens][n_heads], dense): log of the sum of
  * exp(scale q k), -inf where there are no cells.  16-bit types: the probabilities are
- * rounded to 16 bits before their product with v; on e4m3 cells a value of magnitude
- * below 2^-20 of the largest that the batch's row meets may lose bits with a small
- * probability.  fp32: products and sums have fp32 accuracy.  Cells that a token may not
+ * rounded to 16 bits before their product with v; on e4m3 cells those below 2^-26 of a
+ * row's largest may be lost, and rows whose sequences' cells have values of v in scales
+ * further than 2^20 apart take more time (they are computed again without the tensor
+ * cores).  fp32: products and sums have fp32 accuracy.  Cells that a token may not
  * attend to never reach its output, whatever they hold; where a cell that it may attend to
  * holds a NaN its output is NaN.  Equal calls give equal bits; the same row in another
  * batch may differ in its last ones (the split of its cells differs).  Errors:

@@ -11,7 +11,8 @@
 //   - e4m3 codes are widened in registers to f16 (one conversion for two, exact), whatever the rows' type:
 //     bf16 rows of q become f16 ones with their largest magnitude brought to 8 .. 16 by a power of two,
 //     exact down to 2^-18 of it.  A cell's scale of K goes to its score and that of V, relative to the
-//     largest met so far, to its probability, in fp32 (scales far below the largest: in part to the values).
+//     largest met so far, to its probability, in fp32 (scales far below the largest: in part to the values; a
+//     spread beyond what f16 then holds sends the rows to the definition).
 // fp32 rows take the same way with TF32 products: every operand is split in two TF32 halves, a = a_hi + a_lo,
 // and a product is a_hi b_hi + a_hi b_lo + a_lo b_hi (codes are TF32 values as they are: two products).
 // What a row's scores are taken relative to lies 7 below their running maximum and moves only when that
@@ -33,6 +34,13 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kAlign = 16;
+
+// 16-bit rows on codes: how far apart, in powers of two, the scales of V that a warp meets may lie.  A probability
+// p <= 1 of its row's largest is held as an f16 number near 2^7 p, in units of 2^-25 at worst.  A cell's scale
+// relative to the largest goes to its value down to 2^-14, exactly, and below that to the probability, which then is
+// good to 2^-32 / 2^-6 = 2^-26 of the row's largest at 2^-20.  Past that the rows are done by the definition.
+// (Following the scales costs 64 sequences on codes 172 -> 174 us.)
+constexpr int kSpread = 20;
 
 template <class T, bool E4M3, int DP>
 struct Few {
@@ -414,7 +422,8 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
         if (F::kSharedQ) __syncthreads();
 
         float o[ND][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-        int v_top = 0;                                       // E4M3: the largest scale byte of V so far; o is in its unit
+        int v_top = 0, v_low = 255;                          // E4M3: the largest scale byte of V so far (o is in its unit); the
+                                                             // least of this lane's cells
 #pragma unroll
         for (int i = 0; i < ND; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
 
@@ -442,8 +451,20 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                 const bool in = lane < WK && start + lane >= begin && start + lane < end;
                 const uint32_t yk = in ? *reinterpret_cast<const uint8_t *>(sc + lane) : 0u;
                 const uint32_t yv = in ? *reinterpret_cast<const uint8_t *>(sc + WK + lane) : 0u;
+                // a scale that bears on the others' precision (not a NaN's, nor that of a row of zeros)
+                bool bears = in && yv != 255u;
                 if constexpr (!F::kF32) {
-                    const int most = (int)__reduce_max_sync(0xffffffffu, yv == 255u ? 0u : yv);
+                    if (bears && yv == 0u) {
+                        uint32_t any = 0;
+#pragma unroll
+                        for (int c = 0; c < F::kRow; c += 16) {
+                            const float4 x = lds16(st + WK * F::kRow + swz<F::kRow, false>(lane, c, true));
+                            any |= __float_as_uint(x.x) | __float_as_uint(x.y) | __float_as_uint(x.z) | __float_as_uint(x.w);
+                        }
+                        bears = (any & 0x7F7F7F7Fu) != 0;
+                    }
+                    const int most = (int)__reduce_max_sync(0xffffffffu, bears ? yv : 0u);
+                    if (bears) v_low = min(v_low, (int)yv);
                     if (most > v_top) {
                         const float f = scale_of((uint32_t)max(127 + v_top - most, 0));
 #pragma unroll
@@ -455,7 +476,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                 // probability, to the value)
                 // (a scale below 2^-7 of the largest: 2^-14 .. 1 of it goes to the values instead, so that the
                 // probability keeps its bits in f16)
-                const int low = F::kF32 || !in || yv == 255u || yv == 0u ? 0 : (int)yv - v_top;
+                const int low = F::kF32 || !bears ? 0 : (int)yv - v_top;
                 split = !F::kF32 && __any_sync(0xffffffffu, low < -7);
                 const int to_value = split ? max(low, -14) : 0;
                 mine[0] = scale_of(yk);
@@ -717,6 +738,9 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
         float *join = reinterpret_cast<float *>(smem);
         constexpr int JR = DP + 2;
         const float unit = E4M3 && !F::kF32 ? scale_of((uint32_t)v_top) : 1.f;
+        // Scales of V further apart than kSpread: probabilities of the smallest ones' cells no longer fit f16, and
+        // the largest may be of a cell that a row does not see, or that adds nothing to it.
+        const bool far = E4M3 && !F::kF32 && __any_sync(0xffffffffu, v_top - v_low > kSpread);
         int bad = 0;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -731,11 +755,11 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                 row[d + (F::kF32 ? 4 : E4M3 ? 2 : 1)] = x1;
             }
             if (t == 0) { row[DP] = m[half]; row[DP + 1] = l[half]; }
-            bad |= !fine && g + half * 8 < w.rows;
+            bad |= (far || !fine) && g + half * 8 < w.rows;
         }
         const int chunks = D / 8;
-        // rows whose sums are not numbers are done again by the definition, from the cells they may
-        // attend to alone: a masked cell's NaN or infinity has met a probability of 0
+        // rows whose sums are not numbers, or have lost bits to far larger scales, are done again by the definition,
+        // from the cells they may attend to alone: a masked cell's NaN or infinity has met a probability of 0
         if (__syncthreads_or(bad)) {
             const int j0 = w.t0 < nA ? w.t0 * F::kTile : max(w.b0, b_al + (w.t0 - nA) * F::kTile);
             const int j1 = w.t1 <= nA ? min(w.a1, w.t1 * F::kTile) : min(w.b1, b_al + (w.t1 - nA) * F::kTile);

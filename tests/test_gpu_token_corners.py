@@ -24,3 +24,76 @@ def test_chunks_without_cells_after_short_ones(M, ctx, d, window, pos):  # noqa:
     for _ in range(2):
         out, lse = t.check()
         assert not bool(out[200 * 128:].any()) and bool((lse[200 * 128:] == -math.inf).all())
+
+
+def byte_at(t, b, j):
+    """Index of cell j of sequence b in a pool, all heads."""
+    return int(t.table[b, j // t.page]), slice(None), j % t.page
+
+
+def compare(t, rows, got=None):
+    """The given rows against 64 bits, with no allowance for an output below the tolerance's floor."""
+    out, lse = got if got is not None else t.M.mure_tokens_attend(t.cache, t.plan, t.q, lse=True)
+    t.M.mure_synchronize(t.ctx)
+    ref, tol, rlse, ltol = (x[rows] for x in t.reference())
+    assert bool(((out[rows].double() - ref).abs() <= tol).all()), float(((out[rows].double() - ref).abs() / tol).max())
+    assert bool(((lse[rows].double() - rlse).abs() <= ltol).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("heads,new", [(2, 2), (2, 8), (32, 2), (2, 100)])
+@pytest.mark.parametrize("above", [24, 40, 48, 130])
+def test_loud_values_in_masked_cells(M, ctx, dtype, heads, new, above):  # noqa: F811
+    """A finite value 2^24 to 2^130 above all others in a cell that only a chunk's first token sees (the last
+    cell before its window's end; the next token's own window starts after it), and one in the last token's own
+    cell: the other rows' outputs are as if these cells were empty."""
+    t = Batch(M, ctx, [new], [300], [300 + new], heads, 2, 64, 16, dtype, "e4m3", window=16)
+    t.pools[3].copy_((t.pools[3].int() - 8 * (above > 100)).to(torch.uint8))
+    for j in (300 - 15, 300 + new - 1):
+        at = byte_at(t, 0, j)
+        t.pools[3][at] = int(min(250, int(t.pools[3][byte_at(t, 0, 290)][0]) + above))
+        t.pools[1].view(torch.uint8)[at] = 0x30        # 1/2
+    compare(t, slice(1, new - 1) if new > 2 else slice(0, 0))
+    if new == 2:                                       # (one row between the two: without the later cell)
+        t.pools[3][byte_at(t, 0, 300 + new - 1)] = t.pools[3][byte_at(t, 0, 290)]
+        compare(t, slice(1, 2))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("heads", [2, 16])
+@pytest.mark.parametrize("above", [24, 30, 44, 56])
+def test_loud_values_of_no_probability(M, ctx, dtype, heads, above):  # noqa: F811
+    """A single token's loud cell is visible, but its score lies 250 below the others': it adds nothing, and
+    takes no bits from what the others add.  (The others within f16.)"""
+    t = Batch(M, ctx, [1], [500], [501], heads, 2, 64, 16, dtype, "e4m3", scale=1.0)
+    t.q.fill_(1.0)
+    t.pools[0].view(torch.uint8)[:] = 0
+    t.pools[3].fill_(112 if dtype == "f16" else 100)   # values around 2^-8, 2^-20
+    at = byte_at(t, 0, 123)
+    t.pools[2][at] = 127
+    t.pools[0].view(torch.uint8)[at] = 0xC8            # -4: a score of -256
+    t.pools[3][at] = int(t.pools[3][0, 0, 0]) + above
+    t.check()
+    t.pools[3].clamp_(max=int(t.pools[3][at][0]) - above)
+    t.check()
+
+
+@pytest.mark.parametrize("loud", [10, 25, 60])
+def test_least_scales_beside_larger_ones(M, ctx, loud):  # noqa: F811
+    """Cells of the least scale byte with codes that are not zero, beside a masked cell of a larger scale: bf16 rows
+    keep them.  (Their values, some 2^-119, lie below the tolerance's floor: compared times 2^60.)"""
+    t = Batch(M, ctx, [2], [40], [42], 2, 2, 64, 16, "bf16", "e4m3", window=16)
+    t.pools[3].fill_(0)
+    t.pools[1].view(torch.uint8)[:] |= 0x70            # magnitudes 128 to 448
+    t.pools[1].view(torch.uint8)[(t.pools[1].view(torch.uint8) & 0x7F) == 0x7F] -= 1
+    t.pools[3][byte_at(t, 0, 41)] = loud               # the second token's own
+    out, _ = M.mure_tokens_attend(t.cache, t.plan, t.q, lse=True)
+    M.mure_synchronize(ctx)
+    scaled = out.double() * 2.0 ** 60
+    t.pools[3][t.pools[3] == 0] = 60
+    ref, tol, _, _ = t.reference()
+    assert bool(((scaled - ref).abs() <= tol)[0].all()), float(((scaled - ref).abs() / tol)[0].max())
+    zero = t.pools[1].view(torch.uint8)
+    zero[:] = 0                                        # rows of zeros of any scale are zeros
+    t.pools[3][t.pools[3] == 60] = 0
+    t.check()
