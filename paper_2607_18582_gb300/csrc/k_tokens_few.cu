@@ -39,8 +39,13 @@ constexpr int kAlign = 16;
 // p <= 1 of its row's largest is held as an f16 number near 2^7 p, in units of 2^-25 at worst.  A cell's scale
 // relative to the largest goes to its value down to 2^-14, exactly, and below that to the probability, which then is
 // good to 2^-32 / 2^-6 = 2^-26 of the row's largest at 2^-20.  Past that the rows are done by the definition.
-// (Following the scales costs 64 sequences on codes 172 -> 174 us.)
+// (Following the scales, K's too, costs 64 sequences on codes 172 -> 175 us.)
 constexpr int kSpread = 20;
+
+// The largest scale byte of K on codes: a sum of products of q (up to 2^16) and codes (2^9), 256 of them, times the
+// scale stays below 2^127.  Past it the product overflows before its last factor, which may be small, and a
+// score that overflows to -inf would look like a masked one: such rows, too, are done by the definition.
+constexpr int kMostScaleK = 127 + 127 - (16 + 9 + 8);
 
 template <class T, bool E4M3, int DP>
 struct Few {
@@ -424,6 +429,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
         float o[ND][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
         int v_top = 0, v_low = 255;                          // E4M3: the largest scale byte of V so far (o is in its unit); the
                                                              // least of this lane's cells
+        int k_top = 0;                                       // E4M3: the largest scale byte of K of this lane's cells
 #pragma unroll
         for (int i = 0; i < ND; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
 
@@ -451,6 +457,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                 const bool in = lane < WK && start + lane >= begin && start + lane < end;
                 const uint32_t yk = in ? *reinterpret_cast<const uint8_t *>(sc + lane) : 0u;
                 const uint32_t yv = in ? *reinterpret_cast<const uint8_t *>(sc + WK + lane) : 0u;
+                k_top = max(k_top, (int)yk);                 // (a NaN's byte counts too: rows that see it are done again anyway)
                 // a scale that bears on the others' precision (not a NaN's, nor that of a row of zeros)
                 bool bears = in && yv != 255u;
                 if constexpr (!F::kF32) {
@@ -740,7 +747,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
         const float unit = E4M3 && !F::kF32 ? scale_of((uint32_t)v_top) : 1.f;
         // Scales of V further apart than kSpread: probabilities of the smallest ones' cells no longer fit f16, and
         // the largest may be of a cell that a row does not see, or that adds nothing to it.
-        const bool far = E4M3 && !F::kF32 && __any_sync(0xffffffffu, v_top - v_low > kSpread);
+        const bool far = E4M3 && __any_sync(0xffffffffu, (!F::kF32 && v_top - v_low > kSpread) || k_top > kMostScaleK);
         int bad = 0;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {

@@ -155,6 +155,10 @@ __device__ __forceinline__ void attend_row(const TokPool &pool, const int32_t *t
                                            float &l)
 {
     const int lane = threadIdx.x & 31, D = pool.d;
+    // half of a small scale's power of two goes to q (exactly), so that a sum of products cannot overflow where
+    // the score does not
+    const int half = min((int)(__float_as_uint(scale_log2) >> 23) - 127, 0) / 2;
+    const float before = __uint_as_float((uint32_t)(127 + half) << 23), after = scale_log2 * __uint_as_float((uint32_t)(127 - half) << 23);
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
@@ -177,9 +181,9 @@ __device__ __forceinline__ void attend_row(const TokPool &pool, const int32_t *t
                 cell8<T, E4M3>(pool.k, pool.ks, row, D, c, a);
                 load8(q + c, qvec, b);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s = fmaf(a[i], b[i], s);
+                for (int i = 0; i < 8; ++i) s = fmaf(a[i], b[i] * before, s);
             }
-            s *= scale_log2;
+            s *= after;
         }
         float top = see ? s : -INFINITY;
         bool bad = see && isnan(s);

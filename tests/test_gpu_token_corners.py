@@ -97,3 +97,17 @@ def test_least_scales_beside_larger_ones(M, ctx, loud):  # noqa: F811
     zero[:] = 0                                        # rows of zeros of any scale are zeros
     t.pools[3][t.pools[3] == 60] = 0
     t.check()
+
+
+@pytest.mark.parametrize("dtype,heads", [("bf16", 2), ("bf16", 32), ("f16", 2), ("f32", 2)])
+def test_scores_whose_factors_pass_the_range(M, ctx, dtype, heads):  # noqa: F811
+    """Keys of 2^124 against a query or a scale so small that the scores are a few units, all negative: the product
+    before its last factor is beyond fp32, the score is not."""
+    t = Batch(M, ctx, [1, 3], [200, 90], [201, 93], heads, 2, 64, 16, dtype, "e4m3", scale=2.0 ** -124 if dtype == "f16" else 1.0)
+    t.q.copy_(torch.rand_like(t.q.float()) + 1)
+    if dtype != "f16":
+        t.q.mul_(2.0 ** -64).mul_(2.0 ** -64)          # (in two steps: 2^-128 is subnormal)
+    t.pools[0].view(torch.uint8)[:] = 0xB8             # -1
+    t.pools[0].view(torch.uint8)[:, :, ::3] = 0xB4     # -3/4
+    t.pools[2].fill_(251)
+    t.check()
