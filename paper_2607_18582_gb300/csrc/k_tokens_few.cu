@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                     const char *kb = static_cast<const char *>(p.pool.k) + row * row_bytes;
                     const char *vb = static_cast<const char *>(p.pool.v) + row * row_bytes;
                     if (j0 + 7 < begin || j0 >= end) kb = static_cast<const char *>(p.pool.k), vb = static_cast<const char *>(p.pool.v);
-#pragma unroll
+#pragma unroll(F::kF32 && DP > 128 ? 4 : 16)   // (fp32 of 256 values: 16 addresses at a time would spill)
                     for (int e = 0; e < 8 * REP; e += PER) {
                         const int r = e / REP + r0, byte = (REP > 1 ? lane + e % REP * 32 : lane % CH) * 16;
                         const bool in = j0 + r >= begin && j0 + r < end;
@@ -648,11 +648,9 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
 #pragma unroll
                 for (int J = 0; J < DP / 8; J += VW) {
                     // A step's products in accumulators of their own, added to the sums by rounded fp32
-                    // additions: the tensor cores' truncate, and a long axis has thousands of them
-                    // (of 256 values: straight into the sums, registers are short)
-                    constexpr bool kStraight = DP > 128;
+                    // additions: the tensor cores' truncate, and a long axis has thousands of them (of 256 values: 12 to
+                    // 15 % of the time; sums straight in the accumulators were off by 7e-4 over 300,000 cells)
                     float d[VW][4] = {};
-                    auto sum = [&](int i) -> float * { return kStraight ? o[J + i] : d[i]; };
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         float c[2][4];
@@ -675,20 +673,18 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                             halves(c[1][i], h1[i], l1[i]);
                         }
 #pragma unroll
-                        for (int i = 0; i < VW; ++i) mma_tf32(sum(i), lo[n], h0[i], h1[i]);
+                        for (int i = 0; i < VW; ++i) mma_tf32(d[i], lo[n], h0[i], h1[i]);
                         if (!E4M3) {
 #pragma unroll
-                            for (int i = 0; i < VW; ++i) mma_tf32(sum(i), hi[n], l0[i], l1[i]);
+                            for (int i = 0; i < VW; ++i) mma_tf32(d[i], hi[n], l0[i], l1[i]);
                         }
 #pragma unroll
-                        for (int i = 0; i < VW; ++i) mma_tf32(sum(i), hi[n], h0[i], h1[i]);
+                        for (int i = 0; i < VW; ++i) mma_tf32(d[i], hi[n], h0[i], h1[i]);
                     }
-                    if (!kStraight) {
 #pragma unroll
-                        for (int i = 0; i < VW; ++i)
+                    for (int i = 0; i < VW; ++i)
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) o[J + i][k] += d[i][k];
-                    }
+                        for (int k = 0; k < 4; ++k) o[J + i][k] += d[i][k];
                 }
             } else {
             auto products = [&](auto with_split) {

@@ -111,3 +111,24 @@ def test_scores_whose_factors_pass_the_range(M, ctx, dtype, heads):  # noqa: F81
     t.pools[0].view(torch.uint8)[:, :, ::3] = 0xB4     # -3/4
     t.pools[2].fill_(251)
     t.check()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("form", ["same", "e4m3"])
+def test_fp32_sums_over_long_axes(M, ctx, form, d):  # noqa: F811
+    """fp32 rows over 300,000 cells whose values have one sign and nearly equal probabilities, in pieces of work
+    that are not cut (a sequence per resident block and more, all on the same pages): rounding errors must not
+    add up on one side."""
+    n, many = 300_000, 500
+    t = Batch(M, ctx, [1], [n - 1], [n], 1, 1, d, 64, "f32", form)
+    t.q.mul_(0.01)
+    if form == "same":
+        t.pools[1].abs_().add_(0.5)
+    else:
+        t.pools[1].view(torch.uint8).bitwise_and_(0x7F)
+    ref, tol, rlse, ltol = t.reference()
+    plan = M.mure_tokens_plan(t.cache, 1, [1] * many, [n - 1] * many, [n] * many, np.repeat(t.table, many, 0))
+    out, lse = M.mure_tokens_attend(t.cache, plan, t.q.repeat(many, 1, 1), lse=True)
+    M.mure_synchronize(ctx)
+    assert bool(((out.double() - ref).abs() <= tol).all()), float(((out.double() - ref).abs() / tol).max())
+    assert bool(((lse.double() - rlse).abs() <= ltol).all())
