@@ -206,6 +206,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
     // stages 0 .. kStages / 2 - 1 hold K tiles, the others V tiles
     __shared__ __align__(8) uint64_t bar_full[C::kStages], bar_empty[C::kStages], bar_q[2], bar_s[2], bar_p[2][2], bar_o[2], bar_pv[2], bar_turn[2], bar_drain[2];
     __shared__ uint32_t tmem_sh;
+    __shared__ int again_sh;                  // rows are marked
     __shared__ WaitCtl ctl_sh;
     __shared__ TokItem item_sh[12];           // each warp's piece of work
     __shared__ int page_sh[2][2][16];         // copying warps: the pages of a tile's boxes
@@ -220,6 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (threadIdx.x == 0) {
+        again_sh = 0;
         ctl_sh.abort = 0;
         ctl_sh.limit = p.spin > 0 ? p.spin : kSpin;
         for (int i = 0; i < C::kStages; ++i) {
@@ -492,33 +494,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                     p.lse[(int64_t)token * p.b.n_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945f;
                 }
             }
-            // rows whose sums are not numbers are done again by the definition, from the cells they may
-            // attend to alone: a masked cell's NaN or infinity has met a probability of 0
-            uint32_t again = __ballot_sync(0xffffffffu, bad && real);
-            while (again) {
-                const int b = __ffs(again) - 1;
-                again &= again - 1;
-                const int at_b = __shfl_sync(0xffffffffu, at, b);
-                const int tok_b = __shfl_sync(0xffffffffu, token, b), head_b = __shfl_sync(0xffffffffu, head, b);
-                const T *q = reinterpret_cast<const T *>(p.q.p) + tok_b * p.q.ts + head_b * p.q.hs;
-                const TileCells first = tile_cells(w, t0, p.box), end = tile_cells(w, t1 - 1, p.box);
-                float y[8], mm, ll;
-                attend_row<T, false>(p.pool, p.b.table + w.table0, w.h, q, p.q.vec, at_b,
-                                     first.start, min(end.end, end.start + kCells), p.b.window, p.b.sinks, p.b.scale_log2, y, mm, ll);
-                __syncwarp();
-                if (parts > 1) {
-                    const int64_t pr = (int64_t)part * 256 + h * 128 + (r & ~31) + b;
-                    if (lane * 8 < D) store8(p.w.part + pr * DP + lane * 8, 1, y);
-                    if (lane == 0) { p.ml[pr * 2] = mm; p.ml[pr * 2 + 1] = ll; }
-                } else {
-                    const float f = ll == 0.f ? 0.f : p.unit / ll;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] *= f;
-                    if (lane * 8 < D)
-                        store8(reinterpret_cast<T *>(p.out.p) + tok_b * p.out.ts + head_b * p.out.hs + lane * 8, p.out.vec, y);
-                    if (p.lse && lane == 0)
-                        p.lse[(int64_t)tok_b * p.b.n_heads + head_b] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.693147180559945f;
-                }
+            // rows whose sums are not numbers are marked, to be done again once every role is through
+            const uint32_t again = __ballot_sync(0xffffffffu, bad && real);
+            if (lane == 0) {
+                p.w.again[(int64_t)it * (kChunkRows / 32) + warp] = again;
+                if (again) again_sh = 1;
             }
         }
     } else if (warp == 8 || warp == 11) {
@@ -695,6 +675,34 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
     if (warp == 8) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+    }
+    if (!again_sh || ctl_sh.abort) return;
+
+    // Marked rows by the definition, a warp per row, from the cells they may attend to alone: a masked cell's NaN or
+    // infinity has met a probability of 0.  Here, where no wait is left that their time could run out on.
+    for (int it = it0; it < it1; ++it) {
+        take(it);
+        for (int r = warp; r < w.rows; r += kThreads / 32) {
+            if (!(p.w.again[(int64_t)it * (kChunkRows / 32) + r / 32] >> (r & 31) & 1)) continue;
+            const int row = w.r0 + r, token = w.row0 + row / p.b.group, head = w.h * p.b.group + row % p.b.group;
+            const T *q = reinterpret_cast<const T *>(p.q.p) + token * p.q.ts + head * p.q.hs;
+            const TileCells first = tile_cells(w, w.t0, p.box), end = tile_cells(w, w.t1 - 1, p.box);
+            float y[8], m, l;
+            attend_row<T, false>(p.pool, p.b.table + w.table0, w.h, q, p.q.vec, w.pos + row / p.b.group, first.start,
+                                 min(end.end, end.start + kCells), p.b.window, p.b.sinks, p.b.scale_log2, y, m, l);
+            if (w.parts > 1) {
+                const int64_t pr = (int64_t)w.part * kChunkRows + r;
+                if (lane * 8 < D) store8(p.w.part + pr * DP + lane * 8, 1, y);
+                if (lane == 0) { p.ml[pr * 2] = m; p.ml[pr * 2 + 1] = l; }
+            } else {
+                const float f = l == 0.f ? 0.f : p.unit / l;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] *= f;
+                if (lane * 8 < D)
+                    store8(reinterpret_cast<T *>(p.out.p) + token * p.out.ts + head * p.out.hs + lane * 8, p.out.vec, y);
+                if (p.lse && lane == 0) p.lse[(int64_t)token * p.b.n_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945f;
+            }
+        }
     }
 }
 

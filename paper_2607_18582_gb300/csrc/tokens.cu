@@ -341,7 +341,8 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
     const size_t o_wt = im.add(wide_table), o_wp = im.add(wide_pages);
     const size_t few_part = ((size_t)fs.parts * few_part_floats(d.head_dim) * 4 + 255) / 256 * 256;
     reserve(c, p->mem, p->mem_bytes, im.bytes.size());
-    reserve(c, p->part, p->part_bytes, few_part + (size_t)cs.parts * chunk_part_floats(d.head_dim) * 4);
+    const size_t chunk_part = (size_t)cs.parts * chunk_part_floats(d.head_dim) * 4;
+    reserve(c, p->part, p->part_bytes, few_part + chunk_part + cs.items.size() * (kChunkRows / 8));
     if (!wide_pages.empty()) {
         const int64_t pool = (int64_t)wide_pages.size() * d.n_kv_heads * d.page_size * d.head_dim * 2;
         reserve(c, p->wide, p->wide_bytes, 2 * (size_t)pool);
@@ -367,6 +368,7 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
     p->chunk.w.first = reinterpret_cast<int32_t *>(m + o_chunk1);
     p->chunk.w.blocks = (int)cs.first.size() - 1;
     p->chunk.w.part = reinterpret_cast<float *>(static_cast<char *>(p->part) + few_part);
+    p->chunk.w.again = reinterpret_cast<uint32_t *>(static_cast<char *>(p->part) + few_part + chunk_part);
     p->chunk.ml = p->chunk.w.part + (int64_t)cs.parts * (chunk_part_floats(d.head_dim) - 2 * kChunkRows);
     p->chunk.cut = reinterpret_cast<TokItem *>(m + o_cut);
     p->chunk.n_cut = (int)cs.cut.size();

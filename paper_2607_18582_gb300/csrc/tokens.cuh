@@ -67,6 +67,7 @@ struct TokWork {
     int blocks = 0;
     float *part = nullptr;            // [parts][rows of a piece][padded d + 2]: sums, maximum, sum of powers
     int32_t *count = nullptr;         // [units], zero between calls
+    uint32_t *again = nullptr;        // chunks: [items][kChunkRows / 32] a bit per row that is done again
 };
 
 // Rows of a piece and cells of a tile of the kernel for few rows.

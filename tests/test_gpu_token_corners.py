@@ -132,3 +132,26 @@ def test_fp32_sums_over_long_axes(M, ctx, form, d):  # noqa: F811
     M.mure_synchronize(ctx)
     assert bool(((out.double() - ref).abs() <= tol).all()), float(((out.double() - ref).abs() / tol).max())
     assert bool(((lse.double() - rlse).abs() <= ltol).all())
+
+
+@pytest.mark.parametrize("dtype,form", [("bf16", "same"), ("f16", "e4m3")])
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_done_again_are_no_expired_wait(M, d, dtype, form):  # noqa: F811
+    """NaN in dead cells of every sequence's last page: its rows are computed again by the definition, which takes
+    milliseconds a piece.  With waits limited to 2,000,000 cycles (a millisecond; the kernel's own last some
+    microseconds) the other roles must not give up meanwhile, whatever the pieces before and after."""
+    ctx = M.mure_create(0)
+    new, past = [130, 256, 300, 70] * 50, [1500, 2000, 900, 2200] * 50
+    t = Batch(M, ctx, new, past, [a + b for a, b in zip(new, past)], 2, 2, d, 16, dtype, form)
+    for b, k in enumerate(t.kv):
+        if k % t.page and b % 3:
+            page = int(t.table[b, k // t.page])
+            if form == "e4m3":
+                t.pools[3][page, :, k % t.page:] = 255
+            else:
+                t.pools[1][page, :, k % t.page:] = math.nan
+    M.mure_set_wait_limit(ctx, 2_000_000)
+    for _ in range(2):
+        out, _ = t.check()
+        assert bool(torch.isfinite(out).all())
+    M.mure_set_wait_limit(ctx, 0)
