@@ -207,7 +207,10 @@ __global__ void __launch_bounds__(kThreads) k_tokens_read(CellParams p)
     }
 }
 
-// Whole pages of codes as 16-bit pages, in the order of the list; f16: of half the values.
+// Whole pages of codes as 16-bit pages, in the order of the list.  bf16 holds every code times its scale (but for
+// the last places of subnormals); f16 those of f16 rows that were appended, except the largest, whose code may
+// have been rounded up past 65,504.  Values beyond become NaN: an infinity times a q of the other sign would look
+// like a masked cell's score.
 template <class T>
 __global__ void __launch_bounds__(kThreads) k_tokens_widen(TokPool p, const int32_t *pages, int64_t rows, int lanes, T *k, T *v)
 {
@@ -220,11 +223,10 @@ __global__ void __launch_bounds__(kThreads) k_tokens_widen(TokPool p, const int3
         cell8<T, true>(p.k, p.ks, row, p.d, c, x);
         cell8<T, true>(p.v, p.vs, row, p.d, c, y);
         if constexpr (std::is_same<T, __half>::value) {
-            // halves: a code may have been rounded up past f16's largest value (65,504 to 65,536)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                x[i] *= 0.5f;
-                y[i] *= 0.5f;
+                x[i] = fabsf(x[i]) <= 65504.f ? x[i] : NAN;
+                y[i] = fabsf(y[i]) <= 65504.f ? y[i] : NAN;
             }
         }
         store8(k + r * p.d + c, 1, x);

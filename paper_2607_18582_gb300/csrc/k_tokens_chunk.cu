@@ -62,7 +62,8 @@ struct ChunkParams {
     float *ml;               // partial results' maxima and sums, [parts][256][2]
     int64_t n_pages;
     int box;                 // cells of a copied box
-    float unit;              // what the values are in units of (widened f16 cells: 2)
+    TokPool codes;           // widened cells: where they were widened from,
+    const int32_t *code_table = nullptr;      // and the pages there (null: the cells are what the caches hold)
     int *err;
     long long spin;
     CUtensorMap map_k, map_v;
@@ -425,7 +426,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
             }
             const int parts = w.parts, part = w.part;
             const int token = w.row0 + row / p.b.group, head = w.h * p.b.group + row % p.b.group;
-            const float inv = l == 0.f ? 0.f : p.unit / l;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
             bool bad = !(fabsf(l) < INFINITY) || isnan(m);
             // The rows leave through the warp's part of Q's tile (no product reads it any more), in its
             // swizzle: the lanes then lie along the rows again.  Partial results (fp32) in two passes.
@@ -688,14 +689,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
             const T *q = reinterpret_cast<const T *>(p.q.p) + token * p.q.ts + head * p.q.hs;
             const TileCells first = tile_cells(w, w.t0, p.box), end = tile_cells(w, w.t1 - 1, p.box);
             float y[8], m, l;
-            attend_row<T, false>(p.pool, p.b.table + w.table0, w.h, q, p.q.vec, w.pos + row / p.b.group, first.start,
-                                 min(end.end, end.start + kCells), p.b.window, p.b.sinks, p.b.scale_log2, y, m, l);
+            const int pos = w.pos + row / p.b.group, j0 = first.start, j1 = min(end.end, end.start + kCells);
+            if (p.code_table)
+                attend_row<T, true>(p.codes, p.code_table + w.table0, w.h, q, p.q.vec, pos, j0, j1, p.b.window, p.b.sinks,
+                                    p.b.scale_log2, y, m, l);
+            else
+                attend_row<T, false>(p.pool, p.b.table + w.table0, w.h, q, p.q.vec, pos, j0, j1, p.b.window, p.b.sinks,
+                                     p.b.scale_log2, y, m, l);
             if (w.parts > 1) {
                 const int64_t pr = (int64_t)w.part * kChunkRows + r;
                 if (lane * 8 < D) store8(p.w.part + pr * DP + lane * 8, 1, y);
                 if (lane == 0) { p.ml[pr * 2] = m; p.ml[pr * 2 + 1] = l; }
             } else {
-                const float f = l == 0.f ? 0.f : p.unit / l;
+                const float f = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) y[i] *= f;
                 if (lane * 8 < D)
@@ -708,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
 
 // Joins the parts of rows that were cut: a warp per row, the parts in their order.
 template <class T>
-__global__ void __launch_bounds__(256) k_tokens_join(const TokItem *cut, int DP, TokBatch b, int D, float unit, TokRows out, float *lse,
+__global__ void __launch_bounds__(256) k_tokens_join(const TokItem *cut, int DP, TokBatch b, int D, TokRows out, float *lse,
                                                      const float *part, const float *ml)
 {
     const TokItem &w = cut[blockIdx.x];
@@ -730,7 +736,7 @@ __global__ void __launch_bounds__(256) k_tokens_join(const TokItem *cut, int DP,
         for (int k = 0; k < 4; ++k)
             if (k * 32 + lane < D) x[k] = fmaf(f, part[at * DP + k * 32 + lane], x[k]);
     }
-    const float inv = l == 0.f ? 0.f : unit / l;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     const int row = w.r0 + r, token = w.row0 + row / b.group, head = w.h * b.group + row % b.group;
     T *o = reinterpret_cast<T *>(out.p) + token * out.ts + head * out.hs;
 #pragma unroll
@@ -745,7 +751,7 @@ int go(const ChunkParams &p, const TokChunk &c, cudaStream_t s)
     allow_dynamic_smem_once<k_tokens_chunk<T, DP>>(Chunk<DP>::kSmem);
     k_tokens_chunk<T, DP><<<p.w.blocks, kThreads, Chunk<DP>::kSmem, s>>>(p);
     if (c.n_cut == 0) return 1;
-    k_tokens_join<T><<<dim3(c.n_cut, 32), 256, 0, s>>>(c.cut, DP, p.b, p.pool.d, p.unit, p.out, p.lse, p.w.part, p.ml);
+    k_tokens_join<T><<<dim3(c.n_cut, 32), 256, 0, s>>>(c.cut, DP, p.b, p.pool.d, p.out, p.lse, p.w.part, p.ml);
     return 2;
 }
 
@@ -771,16 +777,18 @@ bool chunk_map(CUtensorMap &map, void *pool, int dtype, int hk, int d, int page_
 }
 
 int launch_tokens_chunk(const TokPool &pool, const TokBatch &b, const TokChunk &c, int dtype, TokRows q, TokRows out, float *lse,
-                        int64_t n_pages, const CUtensorMap &map_k, const CUtensorMap &map_v, bool widened, int *err, int64_t spin,
-                        cudaStream_t s)
+                        int64_t n_pages, const CUtensorMap &map_k, const CUtensorMap &map_v, const TokPool *codes,
+                        const int32_t *code_table, int *err, int64_t spin, cudaStream_t s)
 {
     if (c.w.blocks == 0) return 0;
     ChunkParams p{};
     p.pool = pool; p.b = b; p.w = c.w; p.q = q; p.out = out; p.lse = lse;
     p.ml = c.ml;
     p.n_pages = n_pages;
-    p.unit = widened && dtype == MURE_F16 ? 2.f : 1.f;
-    p.b.scale_log2 *= p.unit;
+    if (codes) {
+        p.codes = *codes;
+        p.code_table = code_table;
+    }
     p.box = chunk_box(1 << pool.page_log2);
     p.err = err;
     p.spin = spin;

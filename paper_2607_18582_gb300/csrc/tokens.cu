@@ -589,7 +589,8 @@ mure_status mure_tokens_attend(mure_tokens *t, mure_tokens_plan *p, const mure_t
         const mure_tokens_desc &d = t->d;
         c->launches += launch_tokens_few(pool_of(t), p->b, p->few, d.dtype, d.form, qr, orow, lse, c->stream);
         if (p->chunk.w.blocks > 0) {
-            TokPool pool = pool_of(t);
+            const TokPool codes = pool_of(t);
+            TokPool pool = codes;
             TokBatch b = p->b;
             const bool wide = d.form == MURE_FORM_E4M3;
             if (wide) {
@@ -597,11 +598,11 @@ mure_status mure_tokens_attend(mure_tokens *t, mure_tokens_plan *p, const mure_t
                 pool.k = p->wide;
                 pool.v = static_cast<char *>(p->wide) + bytes;
                 b.table = p->wide_table;
-                c->launches += launch_tokens_widen(pool_of(t), d.dtype, p->wide_pages, p->n_wide, pool.k, pool.v, c->stream);
+                c->launches += launch_tokens_widen(codes, d.dtype, p->wide_pages, p->n_wide, pool.k, pool.v, c->stream);
             }
             c->launches += launch_tokens_chunk(pool, b, p->chunk, d.dtype, qr, orow, lse, wide ? p->n_wide : d.n_pages,
-                                               wide ? p->map_k : t->map_k, wide ? p->map_v : t->map_v, wide, c->err_dev, c->wait_limit,
-                                               c->stream);
+                                               wide ? p->map_k : t->map_k, wide ? p->map_v : t->map_v, wide ? &codes : nullptr,
+                                               p->b.table, c->err_dev, c->wait_limit, c->stream);
         }
         check_launch(c);
     });

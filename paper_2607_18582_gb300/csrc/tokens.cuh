@@ -94,10 +94,11 @@ int chunk_box(int page_size);         // cells of a box its copies take (and its
 int64_t chunk_part_floats(int d);
 bool chunk_map(CUtensorMap &map, void *pool, int dtype, int hk, int d, int page_size, int64_t n_pages);
 int launch_tokens_chunk(const TokPool &pool, const TokBatch &b, const TokChunk &c, int dtype, TokRows q, TokRows out, float *lse,
-                        int64_t n_pages, const CUtensorMap &map_k, const CUtensorMap &map_v, bool widened, int *err, int64_t spin,
-                        cudaStream_t s);
-// E4M3 pages pages[0 .. n_list) as pages 0 .. n_list - 1 of 16-bit pools k and v (f16: of half the values),
-// which launch_tokens_chunk takes as `widened`.
+                        int64_t n_pages, const CUtensorMap &map_k, const CUtensorMap &map_v, const TokPool *codes,
+                        const int32_t *code_table, int *err, int64_t spin, cudaStream_t s);
+// E4M3 pages pages[0 .. n_list) as pages 0 .. n_list - 1 of 16-bit pools k and v, which launch_tokens_chunk takes
+// together with where they come from (`codes`, `code_table`).  A value that f16 does not reach becomes a NaN:
+// the rows that meet it are done from the codes.
 int launch_tokens_widen(const TokPool &pool, int dtype, const int32_t *pages, int64_t n_list, void *k, void *v, cudaStream_t s);
 
 int launch_tokens_append(const TokPool &pool, const TokBatch &b, int dtype, int form, TokRows k, TokRows v, int64_t tiles,

@@ -155,3 +155,37 @@ def test_rows_done_again_are_no_expired_wait(M, d, dtype, form):  # noqa: F811
         out, _ = t.check()
         assert bool(torch.isfinite(out).all())
     M.mure_set_wait_limit(ctx, 0)
+
+
+@pytest.mark.parametrize("new", [1, 100])
+def test_f16_codes_beyond_f16(M, ctx, new):  # noqa: F811
+    """Pools of the caller's whose codes times scales pass f16's range: keys of 2^24 against small queries, of
+    both signs, and values of 2^18 with small probabilities.  What comes out does not depend on the number of
+    new tokens."""
+    t = Batch(M, ctx, [new], [260], [260 + new], 4, 2, 64, 16, "f16", "e4m3", scale=2.0 ** -20)
+    t.q.mul_(0.01)
+    t.pools[2].fill_(127 + 18)                         # K around 2^24
+    lowest = t.pools[0].view(torch.uint8)
+    lowest[:] &= 0xBF                                  # (magnitudes below 2)
+    page, heads, slot = byte_at(t, 0, 57)
+    t.q[..., 0] = 4.0
+    lowest[..., 0] = 0x38                              # +1
+    lowest[page, heads, slot, 0] = 0xD0                # -8: a score lower by 9
+    t.pools[3].fill_(112)
+    t.pools[3][page, heads, slot] = 127 + 8
+    out, _ = t.check()
+    assert bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("new", [1, 20, 200])
+def test_f16_subnormals_come_back(M, ctx, new):  # noqa: F811
+    """Each token attends to its own cell alone (a window of one): the output is the cell, bit for bit, down to
+    f16's smallest numbers."""
+    t = Batch(M, ctx, [new], [33], [33 + new], 8, 2, 64, 16, "f16", "e4m3", window=1)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    v = torch.randint(-16, 17, (new, 2, 64), generator=g, device="cuda").half() * 2.0 ** -24
+    M.mure_tokens_append(t.cache, t.plan, t.k, v)
+    out = M.mure_tokens_attend(t.cache, t.plan, t.q)
+    _, got = M.mure_tokens_read(t.cache, t.plan, new=True)
+    M.mure_synchronize(ctx)
+    assert torch.equal(got, v) and torch.equal(out, v.repeat_interleave(4, 1))
