@@ -453,7 +453,9 @@ mure_status mure_tokens_buffers(const mure_tokens *tokens, mure_tokens_desc *out
  * every cache of the context with `tokens`' geometry (heads, head_dim, page_size, dtype,
  * form, n_pages), not that one alone.  mure_tokens_plan_set gives an existing plan a new
  * batch (the next step of the same sequences, say) and keeps its device memory; when it
- * fails the plan is left without a batch.  A plan holds its tables, room for partial sums
+ * fails the plan is left without a batch.  A batch whose tables take more than 1 MiB (some
+ * 200,000 pages) is copied once the stream's earlier work is done: the call then waits for
+ * it.  A plan holds its tables, room for partial sums
  * and, for chunks on e4m3 cells, the pages they read widened to 16 bits (each page once
  * however many sequences share it).  Errors: INVALID_ARG (a NULL array, a negative
  * length, positions past 2^30, a page id out of range, head counts that do not divide,

@@ -189,3 +189,26 @@ def test_f16_subnormals_come_back(M, ctx, new):  # noqa: F811
     _, got = M.mure_tokens_read(t.cache, t.plan, new=True)
     M.mure_synchronize(ctx)
     assert torch.equal(got, v) and torch.equal(out, v.repeat_interleave(4, 1))
+
+
+def test_plans_do_not_wait_for_the_stream(M):  # noqa: F811
+    """A new batch of some 600 KB of tables in an existing plan, behind tens of milliseconds of work on the context's
+    stream: the call returns while that work still runs, and its tables are right."""
+    s = torch.cuda.Stream()
+    own = M.mure_create(0, stream=s)
+    n, kv, page = 100, 12000, 8
+    t = Batch(M, own, [1] * n, [kv - 1] * n, [kv] * n, 2, 1, 64, page, "bf16", "same")
+    x = torch.randn(8192, 8192, device="cuda", dtype=torch.bfloat16)
+    t.make_plan(t.plan)
+    done = torch.cuda.Event()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        x @ x
+        for _ in range(60):
+            x @ x
+        done.record()
+        t.make_plan(t.plan)
+        waited = done.query()
+        out, lse = M.mure_tokens_attend(t.cache, t.plan, t.q, lse=True)
+    assert not waited
+    t.check((out, lse))
