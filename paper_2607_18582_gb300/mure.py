@@ -553,12 +553,33 @@ def mure_tokens_create(ctx: Context, n_kv_heads: int, head_dim: int, page_size: 
     return Tokens(ctx, out.value, d, dtype, form, buffers)
 
 
+def _int32(a, name, past=None):
+    """Whole numbers as a dense int32 array.  past: what stands for one that does not fit (None: refused)."""
+    a = np.asarray(a)
+    if a.dtype == np.int32 or a.size == 0:
+        return np.ascontiguousarray(a, np.int32)
+    if a.dtype.kind not in "biuf":
+        raise ValueError(f"{name}: whole numbers are wanted")
+    fits = (a >= -2 ** 31) & (a < 2 ** 31) if a.dtype.kind == "f" else None
+    if fits is None or fits.all():
+        b = np.ascontiguousarray(a).astype(np.int32)
+        same = b == a
+        if same.all():
+            return b
+    if a.dtype.kind == "f" or past is None:
+        raise ValueError(f"{name}: whole numbers of 32 bits are wanted")
+    b[~same] = past
+    return b
+
+
 def _tokens_batch(n_heads, new_len, pos, kv_len, page_table, window, sinks, scale):
-    new_len, pos, kv_len = (np.ascontiguousarray(a, np.int32).reshape(-1) for a in (new_len, pos, kv_len))
+    new_len, pos, kv_len = (_int32(a, name).reshape(-1)
+                            for a, name in ((new_len, "new_len"), (pos, "pos"), (kv_len, "kv_len")))
     n = len(new_len)
     if len(pos) != n or len(kv_len) != n:
         raise ValueError("new_len, pos and kv_len have different lengths")
-    table = np.ascontiguousarray(page_table, np.int32)
+    # (an id that does not fit is none; the library refuses it where a sequence's cells need it)
+    table = _int32(page_table, "page_table", past=-1)
     if table.ndim != 2 or table.shape[0] < n:
         raise ValueError("page_table: a row of page ids for every sequence")
     b = _TokensBatch(n, int(n_heads), _ptr(new_len), _ptr(pos), _ptr(kv_len), _ptr(table), table.shape[1], int(window),
