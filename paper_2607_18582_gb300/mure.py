@@ -532,8 +532,8 @@ def mure_tokens_create(ctx: Context, n_kv_heads: int, head_dim: int, page_size: 
     """A cache of n_pages pages.  buffers: the caller's pools as CUDA tensors, (k, v) or with form
     "e4m3" (k, v, k_scale, v_scale), [n_pages][n_kv_heads][page_size][head_dim] (scales: without the
     last dimension); by default the library allocates them, filled with zeros."""
-    d = _TokensDesc(int(n_kv_heads), int(head_dim), int(page_size), TOKEN_DTYPES[dtype], TOKEN_FORMS[form], 0,
-                    int(n_pages))
+    d = _TokensDesc(_whole(n_kv_heads, "n_kv_heads"), _whole(head_dim, "head_dim"), _whole(page_size, "page_size"),
+                    TOKEN_DTYPES[dtype], TOKEN_FORMS[form], 0, _whole(n_pages, "n_pages", 64))
     if buffers is not None:
         import torch
         if len(buffers) != (4 if form == "e4m3" else 2):
@@ -551,6 +551,14 @@ def mure_tokens_create(ctx: Context, n_kv_heads: int, head_dim: int, page_size: 
     out = C.c_void_p()
     ctx.check(lib().mure_tokens_create(ctx.h, C.byref(d), C.byref(out)))
     return Tokens(ctx, out.value, d, dtype, form, buffers)
+
+
+def _whole(x, name, bits=32):
+    """A whole number that an integer of so many bits holds."""
+    x = int(x)
+    if not -1 << (bits - 1) <= x < 1 << (bits - 1):
+        raise ValueError(f"{name}: {x} does not fit {bits} bits")
+    return x
 
 
 def _int32(a, name, past=None):
@@ -582,8 +590,8 @@ def _tokens_batch(n_heads, new_len, pos, kv_len, page_table, window, sinks, scal
     table = _int32(page_table, "page_table", past=-1)
     if table.ndim != 2 or table.shape[0] < n:
         raise ValueError("page_table: a row of page ids for every sequence")
-    b = _TokensBatch(n, int(n_heads), _ptr(new_len), _ptr(pos), _ptr(kv_len), _ptr(table), table.shape[1], int(window),
-                     int(sinks), float(scale or 0.0), 0)
+    b = _TokensBatch(n, _whole(n_heads, "n_heads"), _ptr(new_len), _ptr(pos), _ptr(kv_len), _ptr(table), table.shape[1],
+                     _whole(window, "window"), _whole(sinks, "sinks"), float(scale or 0.0), 0)
     return b, (new_len, pos, kv_len, table)
 
 

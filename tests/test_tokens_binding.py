@@ -46,3 +46,18 @@ def test_shapes():
     for bad in (dict(new=(1, 2)), dict(kv=()), dict(table=(0, 1)), dict(table=np.zeros((0, 4), np.int32))):
         with pytest.raises(ValueError):
             batch(**bad)
+
+
+@pytest.mark.parametrize("bad", [dict(n_heads=2 ** 32 + 4), dict(window=2 ** 32 + 16), dict(window=2 ** 31), dict(sinks=-2 ** 32 + 4)])
+def test_single_numbers_do_not_wrap(bad):
+    args = dict(n_heads=4, new_len=(2,), pos=(14,), kv_len=(16,), page_table=((0,),), window=0, sinks=0, scale=0.0)
+    with pytest.raises(ValueError):
+        mure._tokens_batch(**{**args, **bad})
+
+
+@pytest.mark.parametrize("bad", [dict(n_kv_heads=2 ** 32 + 2), dict(head_dim=2 ** 32 + 64), dict(page_size=2 ** 32 + 16),
+                                 dict(n_pages=2 ** 64 + 4)])
+def test_a_cache_s_sizes_do_not_wrap(bad):
+    """(They are looked at before the context is.)"""
+    with pytest.raises(ValueError):
+        mure.mure_tokens_create(None, **{**dict(n_kv_heads=2, head_dim=64, page_size=16, n_pages=4), **bad})
