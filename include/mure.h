@@ -434,7 +434,7 @@ typedef struct {
                                            sequence's last cell are not read */
     int64_t table_stride;
     int32_t window, sinks;              /* 0 0: causal over all cells */
-    float scale;                        /* factor of the scores; 0: head_dim^-1/2 */
+    float scale;                        /* factor of the scores, up to 2.3e38; 0: head_dim^-1/2 */
     int32_t reserved;                   /* 0 */
 } mure_tokens_batch;
 

@@ -258,7 +258,9 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
     FAILIF(b.n_seqs > 0 && (!b.new_len || !b.pos || !b.kv_len), c, MURE_ERR_INVALID_ARG, "NULL lengths");
     FAILIF(b.window < 0 || b.sinks < 0, c, MURE_ERR_INVALID_ARG, "negative window or sinks");
     FAILIF(b.window == 0 && b.sinks != 0, c, MURE_ERR_INVALID_ARG, "sinks without a window");
-    FAILIF(!(b.scale >= 0.f) || std::isinf(b.scale), c, MURE_ERR_INVALID_ARG, "scale must be finite and not negative");
+    // (of powers of two, as the kernels take it: its product with log2 e, too, has to be a number)
+    const float scale_log2 = (float)((b.scale > 0.f ? (double)b.scale : 1.0 / std::sqrt((double)d.head_dim)) * 1.4426950408889634);
+    FAILIF(!(b.scale >= 0.f) || !std::isfinite(scale_log2), c, MURE_ERR_INVALID_ARG, "scale must be in 0..2.3e38");
 
     const int page_log2 = log2_of(d.page_size), n = b.n_seqs;
     std::vector<TokSeq> seq(n);
@@ -393,7 +395,7 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
     v.group = group;
     v.window = b.window;
     v.sinks = b.sinks;
-    v.scale_log2 = (float)((b.scale > 0.f ? (double)b.scale : 1.0 / std::sqrt((double)d.head_dim)) * 1.4426950408889634);
+    v.scale_log2 = scale_log2;
     p->n_new = n_new;
     p->n_cells = n_cells;
     p->tiles_new = t_new;

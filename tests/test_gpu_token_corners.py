@@ -212,3 +212,18 @@ def test_plans_do_not_wait_for_the_stream(M):  # noqa: F811
         out, lse = M.mure_tokens_attend(t.cache, t.plan, t.q, lse=True)
     assert not waited
     t.check((out, lse))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scales_up_to_the_largest(M, ctx, dtype):  # noqa: F811
+    """A factor of the scores that leaves fp32 once it is in powers of two is refused; up to there scores of 0 are 0."""
+    t = Batch(M, ctx, [1, 100], [50, 20], [51, 120], 4, 2, 64, 16, dtype, "same")
+    t.q.zero_()
+    t.scale = 2e38
+    t.make_plan(t.plan)
+    t.check()
+    for scale in (2.4e38, 3.4e38):
+        t.scale = scale
+        with pytest.raises(M.MureError) as ei:
+            t.make_plan(t.plan)
+        assert ei.value.status == 1
