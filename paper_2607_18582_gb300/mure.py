@@ -642,7 +642,14 @@ def _leave(streams):
         streams[0].wait_stream(streams[1])
 
 
+def _grad_enabled():
+    import torch
+    return torch.is_grad_enabled()
+
+
 def _token_rows(t, tokens, n, heads, name):
+    if t.requires_grad and _grad_enabled():
+        raise ValueError(f"{name} requires a gradient, and token caches record none: detach it or call under torch.no_grad()")
     if t.dtype is not tokens.torch_dtype or t.device != tokens.torch_device:
         raise ValueError(f"{name}: a {tokens.torch_dtype} tensor on {tokens.torch_device} is wanted")
     s = t.stride()
@@ -684,7 +691,8 @@ def mure_tokens_read(tokens: Tokens, plan: TokensPlan, new: bool = False, out=No
 
 def mure_tokens_attend(tokens: Tokens, plan: TokensPlan, q, out=None, lse: bool = False):
     """Attention of the batch's new tokens q [tokens][n_heads][head_dim] over their sequences' cells:
-    out (same shape), with lse=True also the logs of the rows' sums, fp32 [tokens][n_heads]."""
+    out (same shape), with lse=True also the logs of the rows' sums, fp32 [tokens][n_heads].  Token caches
+    record no gradients: rows that require one are refused unless under torch.no_grad()."""
     import torch
     ctx, n = tokens.ctx, plan.n_new
     qr = _token_rows(q, tokens, n, plan.n_heads, "q")

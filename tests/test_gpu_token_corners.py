@@ -227,3 +227,21 @@ def test_scales_up_to_the_largest(M, ctx, dtype):  # noqa: F811
         with pytest.raises(M.MureError) as ei:
             t.make_plan(t.plan)
         assert ei.value.status == 1
+
+
+def test_rows_that_require_gradients_are_refused(M, ctx):  # noqa: F811
+    """No call records a gradient; none drops one silently."""
+    t = Batch(M, ctx, [3], [14], [17], 4, 2, 64, 16, "bf16", "same")
+    q, k = t.q.clone().requires_grad_(), t.k.clone().requires_grad_()
+    before = [p.clone() for p in t.pools]
+    calls = [lambda: M.mure_tokens_attend(t.cache, t.plan, q), lambda: M.mure_tokens_append(t.cache, t.plan, k, t.v),
+             lambda: M.mure_tokens_append(t.cache, t.plan, t.k, k), lambda: M.mure_tokens_read(t.cache, t.plan, new=True, out=(k, t.v))]
+    for call in calls:
+        with pytest.raises(ValueError):
+            call()
+    M.mure_synchronize(ctx)
+    assert all(torch.equal(a, b) for a, b in zip(before, t.pools))
+    want = M.mure_tokens_attend(t.cache, t.plan, t.q)
+    assert torch.equal(M.mure_tokens_attend(t.cache, t.plan, q.detach()), want)
+    with torch.no_grad():
+        assert torch.equal(M.mure_tokens_attend(t.cache, t.plan, q), want)
