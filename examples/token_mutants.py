@@ -5,8 +5,8 @@ projection, added to the block's input), and a classifier on the last token.  Th
 every input and leaves each layer's keys and values in a token cache.  Mutants of the last
 block's queries or output projection and of the classifier leave those keys and values as they are: a
 mutant's sequence names the original's pages in its table, and only the last token's query attends
-again, all mutants and all inputs in one call.  The same mutants run end to end without any cache, in
-plain torch, for comparison.
+again, all mutants and all inputs in one call (or in several of 65,535 sequences).  The same mutants run
+end to end without any cache, in plain torch, for comparison.
 
     python examples/token_mutants.py            # small, a few seconds on a GB300
     python examples/token_mutants.py --inputs 200 --mutants 100 --form e4m3
@@ -23,6 +23,8 @@ if ROOT not in sys.path:
     sys.path.insert(0, ROOT)
 
 from paper_2607_18582_gb300 import mure  # noqa: E402
+
+SEQS = 65_535        # sequences of a plan, at most
 
 
 class Net:
@@ -76,16 +78,22 @@ class Memo:
             self.table[b, :n] = np.arange(sum(pages[:b]), sum(pages[:b]) + n)
         self.caches = [mure.mure_tokens_create(ctx, net.kv_heads, net.dim, page, sum(pages), dtype="f32", form=form)
                        for _ in range(net.layers)]
-        zero = [0] * len(lengths)
-        plan = mure.mure_tokens_plan(self.caches[0], net.heads, lengths, zero, lengths, self.table)   # every layer's
         x = net.embed[tokens]                                   # the inputs' tokens, one after the other
+        plans, at = [], 0                                       # every layer's: (rows, plan) of up to SEQS inputs
+        for i in range(0, len(lengths), SEQS):
+            part = lengths[i:i + SEQS]
+            plans.append((slice(at, at + sum(part)), mure.mure_tokens_plan(self.caches[0], net.heads, part, [0] * len(part), part,
+                                                                           self.table[i:i + SEQS])))
+            at += sum(part)
         for i, cache in enumerate(self.caches):
             last = i == net.layers - 1
             if last:
                 self.x = x
             rows = [(x @ w.T).unflatten(1, (-1, net.dim)) for w in (net.q[i], net.k[i], net.v[i])]
-            mure.mure_tokens_append(cache, plan, rows[1], rows[2])
-            a = mure.mure_tokens_attend(cache, plan, rows[0])
+            a = torch.empty_like(rows[0])
+            for r, plan in plans:
+                mure.mure_tokens_append(cache, plan, rows[1][r], rows[2][r])
+                mure.mure_tokens_attend(cache, plan, rows[0][r], out=a[r])
             x = x + a.flatten(1) @ net.o[i].T
         ends = torch.tensor(np.cumsum(lengths) - 1, device="cuda")
         self.x = self.x[ends]                                   # the last block's input at each last token
@@ -96,18 +104,26 @@ class Memo:
         net, n, m = self.net, len(self.lengths), len(mutants_)
         w = [mutated(net, u) for u in mutants_]
         q = torch.stack([self.x @ wq.T for wq, _, _ in w]).reshape(m * n, net.heads, net.dim)
-        lengths = self.lengths * m
-        plan = mure.mure_tokens_plan(self.caches[-1], net.heads, [1] * (m * n), [k - 1 for k in lengths], lengths,
-                                     np.tile(self.table, (m, 1)))
-        a = mure.mure_tokens_attend(self.caches[-1], plan, q).reshape(m, n, -1)
+        a = torch.empty_like(q)
+        lengths = np.asarray(self.lengths, np.int32)
+        for i in range(0, m * n, SEQS):
+            part = np.arange(i, min(i + SEQS, m * n)) % n       # the inputs of these (mutant, input) pairs
+            plan = mure.mure_tokens_plan(self.caches[-1], net.heads, np.ones(len(part), np.int32), lengths[part] - 1, lengths[part],
+                                         self.table[part])
+            mure.mure_tokens_attend(self.caches[-1], plan, q[i:i + SEQS], out=a[i:i + SEQS])
+        a = a.reshape(m, n, -1)
         logits = torch.stack([(self.x + a[i] @ wo.T) @ wc.T for i, (_, wo, wc) in enumerate(w)])
         return logits.argmax(-1) != self.pred, logits
 
     def cells(self):
         """The last block's keys and values as its mutants see them, dense (inputs one after the other)."""
-        plan = mure.mure_tokens_plan(self.caches[-1], self.net.heads, [0] * len(self.lengths), [0] * len(self.lengths),
-                                     self.lengths, self.table)
-        return mure.mure_tokens_read(self.caches[-1], plan)
+        parts = []
+        for i in range(0, len(self.lengths), SEQS):
+            held = self.lengths[i:i + SEQS]
+            zero = [0] * len(held)
+            plan = mure.mure_tokens_plan(self.caches[-1], self.net.heads, zero, zero, held, self.table[i:i + SEQS])
+            parts.append(mure.mure_tokens_read(self.caches[-1], plan))
+        return tuple(torch.cat(x) for x in zip(*parts))
 
 
 def vanilla_logits(net, mutant, tokens, lengths):
