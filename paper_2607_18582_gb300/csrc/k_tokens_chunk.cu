@@ -339,7 +339,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                     for (int i = 0; i < 64; ++i) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(s[i]));
                 }
                 const float mt = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.b.scale_log2;
-                if (C::kApart && t > t0) {                           // the product before has read P and added to O
+                // the product before (the last piece's at first, whose arrival no other wait stands for) has read P and
+                // added to O
+                if (C::kApart && n_s > 1) {
                     ok = warp_wait(smem_u32(&bar_pv[h]), (n_s - 2) & 1, ctl);
                     if (!ok) return;
                     fence_after();
