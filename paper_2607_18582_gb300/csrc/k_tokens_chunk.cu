@@ -15,16 +15,23 @@
 // What a row's scores are taken relative to lies 7 below their running maximum and moves only when that
 // grows by more than 8 (in powers of two; f16 holds powers up to 2^15, and those down to 2^-21 of the
 // largest keep all its bits), so O is hardly ever rescaled; where it is, S's arrival (or, where P lies
-// beside S, a barrier of the product's own) has shown that every earlier product is done.  Whole units of work go to the CTAs, the longest first; the ones that
-// do not fit an even share are cut along the cells and joined by a second kernel in the order of
-// their parts.
+// beside S, a barrier of the product's own) has shown that every earlier product is done.  Whole units of work
+// go to the CTAs, the longest first; the ones that do not fit an even share are cut along the cells and joined
+// by a second kernel in the order of their parts.
+//
+// One pass over the cells with a running maximum and sum is the online softmax of Milakov and Gimelshein (2018),
+// with attention's sums carried along as Rabe and Staats (2021) do.  P is rounded to the cells' type because
+// that is what the product takes (as low halves of its own it would cost a third more tensor work); the row's
+// sum is of the powers before that rounding, and everything else is held in fp32: 1.35 to 1.4 times the error of
+// an output rounded once.  Powers come from the hardware's approximation (2 units in fp32's last place).
 // Every wait is bounded, as in the GEMM kernel.
 //
 // Measured (GB300): 8,192 new tokens over 16,384 cells, 32 heads of 128 bf16 values on 8: 1,155 to 1,184 us,
 // 1,390 to 1,430 TFLOP/s (0.74 to 0.76 of cuBLAS's burst rate); a 256 x 128 tile takes 2,750 cycles, the
-// tensor pipe is busy for 2,270.  Twelve ragged chunks of 90 to 700 tokens over up to 6,000 cells: 260 us
+// tensor pipe is busy for 2,270.  Twelve ragged chunks of 90 to 700 tokens over up to 6,000 cells: 261 us
 // (pieces of a few dozen tiles, 12,000 cycles of beginning and end each).  Chunks within a window
-// (64 values): 73 us, bound by the softmax's latency, 1,800 cycles per tile of which 1,024 exponentials.
+// (64 values): 72 us: the softmax's latency, 1,800 cycles per tile of which 1,024 exponentials, and a beginning
+// and end for every ten tiles, not measured by themselves for 64 values.
 #include <type_traits>
 
 #include "simt_tile.cuh"

@@ -10,7 +10,8 @@
 //     own, and a ring of cp.async stages of its own: no barrier in the loop;
 //   - e4m3 codes are widened in registers to f16 (one conversion for two, exact), whatever the rows' type:
 //     bf16 rows of q become f16 ones with their largest magnitude brought to 8 .. 16 by a power of two,
-//     exact down to 2^-18 of it.  A cell's scale of K goes to its score and that of V, relative to the
+//     exact down to 2^-18 of it and in units of 2^-27 of it below (f16 products take half the conversions of
+//     bf16 ones here, and a score moves by no more than 2^-28 of the largest q times the sum of |k|).  A cell's scale of K goes to its score and that of V, relative to the
 //     largest met so far, to its probability, in fp32 (scales far below the largest: in part to the values; a
 //     spread beyond what f16 then holds sends the rows to the definition).
 // fp32 rows take the same way with TF32 products: every operand is split in two TF32 halves, a = a_hi + a_lo,
@@ -19,11 +20,17 @@
 // grows by more than 8 (in powers of two): the sums then need no rescaling in nearly all steps. Powers
 // reach 2^15, which f16 holds, and those down to 2^-21 of the largest keep all its bits.
 //
-// Measured (GB300): two sequences of 100,000 and 131,000 cells, 8 cached heads of 128 bf16 values: 153 us,
-// 6.4 TB/s.  64 sequences of 500 to 12,000 e4m3 cells, the same heads: 172 us, 5.0 TB/s: bound by its
-// instructions there (920 per warp and 32 cells, of which 128 widen codes; the issue slots are 47 %
-// busy at three blocks per SM).  96 sequences of f16 cells within a window of 1,024: 26 us, 3.9 TB/s, a unit
-// of ten tiles per block.  fp32 chunks (6 sequences, 12 heads of 64): 128 us, the mma pipe 43 % busy.
+// The 16-bit products take P = 2^(s - m) rounded to the cells' type (f16 on codes): that is what the mma takes,
+// and the sums of P beside it keep all their bits.  A second product with P's low half would halve the error
+// (1.2 to 1.4 times that of an output rounded once) for half of the mma work more.  Powers come from the
+// hardware's approximation, 2 units in fp32's last place.
+//
+// Measured (GB300): two sequences of 100,000 and 131,000 cells, 8 cached heads of 128 bf16 values: 155 us,
+// 6.3 TB/s.  64 sequences of 500 to 12,000 e4m3 cells, the same heads: 175 us, 4.9 TB/s: bound by latency there,
+// not by issue: three blocks per SM, 2.7 warps per scheduler, issue in 47 % of the cycles and wait most of all for
+// results of fixed latency (870 instructions per warp and 32 cells, of which 128 widen codes).  96 sequences of f16
+// cells within a window of 1,024: 26 us, 3.8 TB/s, a unit of ten tiles per block.  fp32 chunks (6 sequences,
+// 12 heads of 64): 127 us, the mma pipe 43 % busy.
 #include <type_traits>
 
 #include "tokens_util.cuh"

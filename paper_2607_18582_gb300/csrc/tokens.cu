@@ -49,6 +49,7 @@ namespace {
 // again for every 16.  16 sequences of 4,000 cells, 8 heads (few rows / chunk, us): 128 values, 32 rows
 // 70 / 58; 64 values, 32 rows 45 / 50, 64 rows 70 / 51; codes, whose pages a chunk's kernel wants
 // widened first, 128 values, 64 rows 126 / 137, 128 rows 225 / 138, 64 values 90 / 92 and 164 / 93.
+// (Measured at that one shape.  fp32 rows, and heads of more than 128 values, have no other kernel.)
 int few_rows_up_to(bool codes, int d) { return codes ? 64 : d <= 64 ? 32 : 16; }
 
 constexpr int64_t kMostPos = int64_t(1) << 30, kMostStride = int64_t(1) << 40, kMostUnits = int64_t(1) << 24;
