@@ -496,7 +496,8 @@ mure_status mure_tokens_read(mure_tokens *tokens, mure_tokens_plan *plan, int32_
  * cores), as do rows of MURE_F16 that meet a cell past 65,504; chunks hold the cells of
  * a MURE_F16 cache in multiples of 2^-24, as f16 does.  Single tokens and other short rows
  * of MURE_BF16 queries on e4m3 cells: what lies below 2^-18 of a query row's largest value
- * is held in multiples of 2^-27 of it.  fp32: products and sums have fp32 accuracy.  Cells that a token may not
+ * is held in multiples of 2^-27 of it.  fp32: products and sums have fp32 accuracy
+ * (of magnitudes above 2^-100).  Cells that a token may not
  * attend to never reach its output, whatever they hold; where a cell that it may attend to
  * holds a NaN its output is NaN.  Equal calls give equal bits; the same row in another
  * batch may differ in its last ones (the split of its cells differs).  Errors:

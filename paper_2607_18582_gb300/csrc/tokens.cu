@@ -116,7 +116,8 @@ struct Unit {
     int tiles;
 };
 
-// What a kernel's pieces are made of.
+// What a kernel's pieces are made of.  (`start` and `half` were set on ragged chunks, 12 of 90 to 700 tokens over up to
+// 6,000 cells; they decide how the work is shared out, not what comes out.)
 struct Shape {
     int rows;      // of a piece
     int tile;      // cells
