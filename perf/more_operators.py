@@ -21,6 +21,7 @@ token's parent is one of the `branch` tokens before it (1: a chain, 0: no tree, 
 import math
 import random
 
+import numpy as np
 import torch
 
 own = False
@@ -261,6 +262,7 @@ def prepare(case, seed):
                                                k_weight=s.weights[1].numpy() if case["norm"] else None)
         if case["op"] == "step":
             s.kept = [_path(parents) for parents, _ in s.trees]
+        s.src, s.dst = np.array(s.src, np.int32), np.array(s.dst, np.int32)
         s.mure = mure
         return s
     # whose token each row is, and the cells, as indices for the plain form
