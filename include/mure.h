@@ -465,6 +465,20 @@ mure_status mure_tokens_plan_create(mure_tokens *tokens, const mure_tokens_batch
 mure_status mure_tokens_plan_set(mure_tokens_plan *plan, const mure_tokens_batch *batch);
 void mure_tokens_plan_free(mure_tokens_plan *plan);
 
+/* Trees of new tokens: the continuations of one sequence that share its earlier tokens and diverge (of several
+ * mutants, or drafts of which one path will be kept).  Calls as the two above, with parents (host, a number for each new
+ * token, packed like their rows): the new token that token i of a sequence follows, among that sequence's own and before
+ * i, or -1 for one that follows the earlier cells.  depth(i) is the number of its ancestors among the new tokens, its
+ * position pos[b] + depth(i), and its cell, as for any batch, the one at pos[b] + i.  It attends to itself, to its
+ * ancestors, and to the cells before pos[b], all within kv_len[b] and, where window > 0, by their positions as above.
+ * A chain (parents i - 1) is an ordinary batch, and gives its results.  Every call takes such a plan.  Errors: as above;
+ * INVALID_ARG (NULL parents with new tokens, a parent that is not before its token), UNSUPPORTED (a tree of more than
+ * MURE_TREE_MAX tokens). */
+enum { MURE_TREE_MAX = 1024 };
+mure_status mure_tokens_plan_create_tree(mure_tokens *tokens, const mure_tokens_batch *batch, const int32_t *parents,
+                                         mure_tokens_plan **out);
+mure_status mure_tokens_plan_set_tree(mure_tokens_plan *plan, const mure_tokens_batch *batch, const int32_t *parents);
+
 /* Rows of activations: element (token, head, i) of a batch's packed tokens (the new
  * tokens of sequence 0, then those of sequence 1, ...) is at
  * p[token * token_stride + head * head_stride + i].  Strides count elements, 0..2^40; rows
@@ -504,6 +518,64 @@ mure_status mure_tokens_read(mure_tokens *tokens, mure_tokens_plan *plan, int32_
  * INVALID_ARG (as above), CUDA. */
 mure_status mure_tokens_attend(mure_tokens *tokens, mure_tokens_plan *plan, const mure_tokens_rows *q,
                                const mure_tokens_rows *out, float *lse);
+
+/* Norm and rotation of queries and keys by their tokens' positions.  For a row x of head_dim values:
+ *   y = x w / sqrt(mean(x^2) + eps)                              where a weight w is given, else y = x;
+ *   each pair (a, b) of y's first rot_dim values becomes (a cos u - b sin u, b cos u + a sin u), u = position * freq[i]
+ * with the position of the token along the pair's axis; the values from rot_dim on stay.  All in fp32, rounded once to
+ * the activations' type; angles are exact to 2^-32 of a turn at any 32-bit position. */
+enum { MURE_PAIRS_HALVES = 0, MURE_PAIRS_ADJACENT = 1 };  /* pair i: values i and i + rot_dim / 2, or 2 i and 2 i + 1 */
+
+typedef struct {
+    int32_t head_dim;                   /* a multiple of 8, 8..256 */
+    int32_t rot_dim;                    /* a multiple of 8, 0..head_dim */
+    int32_t pairs;                      /* MURE_PAIRS_* */
+    int32_t n_axes;                     /* axes of positions (time, height, width, ...), 1..8 */
+    const double *freq;                 /* host [rot_dim / 2] radians per position, magnitudes up to 2^20; NULL:
+                                           base^(-2 i / rot_dim) */
+    double base;                        /* > 0, not read where freq is given */
+    const uint8_t *axis;                /* host [rot_dim / 2] each pair's axis; NULL: 0 */
+    const float *q_weight, *k_weight;   /* host [head_dim]; NULL: queries (keys) are not normed */
+    float eps;                          /* 0..1 */
+    int32_t reserved;                   /* 0 */
+} mure_rotary_desc;
+
+typedef struct mure_rotary mure_rotary;
+
+/* Lay a rotation's tables out on the device (it serves every cache of the context whose heads have head_dim values).
+ * Errors: INVALID_ARG (a size, axis, frequency, base or eps out of range), UNSUPPORTED (unknown pairs), OOM, CUDA. */
+mure_status mure_rotary_create(mure_ctx *ctx, const mure_rotary_desc *desc, mure_rotary **out);
+void mure_rotary_free(mure_rotary *rotary);
+
+/* Norm and rotate the batch's new tokens' queries (the plan's query heads) and keys (the cached heads) into q_out and
+ * k_out; q and q_out, or k and k_out, may be NULL.  Here an output may be its input (the same address and strides).
+ * positions: device int32 [n_axes][position_stride], an element for each new token; NULL: along every axis the
+ * plan's own, pos[b] + i, in a tree pos[b] + depth(i).  Errors: INVALID_ARG (as for mure_tokens_append; rotary and
+ * cache do not fit, position_stride below the number of tokens), CUDA. */
+mure_status mure_tokens_rotate(mure_tokens *tokens, mure_tokens_plan *plan, const mure_rotary *rotary, const int32_t *positions,
+                               int64_t position_stride, const mure_tokens_rows *q, const mure_tokens_rows *k,
+                               const mure_tokens_rows *q_out, const mure_tokens_rows *k_out);
+/* mure_tokens_rotate and mure_tokens_append in one pass: the queries go to q_out (q and q_out may be NULL), the
+ * keys as rotated and the values as they are into the new tokens' cells.  The cells' bits are those that
+ * the two calls would leave.  Errors: as for both. */
+mure_status mure_tokens_append_rotated(mure_tokens *tokens, mure_tokens_plan *plan, const mure_rotary *rotary,
+                                       const int32_t *positions, int64_t position_stride, const mure_tokens_rows *q,
+                                       const mure_tokens_rows *k, const mure_tokens_rows *v, const mure_tokens_rows *q_out);
+
+/* Copy whole pages, keys, values and scales: page to_pages[i] of `to` becomes page from_pages[i] of `from` (host arrays of
+ * n ids; the two may be one cache, and then no page is both a source and a target).  So a sequence that is to
+ * continue in two ways gets its last page twice and shares the full ones, and pages that lie apart are brought together.
+ * The ids go with the launch: a captured call copies the same pages whenever it is replayed.  Errors: INVALID_ARG
+ * (caches of different contexts or geometries, or of pools that overlap in part; a negative n, NULL arrays, an id out of
+ * range, a target given twice or that is a source), CUDA. */
+mure_status mure_tokens_copy_pages(mure_tokens *to, const mure_tokens *from, int64_t n, const int32_t *from_pages,
+                                   const int32_t *to_pages);
+/* Keep some of the batch's new tokens, a path of a tree say: sequence b keeps count[b] of them (host [n_seqs]), index (host,
+ * one sequence's after the other, ascending) of its new tokens; their cells move up to pos[b], pos[b] + 1, ...  What
+ * lies in the cells behind them stays.  A next batch then has pos[b] + count[b] earlier cells.  Indexes
+ * go with the launch, as above.  Errors: INVALID_ARG (as for mure_tokens_append; NULL arrays, a negative count, an
+ * index that is out of range or does not ascend), CUDA. */
+mure_status mure_tokens_keep(mure_tokens *tokens, mure_tokens_plan *plan, const int32_t *count, const int32_t *index);
 
 /* Wait for everything queued on the context's stream.  Errors: TIMEOUT (a device-side
  * wait of a token call gave up: see mure_set_wait_limit; the outputs of the token calls

@@ -28,23 +28,6 @@ struct CellParams {
     int part;        // read: 0 all cells, 1 the new tokens'
 };
 
-// A block's tile: sequence, first token of the tile, tokens.
-struct Tile {
-    int seq, i0, n;
-};
-
-__device__ __forceinline__ Tile tile_of(const TokBatch &b, bool all, TokSeq &sq)
-{
-    const int32_t *prefix = all ? b.tile_all : b.tile_new;
-    Tile t;
-    // (one tile for each sequence, as in a decoding step: no search)
-    t.seq = !all && b.one_new ? (int)blockIdx.x : find_prefix(prefix, b.n_seqs, (int)blockIdx.x);
-    sq = b.seq[t.seq];
-    t.i0 = !all && b.one_new ? 0 : ((int)blockIdx.x - __ldg(prefix + t.seq)) * kTokTile;
-    t.n = min(kTokTile, (all ? sq.kv : sq.n_new) - t.i0);
-    return t;
-}
-
 // Eight values as they lie in memory.
 template <class T, bool E4M3>
 struct Raw {
@@ -249,13 +232,6 @@ int dispatch(const CellParams &p, bool read, int dtype, int form, int64_t tiles,
     if (dtype == MURE_F32) return e ? go<float, true>(p, read, tiles, s) : go<float, false>(p, read, tiles, s);
     if (dtype == MURE_F16) return e ? go<__half, true>(p, read, tiles, s) : go<__half, false>(p, read, tiles, s);
     return e ? go<__nv_bfloat16, true>(p, read, tiles, s) : go<__nv_bfloat16, false>(p, read, tiles, s);
-}
-
-int row_lanes(int d)
-{
-    int n = 1;
-    while (n * 8 < d) n *= 2;
-    return n;
 }
 
 }  // namespace

@@ -206,7 +206,7 @@ __device__ __forceinline__ TileCells tile_cells(const TokItem &w, int t, int ali
     return {(w.b0 & ~(align - 1)) + (t - nA) * kCells, w.b1};
 }
 
-template <class T, int DP>
+template <class T, int DP, bool TREE>
 __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_constant__ ChunkParams p)
 {
     using C = Chunk<DP>;
@@ -308,7 +308,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
             }
 
             const int at = pos + row / p.b.group;                                  // the row's position
-            const int lo = pos + r0 / p.b.group, hi = pos + (r0 + 127) / p.b.group;
+            // (a tree's rows see all cells before its own, and lie no further than a chain's)
+            const int lo = TREE ? pos - 1 : pos + r0 / p.b.group, hi = pos + (r0 + 127) / p.b.group;
+            TreeRow tree{};
+            if (TREE) tree = tree_row(p.b, w.row0 + min(row, w.r0 + rows - 1) / p.b.group);
             float m = -INFINITY, l = 0.f;
             for (int t = t0; t < t1; ++t) {
                 const TileCells tc = tile_cells(w, t, p.box);
@@ -324,7 +327,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 auto mask = [&](uint32_t *x, int i0) {               // 32 cells: a bit each
                     if (open) return;
                     auto below = [&](int n) { return n <= i0 ? 0u : n >= i0 + 32 ? ~0u : (1u << (n - i0)) - 1u; };
-                    const uint32_t bits = below(last + 1) & (~below(first) | below(sink));
+                    const uint32_t bits = TREE ? below(tc.end - tc.start) & tree_seen(tree, tc.start + i0, p.b.window, p.b.sinks)
+                                               : below(last + 1) & (~below(first) | below(sink));
 #pragma unroll
                     for (int i = 0; i < 32; ++i) x[i] = bits & (1u << i) ? x[i] : 0xFF800000u;
                 };
@@ -698,13 +702,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
             const T *q = reinterpret_cast<const T *>(p.q.p) + token * p.q.ts + head * p.q.hs;
             const TileCells first = tile_cells(w, w.t0, p.box), end = tile_cells(w, w.t1 - 1, p.box);
             float y[8], m, l;
-            const int pos = w.pos + row / p.b.group, j0 = first.start, j1 = min(end.end, end.start + kCells);
+            TreeRow tree{};
+            if (TREE) tree = tree_row(p.b, token);
+            const int pos = TREE ? tree.pos : w.pos + row / p.b.group, j0 = first.start, j1 = min(end.end, end.start + kCells);
             if (p.code_table)
-                attend_row<T, true>(p.codes, p.code_table + w.table0, w.h, q, p.q.vec, pos, j0, j1, p.b.window, p.b.sinks,
-                                    p.b.scale_log2, y, m, l);
+                attend_row<T, true, TREE>(p.codes, p.code_table + w.table0, w.h, q, p.q.vec, pos, j0, j1, p.b.window, p.b.sinks,
+                                          p.b.scale_log2, y, m, l, tree);
             else
-                attend_row<T, false>(p.pool, p.b.table + w.table0, w.h, q, p.q.vec, pos, j0, j1, p.b.window, p.b.sinks,
-                                     p.b.scale_log2, y, m, l);
+                attend_row<T, false, TREE>(p.pool, p.b.table + w.table0, w.h, q, p.q.vec, pos, j0, j1, p.b.window, p.b.sinks,
+                                           p.b.scale_log2, y, m, l, tree);
             if (w.parts > 1) {
                 const int64_t pr = (int64_t)w.part * kChunkRows + r;
                 if (lane * 8 < D) store8(p.w.part + pr * DP + lane * 8, 1, y);
@@ -754,11 +760,18 @@ __global__ void __launch_bounds__(256) k_tokens_join(const TokItem *cut, int DP,
     if (lse && lane == 0) lse[(int64_t)token * b.n_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945f;
 }
 
+template <class T, int DP, bool TREE>
+void pieces(const ChunkParams &p, cudaStream_t s)
+{
+    allow_dynamic_smem_once<k_tokens_chunk<T, DP, TREE>>(Chunk<DP>::kSmem);
+    k_tokens_chunk<T, DP, TREE><<<p.w.blocks, kThreads, Chunk<DP>::kSmem, s>>>(p);
+}
+
 template <class T, int DP>
 int go(const ChunkParams &p, const TokChunk &c, cudaStream_t s)
 {
-    allow_dynamic_smem_once<k_tokens_chunk<T, DP>>(Chunk<DP>::kSmem);
-    k_tokens_chunk<T, DP><<<p.w.blocks, kThreads, Chunk<DP>::kSmem, s>>>(p);
+    if (p.b.node) pieces<T, DP, true>(p, s);
+    else pieces<T, DP, false>(p, s);
     if (c.n_cut == 0) return 1;
     k_tokens_join<T><<<dim3(c.n_cut, 32), 256, 0, s>>>(c.cut, DP, p.b, p.pool.d, p.out, p.lse, p.w.part, p.ml);
     return 2;

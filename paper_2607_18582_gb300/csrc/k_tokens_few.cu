@@ -240,7 +240,7 @@ __device__ __forceinline__ uint32_t load2(const T *p, int vec)
     return (uint32_t)u[0] | (uint32_t)u[1] << 16;
 }
 
-template <class T, bool E4M3, int DP>
+template <class T, bool E4M3, int DP, bool TREE>
 __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_tokens_few(FewParams p)
 {
     using F = Few<T, E4M3, DP>;
@@ -260,7 +260,9 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
         if (threadIdx.x < sizeof(TokItem) / 8)
             reinterpret_cast<int2 *>(&w)[threadIdx.x] = __ldg(reinterpret_cast<const int2 *>(p.w.items + it) + threadIdx.x);
         __syncthreads();
-        if (threadIdx.x < 2) ends[threadIdx.x] = w.pos + (w.r0 + (threadIdx.x ? w.rows - 1 : 0)) / p.b.group;
+        // (a tree's rows see all cells before its own, and lie no further than a chain's)
+        if (threadIdx.x < 2)
+            ends[threadIdx.x] = TREE && threadIdx.x == 0 ? w.pos - 1 : w.pos + (w.r0 + (threadIdx.x ? w.rows - 1 : 0)) / p.b.group;
         __syncthreads();
         const int nA = (w.a1 + F::kTile - 1) / F::kTile, b_al = w.b0 & ~(kAlign - 1);
 
@@ -572,7 +574,14 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
             float top[2] = {-INFINITY, -INFINITY};
             uint32_t seen = 0;                               // not open: a bit per score
             int row_pos[2] = {0, 0};
-            if (!open) {
+            uint32_t tree[2] = {0, 0};                       // a tree's rows: a bit per cell of the step
+            if (TREE && !open) {
+                const uint32_t part = bits_below(end - start) & ~bits_below(begin - start);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    tree[i] = part & tree_seen(tree_row(p.b, w.row0 + (w.r0 + min(g + 8 * i, w.rows - 1)) / p.b.group), start,
+                                               p.b.window, p.b.sinks);
+            } else if (!open) {
                 row_pos[0] = w.pos + (w.r0 + g) / p.b.group;
                 row_pos[1] = w.pos + (w.r0 + g + 8) / p.b.group;
             }
@@ -589,7 +598,8 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                     float x = E4M3 ? s[n][i] * (i & 1 ? f1 : f0) : s[n][i];
                     if (!open) {
                         const int j = start + n * 8 + 2 * t + (i & 1);
-                        const bool see = j >= begin && j < end && tok_seen(j, row_pos[i >> 1], p.b.window, p.b.sinks);
+                        const bool see = TREE ? tree[i >> 1] >> (n * 8 + 2 * t + (i & 1)) & 1u
+                                              : j >= begin && j < end && tok_seen(j, row_pos[i >> 1], p.b.window, p.b.sinks);
                         x = see ? x : -INFINITY;
                         seen |= (uint32_t)see << (n * 4 + i);
                     }
@@ -778,8 +788,10 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
                 const T *q = reinterpret_cast<const T *>(p.q.p) + (int64_t)(w.row0 + rr / p.b.group) * p.q.ts +
                              (int64_t)(w.h * p.b.group + rr % p.b.group) * p.q.hs;
                 float x[8], mm, ll;
-                attend_row<T, E4M3>(p.pool, p.b.table + w.table0, w.h, q, p.q.vec, w.pos + rr / p.b.group, j0, j1, p.b.window, p.b.sinks,
-                                    p.b.scale_log2, x, mm, ll);
+                TreeRow tree{};
+                if (TREE) tree = tree_row(p.b, w.row0 + rr / p.b.group);
+                attend_row<T, E4M3, TREE>(p.pool, p.b.table + w.table0, w.h, q, p.q.vec, TREE ? tree.pos : w.pos + rr / p.b.group, j0, j1,
+                                          p.b.window, p.b.sinks, p.b.scale_log2, x, mm, ll, tree);
                 for (int k = 0; k < kWarps; ++k) {
                     float *row = join + (k * kFewRows + r) * JR;
                     if (lane * 8 < D) {
@@ -912,13 +924,19 @@ __global__ void __launch_bounds__(kWarps * 32, Few<T, E4M3, DP>::kBlocks) k_toke
     }
 }
 
-template <class T, bool E4M3, int DP>
+template <class T, bool E4M3, int DP, bool TREE>
 int go(const FewParams &p, cudaStream_t s)
 {
     using F = Few<T, E4M3, DP>;
-    allow_dynamic_smem_once<k_tokens_few<T, E4M3, DP>>(F::kSmem);
-    k_tokens_few<T, E4M3, DP><<<p.w.blocks, kWarps * 32, F::kSmem, s>>>(p);
+    allow_dynamic_smem_once<k_tokens_few<T, E4M3, DP, TREE>>(F::kSmem);
+    k_tokens_few<T, E4M3, DP, TREE><<<p.w.blocks, kWarps * 32, F::kSmem, s>>>(p);
     return 1;
+}
+
+template <class T, bool E4M3, int DP>
+int go(const FewParams &p, cudaStream_t s)
+{
+    return p.b.node ? go<T, E4M3, DP, true>(p, s) : go<T, E4M3, DP, false>(p, s);
 }
 
 template <class T, bool E4M3>

@@ -1,0 +1,181 @@
+// Token caches: pages copied, and cells of kept new tokens moved up.
+//
+// Both are copies of 16-byte words that touch each byte once, bound by device memory where they are large and by the
+// launch where they are small.  What is copied goes with the launch, as kernel arguments: a call needs no workspace, two
+// calls share nothing, and nothing waits for an upload.
+#include <cstring>
+
+#include "tokens_util.cuh"
+
+namespace mure {
+
+namespace {
+
+// ------------------------------------------------------------------- pages --
+constexpr int kThreads = 256;
+constexpr int kWords = 4;                    // 16-byte words that a thread has on their way
+
+// Pairs of a launch: two sizes, so that a short list does not carry a long one's arguments.
+template <int N>
+struct PageParams {
+    const char *from[4];                     // k, v, and their scales
+    char *to[4];
+    int64_t bytes[2];                        // of a page of codes or values, of its scales
+    int n;
+    int32_t page[2 * N];
+};
+
+// blockIdx.x: a pair of pages; y: k or v; z: a share of the page.
+template <int N>
+__global__ void __launch_bounds__(kThreads) k_tokens_copy(const __grid_constant__ PageParams<N> p)
+{
+    const int64_t a = p.page[2 * blockIdx.x], b = p.page[2 * blockIdx.x + 1];
+    const int which = blockIdx.y;
+    {
+        const uint4 *from = reinterpret_cast<const uint4 *>(p.from[which] + a * p.bytes[0]);
+        uint4 *to = reinterpret_cast<uint4 *>(p.to[which] + b * p.bytes[0]);
+        const int n = (int)(p.bytes[0] / 16);
+        for (int i = blockIdx.z * kThreads * kWords + threadIdx.x; i < n; i += gridDim.z * kThreads * kWords) {
+            uint4 w[kWords];
+#pragma unroll
+            for (int u = 0; u < kWords; ++u)
+                if (i + u * kThreads < n) w[u] = from[i + u * kThreads];
+#pragma unroll
+            for (int u = 0; u < kWords; ++u)
+                if (i + u * kThreads < n) to[i + u * kThreads] = w[u];
+        }
+    }
+    if (p.bytes[1] && blockIdx.z == 0) {                             // (pages of 8 cells and up: a multiple of 8 bytes)
+        const uint2 *from = reinterpret_cast<const uint2 *>(p.from[2 + which] + a * p.bytes[1]);
+        uint2 *to = reinterpret_cast<uint2 *>(p.to[2 + which] + b * p.bytes[1]);
+        for (int i = threadIdx.x; i < (int)(p.bytes[1] / 8); i += kThreads) to[i] = from[i];
+    }
+}
+
+template <int N>
+void copy(const TokPool &from, const TokPool &to, int64_t bytes, int64_t scale_bytes, const int32_t *pages, int n, cudaStream_t s)
+{
+    static_assert(sizeof(PageParams<N>) <= 32764, "more than a kernel's arguments");
+    PageParams<N> p;
+    p.from[0] = static_cast<const char *>(from.k); p.from[1] = static_cast<const char *>(from.v);
+    p.from[2] = reinterpret_cast<const char *>(from.ks); p.from[3] = reinterpret_cast<const char *>(from.vs);
+    p.to[0] = static_cast<char *>(to.k); p.to[1] = static_cast<char *>(to.v);
+    p.to[2] = reinterpret_cast<char *>(to.ks); p.to[3] = reinterpret_cast<char *>(to.vs);
+    p.bytes[0] = bytes; p.bytes[1] = scale_bytes;
+    p.n = n;
+    memcpy(p.page, pages, (size_t)n * 2 * sizeof(int32_t));
+    const int64_t z = (bytes / 16 + kThreads * kWords - 1) / (kThreads * kWords);
+    k_tokens_copy<N><<<dim3(n, 2, (unsigned)(z < 1024 ? z : 1024)), kThreads, 0, s>>>(p);
+}
+
+// ------------------------------------------------------------------- cells --
+constexpr int kKeepSeqs = 512, kKeepIndex = 6000;
+
+struct KeepParams {
+    TokPool pool;
+    const TokSeq *seq;
+    const int32_t *table;
+    int elt;                                 // bytes of a value, or of a code
+    int scales;
+    int lanes;                               // threads of a row, a power of two: 8 values each
+    int32_t of[kKeepSeqs], first[kKeepSeqs + 1], to[kKeepSeqs];
+    int32_t index[kKeepIndex];
+};
+
+struct alignas(16) Wide { uint4 a, b; };
+
+// A block moves one sequence's cells, a group of threads a cached head's rows at a time.  A thread takes its part
+// of four cells to registers before it writes any: as the indexes ascend, the fifth source lies past the fourth target,
+// and so does every later one.
+template <class W>                           // eight values: Wide (fp32), uint4 (16 bits), uint2 (codes)
+__global__ void __launch_bounds__(128) k_tokens_keep(const __grid_constant__ KeepParams p)
+{
+    const int b = blockIdx.x;
+    const TokSeq sq = p.seq[p.of[b]];
+    const int32_t *table = p.table + sq.table0;
+    const int D = p.pool.d, slot = threadIdx.x & (p.lanes - 1), c = slot * 8;
+    const int h = blockIdx.y * (128 / p.lanes) + threadIdx.x / p.lanes;
+    if (c >= D || h >= p.pool.hk) return;
+    const int i0 = p.first[b], n = p.first[b + 1] - i0;
+    constexpr int U = 4;
+    for (int i = 0; i < n; i += U) {
+        W k[U], v[U];
+        uint32_t scale[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i + u < n) {
+                const int64_t row = cell_row(p.pool, table, h, sq.pos + p.index[i0 + i + u]);
+                k[u] = *reinterpret_cast<const W *>(static_cast<const char *>(p.pool.k) + (row * D + c) * p.elt);
+                v[u] = *reinterpret_cast<const W *>(static_cast<const char *>(p.pool.v) + (row * D + c) * p.elt);
+                if (p.scales && slot == 0) scale[u] = p.pool.ks[row] | (uint32_t)p.pool.vs[row] << 8;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i + u < n) {
+                const int64_t row = cell_row(p.pool, table, h, sq.pos + p.to[b] + i + u);
+                *reinterpret_cast<W *>(static_cast<char *>(p.pool.k) + (row * D + c) * p.elt) = k[u];
+                *reinterpret_cast<W *>(static_cast<char *>(p.pool.v) + (row * D + c) * p.elt) = v[u];
+                if (p.scales && slot == 0) {
+                    p.pool.ks[row] = (uint8_t)scale[u];
+                    p.pool.vs[row] = (uint8_t)(scale[u] >> 8);
+                }
+            }
+        }
+    }
+}
+
+}  // namespace
+
+int launch_tokens_copy_pages(const TokPool &from, const TokPool &to, int elt, bool scales, const int32_t *pages, int64_t n, cudaStream_t s)
+{
+    constexpr int kShort = 64, kLong = 4000;
+    const int64_t cells = (int64_t)from.hk << from.page_log2;
+    int launches = 0;
+    for (int64_t i = 0; i < n;) {
+        const int take = (int)(n - i < kLong ? n - i : kLong);
+        if (take <= kShort) copy<kShort>(from, to, cells * from.d * elt, scales ? cells : 0, pages + 2 * i, take, s);
+        else copy<kLong>(from, to, cells * from.d * elt, scales ? cells : 0, pages + 2 * i, take, s);
+        i += take;
+        ++launches;
+    }
+    return launches;
+}
+
+int launch_tokens_keep(const TokPool &pool, const TokBatch &b, int elt, bool scales, const int32_t *seq, const int32_t *first,
+                       const int32_t *end, const int32_t *to, const int32_t *index, int64_t n, cudaStream_t s)
+{
+    static_assert(sizeof(KeepParams) <= 32764, "more than a kernel's arguments");
+    const int lanes = row_lanes(pool.d), per = 128 / lanes;
+    int launches = 0;
+    int64_t i = 0;
+    int32_t at = n > 0 ? first[0] : 0;       // the next index of sequence i's
+    while (i < n) {
+        KeepParams p;
+        p.pool = pool; p.seq = b.seq; p.table = b.table;
+        p.elt = elt; p.scales = scales; p.lanes = lanes;
+        int seqs = 0, used = 0;
+        while (i < n && seqs < kKeepSeqs && used < kKeepIndex) {
+            const int take = end[i] - at < kKeepIndex - used ? end[i] - at : kKeepIndex - used;
+            p.of[seqs] = seq[i];
+            p.first[seqs] = used;
+            p.to[seqs] = to[i] + (at - first[i]);
+            memcpy(p.index + used, index + at, (size_t)take * sizeof(int32_t));
+            used += take;
+            at += take;
+            ++seqs;
+            if (at < end[i]) break;    // the rest of a long list follows in the stream's order
+            ++i;
+            if (i < n) at = first[i];
+        }
+        p.first[seqs] = used;
+        const dim3 grid(seqs, (pool.hk + per - 1) / per);
+        if (elt == 4) k_tokens_keep<Wide><<<grid, 128, 0, s>>>(p);
+        else if (elt == 2) k_tokens_keep<uint4><<<grid, 128, 0, s>>>(p);
+        else k_tokens_keep<uint2><<<grid, 128, 0, s>>>(p);
+        ++launches;
+    }
+    return launches;
+}
+
+}  // namespace mure

@@ -12,36 +12,9 @@
 #include <queue>
 #include <unordered_map>
 
-#include "host.cuh"
-#include "tokens.cuh"
+#include "tokens_host.cuh"
 
 using namespace mure;
-
-struct mure_tokens {
-    mure_ctx *ctx = nullptr;
-    mure_tokens_desc d{};
-    void *own = nullptr;      // the library's allocation of the pools (null: the caller's pools)
-    CUtensorMap map_k, map_v; // 16-bit cells of up to kChunkDim values: the pools
-};
-
-struct mure_tokens_plan {
-    mure_ctx *ctx = nullptr;
-    mure_tokens_desc d{};     // the geometry it serves (pools ignored)
-    bool ready = false;
-    TokBatch b;
-    int64_t n_new = 0, n_cells = 0;          // packed rows of the new tokens / of all cells
-    int64_t tiles_new = 0, tiles_all = 0;
-    int new_past_end = -1;                   // a sequence whose new tokens end past its cells
-    std::string append_fault;                // why the batch's new tokens cannot be written ("" if they can)
-    TokWork few;                             // 16-bit types: the rows that the kernel for few rows takes
-    TokChunk chunk;                          // ... and those that the kernel for chunks takes
-    // E4M3: the pages that chunks read, as 16-bit pages
-    const int32_t *wide_pages = nullptr, *wide_table = nullptr;
-    int64_t n_wide = 0;
-    CUtensorMap map_k, map_v;
-    void *mem = nullptr, *part = nullptr, *wide = nullptr;    // tables; partial results; 16-bit pages
-    size_t mem_bytes = 0, part_bytes = 0, wide_bytes = 0;
-};
 
 namespace {
 
@@ -52,16 +25,7 @@ namespace {
 // (Measured at that one shape.  fp32 rows, and heads of more than 128 values, have no other kernel.)
 int few_rows_up_to(bool codes, int d) { return codes ? 64 : d <= 64 ? 32 : 16; }
 
-constexpr int64_t kMostPos = int64_t(1) << 30, kMostStride = int64_t(1) << 40, kMostUnits = int64_t(1) << 24;
-
-int elt_bytes(int dtype) { return dtype == MURE_F32 ? 4 : 2; }
-
-int log2_of(int n)
-{
-    int l = 0;
-    while ((1 << l) < n) ++l;
-    return l;
-}
+constexpr int64_t kMostPos = int64_t(1) << 30, kMostUnits = int64_t(1) << 24;
 
 void check_geometry(mure_ctx *c, const mure_tokens_desc &d)
 {
@@ -76,14 +40,6 @@ void check_geometry(mure_ctx *c, const mure_tokens_desc &d)
     FAILIF(d.n_pages < 1 || d.n_pages > INT32_MAX, c, MURE_ERR_INVALID_ARG, "n_pages %lld not in 1..2^31 - 1",
            (long long)d.n_pages);
     FAILIF(d.reserved != 0, c, MURE_ERR_INVALID_ARG, "reserved fields must be 0");
-}
-
-TokPool pool_of(const mure_tokens *t)
-{
-    TokPool p;
-    p.k = t->d.k; p.v = t->d.v; p.ks = t->d.k_scale; p.vs = t->d.v_scale;
-    p.hk = t->d.n_kv_heads; p.d = t->d.head_dim; p.page_log2 = log2_of(t->d.page_size);
-    return p;
 }
 
 // At least `bytes` of device memory, and up to 16 MiB more where it grows (the next steps' tables do).
@@ -128,7 +84,8 @@ struct Shape {
     double half;   // a tile of at most half the rows, in tiles (chunks, 0.6 -> 0.9: ragged ones 278 -> 258 us)
 };
 
-void add_units(std::vector<Unit> &units, const TokSeq &q, int hk, int group, int window, int sinks, const Shape &sh)
+// node: a tree's tokens (null: a chain).
+void add_units(std::vector<Unit> &units, const TokSeq &q, const TokNode *node, int hk, int group, int window, int sinks, const Shape &sh)
 {
     const int64_t n_rows = (int64_t)q.n_new * group;
     for (int h = 0; h < hk; ++h)
@@ -137,11 +94,17 @@ void add_units(std::vector<Unit> &units, const TokSeq &q, int hk, int group, int
             TokItem &w = u.item;
             w.h = h; w.r0 = (int)r0; w.rows = (int)std::min<int64_t>(sh.rows, n_rows - r0);
             w.pos = q.pos; w.row0 = q.row0; w.table0 = q.table0;
-            const int lo = q.pos + (int)(r0 / group), hi = q.pos + (int)((r0 + w.rows - 1) / group);
-            const int end = std::min(q.kv, hi + 1);
+            const int i0 = (int)(r0 / group), i1 = (int)((r0 + w.rows - 1) / group);
+            int lo = q.pos + i0;
+            if (node) {
+                int depth = node[i0].depth;
+                for (int i = i0 + 1; i <= i1; ++i) depth = std::min(depth, node[i].depth);
+                lo = q.pos + depth;
+            }
+            const int end = std::min(q.kv, q.pos + i1 + 1);          // (an ancestor comes before its token)
             w.b1 = end;
             if (window > 0 && lo >= window) {
-                w.b0 = std::min(lo - window + 1, end);
+                w.b0 = std::min(node ? std::min(lo - window + 1, q.pos) : lo - window + 1, end);
                 w.a1 = std::min(sinks, end);
                 if (w.a1 >= w.b0 / sh.align * sh.align) w.a1 = w.b0 = 0;   // one run from the first cell on
             }
@@ -232,6 +195,30 @@ Shares pack(const std::vector<Unit> &units, const Shape &sh)
     return r;
 }
 
+// A tree's tokens and their bits, or why its parents are none.
+std::string add_tree(std::vector<TokNode> &nodes, std::vector<uint32_t> &bits, const int32_t *parents, int n, int pos, int window, int sinks)
+{
+    const int words = (n + 31) / 32;     // (65,535 trees of the most tokens: 2^31 words)
+    const size_t node0 = nodes.size(), bit0 = bits.size();
+    nodes.resize(node0 + n);
+    bits.resize(bit0 + (size_t)n * words);
+    TokNode *node = nodes.data() + node0;
+    for (int i = 0; i < n; ++i) {
+        const int p = parents[i];
+        if (p < -1 || p >= i) return "new token " + std::to_string(i) + ": parent " + std::to_string(p) + " is not in -1.." + std::to_string(i - 1);
+        uint32_t *mine = bits.data() + bit0 + (size_t)i * words;
+        node[i] = {p < 0 ? 0 : node[p].depth + 1, pos, words, (uint32_t)(mine - bits.data())};
+        if (window == 0) {
+            if (p >= 0) std::copy(mine - (size_t)(i - p) * words, mine - (size_t)(i - p - 1) * words, mine);
+            mine[i / 32] |= 1u << i % 32;
+        } else {
+            for (int a = i; a >= 0; a = parents[a])
+                if (node[a].depth > node[i].depth - window || pos + node[a].depth < sinks) mine[a / 32] |= 1u << a % 32;
+        }
+    }
+    return "";
+}
+
 // The packed device image of a plan's tables: parts at 16-byte boundaries of one host buffer.
 struct Image {
     std::vector<char> bytes;
@@ -245,7 +232,7 @@ struct Image {
     }
 };
 
-void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
+void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp, bool tree = false, const int32_t *parents = nullptr)
 {
     mure_ctx *c = p->ctx;
     p->ready = false;
@@ -275,6 +262,8 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
     std::vector<Span> written;
     std::string fault;
     int past_end = -1;
+    std::vector<TokNode> nodes;
+    std::vector<uint32_t> bits;
     for (int s = 0; s < n; ++s) {
         const int64_t nn = b.new_len[s], pos = b.pos[s], kv = b.kv_len[s];
         FAILIF(nn < 0 || pos < 0 || kv < 0, c, MURE_ERR_INVALID_ARG, "sequence %d: a negative length or position", s);
@@ -295,6 +284,13 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
         FAILIF(n_new > INT32_MAX || t_all > INT32_MAX, c, MURE_ERR_UNSUPPORTED, "more than 2^31 - 1 new tokens or tiles of cells");
         tile_new[s + 1] = (int32_t)t_new;
         tile_all[s + 1] = (int32_t)t_all;
+        if (tree && nn > 0) {
+            FAILIF(!parents, c, MURE_ERR_INVALID_ARG, "NULL parents");
+            FAILIF(nn > MURE_TREE_MAX, c, MURE_ERR_UNSUPPORTED, "sequence %d: a tree of %lld tokens, and %d are the most", s, (long long)nn,
+                   (int)MURE_TREE_MAX);
+            const std::string why = add_tree(nodes, bits, parents + seq[s].row0, (int)nn, (int)pos, b.window, b.sinks);
+            FAILIF(!why.empty(), c, MURE_ERR_INVALID_ARG, "sequence %d: %s", s, why.c_str());
+        }
         if (nn > 0 && pos + nn > kv) {
             if (past_end < 0) past_end = s;
             if (fault.empty())
@@ -334,7 +330,7 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
         const Shape &sh = as_chunk ? chunk_shape : few_shape;
         FAILIF((int64_t)(few.size() + chunk.size()) + (rows + sh.rows - 1) / sh.rows * d.n_kv_heads > kMostUnits, c,
                MURE_ERR_UNSUPPORTED, "more than 2^24 pieces of work");
-        add_units(as_chunk ? chunk : few, q, d.n_kv_heads, group, b.window, b.sinks, sh);
+        add_units(as_chunk ? chunk : few, q, tree ? nodes.data() + q.row0 : nullptr, d.n_kv_heads, group, b.window, b.sinks, sh);
         if (!as_chunk || !wide) continue;
         // the pages that any of its rows reads
         wide_table.resize(table.size(), 0);
@@ -354,7 +350,7 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
     const size_t o_seq = im.add(seq), o_table = im.add(table), o_new = im.add(tile_new), o_all = im.add(tile_all);
     const size_t o_few = im.add(fs.items), o_few1 = im.add(fs.first), o_fewc = im.add(std::vector<int32_t>(fs.cut.size(), 0));
     const size_t o_chunk = im.add(cs.items), o_chunk1 = im.add(cs.first), o_cut = im.add(cs.cut);
-    const size_t o_wt = im.add(wide_table), o_wp = im.add(wide_pages);
+    const size_t o_wt = im.add(wide_table), o_wp = im.add(wide_pages), o_node = im.add(nodes), o_bits = im.add(bits);
     const size_t few_part = ((size_t)fs.parts * few_part_floats(d.head_dim) * 4 + 255) / 256 * 256;
     reserve(c, p->mem, p->mem_bytes, im.bytes.size());
     const size_t chunk_part = (size_t)cs.parts * chunk_part_floats(d.head_dim) * 4;
@@ -390,6 +386,8 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
     p->wide_table = reinterpret_cast<int32_t *>(m + o_wt);
     p->wide_pages = reinterpret_cast<int32_t *>(m + o_wp);
     p->n_wide = (int64_t)wide_pages.size();
+    v.node = tree ? reinterpret_cast<TokNode *>(m + o_node) : nullptr;
+    v.bits = reinterpret_cast<uint32_t *>(m + o_bits);
     v.n_seqs = n;
     v.one_new = t_new == n;
     for (int s = 0; s < n && v.one_new; ++s) v.one_new = tile_new[s + 1] - tile_new[s] == 1;
@@ -404,46 +402,41 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp)
     p->tiles_all = t_all;
     p->new_past_end = past_end;
     p->append_fault = fault;
+    p->seq = std::move(seq);
     p->ready = true;
 }
 
-// A call's cache and plan.
-void check_pair(mure_ctx *c, const mure_tokens *t, const mure_tokens_plan *p)
+mure_status create_plan(mure_tokens *t, const mure_tokens_batch *batch, bool tree, const int32_t *parents, mure_tokens_plan **out)
 {
-    FAILIF(!p, c, MURE_ERR_INVALID_ARG, "NULL plan");
-    FAILIF(p->ctx != c, c, MURE_ERR_INVALID_ARG, "cache and plan belong to different contexts");
-    FAILIF(!p->ready, c, MURE_ERR_INVALID_ARG, "the plan holds no batch");
-    const mure_tokens_desc &a = t->d, &b = p->d;
-    FAILIF(a.n_kv_heads != b.n_kv_heads || a.head_dim != b.head_dim || a.page_size != b.page_size || a.dtype != b.dtype ||
-               a.form != b.form || a.n_pages != b.n_pages,
-           c, MURE_ERR_INVALID_ARG, "the plan was made for caches of another geometry");
+    if (!t) return MURE_ERR_INVALID_ARG;
+    mure_ctx *c = t->ctx;
+    return run(c, [&] {
+        FAILIF(!out, c, MURE_ERR_INVALID_ARG, "NULL out");
+        *out = nullptr;
+        CK(c, cudaSetDevice(c->device));
+        auto p = std::make_unique<mure_tokens_plan>();
+        p->ctx = c;
+        p->d = t->d;
+        try {
+            set_plan(p.get(), batch, tree, parents);
+        } catch (...) {
+            dfree(c, p->mem);
+            dfree(c, p->part);
+            dfree(c, p->wide);
+            throw;
+        }
+        *out = p.release();
+    });
 }
 
-TokRows check_rows(mure_ctx *c, const mure_tokens_rows *r, const mure_tokens_desc &d, int64_t rows, int heads, const char *name)
+mure_status reset_plan(mure_tokens_plan *p, const mure_tokens_batch *batch, bool tree, const int32_t *parents)
 {
-    TokRows o;
-    if (rows == 0) return o;
-    const int e = elt_bytes(d.dtype);
-    FAILIF(!r || !r->p, c, MURE_ERR_INVALID_ARG, "NULL %s", name);
-    FAILIF((uintptr_t)r->p % e != 0, c, MURE_ERR_INVALID_ARG, "%s is not aligned to its type", name);
-    o.p = static_cast<char *>(r->p);
-    FAILIF(r->token_stride < 0 || r->head_stride < 0 || r->token_stride > kMostStride || r->head_stride > kMostStride, c,
-           MURE_ERR_INVALID_ARG, "a stride of %s is not in 0..2^40", name);
-    o.ts = r->token_stride;
-    o.hs = r->head_stride;
-    const int per = 16 / e;
-    o.vec = (uintptr_t)r->p % 16 == 0 && (rows == 1 || o.ts % per == 0) && (heads == 1 || o.hs % per == 0);
-    return o;
-}
-
-// Rows that are written must not lie on one another.
-void check_apart(mure_ctx *c, const TokRows &r, const mure_tokens_desc &d, int64_t rows, int heads, const char *name)
-{
-    if (rows == 0) return;
-    const int64_t ts = r.ts, hs = r.hs, D = d.head_dim;
-    const bool ok = (heads == 1 || rows == 1) ? (heads == 1 || hs >= D) && (rows == 1 || ts >= D)
-                                              : (hs >= D && ts >= hs * (heads - 1) + D) || (ts >= D && hs >= ts * (rows - 1) + D);
-    FAILIF(!ok, c, MURE_ERR_INVALID_ARG, "rows of %s overlap", name);
+    if (!p) return MURE_ERR_INVALID_ARG;
+    return run(p->ctx, [&] {
+        p->ready = false;
+        CK(p->ctx, cudaSetDevice(p->ctx->device));
+        set_plan(p, batch, tree, parents);
+    });
 }
 
 }  // namespace
@@ -511,35 +504,19 @@ mure_status mure_tokens_buffers(const mure_tokens *t, mure_tokens_desc *out)
 
 mure_status mure_tokens_plan_create(mure_tokens *t, const mure_tokens_batch *batch, mure_tokens_plan **out)
 {
-    if (!t) return MURE_ERR_INVALID_ARG;
-    mure_ctx *c = t->ctx;
-    return run(c, [&] {
-        FAILIF(!out, c, MURE_ERR_INVALID_ARG, "NULL out");
-        *out = nullptr;
-        CK(c, cudaSetDevice(c->device));
-        auto p = std::make_unique<mure_tokens_plan>();
-        p->ctx = c;
-        p->d = t->d;
-        try {
-            set_plan(p.get(), batch);
-        } catch (...) {
-            dfree(c, p->mem);
-            dfree(c, p->part);
-            dfree(c, p->wide);
-            throw;
-        }
-        *out = p.release();
-    });
+    return create_plan(t, batch, false, nullptr, out);
 }
 
-mure_status mure_tokens_plan_set(mure_tokens_plan *p, const mure_tokens_batch *batch)
+mure_status mure_tokens_plan_create_tree(mure_tokens *t, const mure_tokens_batch *batch, const int32_t *parents, mure_tokens_plan **out)
 {
-    if (!p) return MURE_ERR_INVALID_ARG;
-    return run(p->ctx, [&] {
-        p->ready = false;
-        CK(p->ctx, cudaSetDevice(p->ctx->device));
-        set_plan(p, batch);
-    });
+    return create_plan(t, batch, true, parents, out);
+}
+
+mure_status mure_tokens_plan_set(mure_tokens_plan *p, const mure_tokens_batch *batch) { return reset_plan(p, batch, false, nullptr); }
+
+mure_status mure_tokens_plan_set_tree(mure_tokens_plan *p, const mure_tokens_batch *batch, const int32_t *parents)
+{
+    return reset_plan(p, batch, true, parents);
 }
 
 void mure_tokens_plan_free(mure_tokens_plan *p)

@@ -24,6 +24,15 @@ struct TokPool {
     int hk = 0, d = 0, page_log2 = 0;
 };
 
+// A new token of a tree: its cells before the sequence's new ones are seen by its position, as in any batch; of the new
+// ones' those whose bit is set (itself and its ancestors, as far as a window holds them).
+struct TokNode {
+    int32_t depth;   // its position is the sequence's first new one's and this
+    int32_t first;   // the cell of the sequence's first new token
+    int32_t words;   // 32-bit words of bits
+    uint32_t at;     // the first one
+};
+
 // A batch on the device.
 struct TokBatch {
     const TokSeq *seq = nullptr;
@@ -35,6 +44,8 @@ struct TokBatch {
     int n_heads = 0, group = 0;              // query heads; query heads per cached one
     int window = 0, sinks = 0;
     float scale_log2 = 0.f;                  // factor of the scores, times log2(e)
+    const TokNode *node = nullptr;           // trees: a new token each (null: new tokens follow one another)
+    const uint32_t *bits = nullptr;
 };
 
 constexpr int kTokTile = 16;
@@ -100,6 +111,28 @@ int launch_tokens_chunk(const TokPool &pool, const TokBatch &b, const TokChunk &
 // together with where they come from (`codes`, `code_table`).  A value that f16 does not reach becomes a NaN:
 // the rows that meet it are done from the codes.
 int launch_tokens_widen(const TokPool &pool, int dtype, const int32_t *pages, int64_t n_list, void *k, void *v, cudaStream_t s);
+
+// Norm and rotation of the new tokens' queries and keys.
+struct TokRotary {
+    const uint64_t *turn = nullptr;      // [rot / 2] a pair's turns per position, times 2^64, modulo 2^64
+    const float *weight = nullptr;       // [2][d] of the queries' norm and the keys'
+    const uint8_t *axis = nullptr;       // [rot / 2] the pair's axis of positions
+    int rot = 0, adjacent = 0;
+    int norm_q = 0, norm_k = 0;
+    float eps = 0.f;
+    const int32_t *positions = nullptr;  // [axes][position_stride] (null: the batch's, along every axis)
+    int64_t position_stride = 0;
+};
+// cells: k and v go into their cells (form as given); else k's rows to k_out, and v is not used.
+int launch_tokens_rotate(const TokPool &pool, const TokBatch &b, const TokRotary &r, int dtype, int form, bool cells, int q_heads,
+                         int k_heads, TokRows q, TokRows k, TokRows v, TokRows q_out, TokRows k_out, int64_t tiles, cudaStream_t s);
+
+// Pages pages[2 i] of one cache to pages[2 i + 1] of another of its geometry (host array, n pairs).
+int launch_tokens_copy_pages(const TokPool &from, const TokPool &to, int elt, bool scales, const int32_t *pages, int64_t n, cudaStream_t s);
+// New tokens' cells moved up: of sequence seq[i] (host arrays), the cells of the new tokens index[first[i] ..
+// end[i] - 1], ascending, to those of its new tokens to[i], to[i] + 1, ...
+int launch_tokens_keep(const TokPool &pool, const TokBatch &b, int elt, bool scales, const int32_t *seq, const int32_t *first,
+                       const int32_t *end, const int32_t *to, const int32_t *index, int64_t n, cudaStream_t s);
 
 int launch_tokens_append(const TokPool &pool, const TokBatch &b, int dtype, int form, TokRows k, TokRows v, int64_t tiles,
                          cudaStream_t s);

@@ -139,20 +139,66 @@ __device__ __forceinline__ int find_prefix(const int32_t *prefix, int n, int x)
     return lo;
 }
 
+// A block's tile: sequence, first token of the tile, tokens.
+struct Tile {
+    int seq, i0, n;
+};
+
+__device__ __forceinline__ Tile tile_of(const TokBatch &b, bool all, TokSeq &sq)
+{
+    const int32_t *prefix = all ? b.tile_all : b.tile_new;
+    Tile t;
+    // (one tile for each sequence, as in a decoding step: no search)
+    t.seq = !all && b.one_new ? (int)blockIdx.x : find_prefix(prefix, b.n_seqs, (int)blockIdx.x);
+    sq = b.seq[t.seq];
+    t.i0 = !all && b.one_new ? 0 : ((int)blockIdx.x - __ldg(prefix + t.seq)) * kTokTile;
+    t.n = min(kTokTile, (all ? sq.kv : sq.n_new) - t.i0);
+    return t;
+}
+
+// Threads of a row of d values, eight each: a power of two.
+inline int row_lanes(int d)
+{
+    int n = 1;
+    while (n * 8 < d) n *= 2;
+    return n;
+}
+
 // Whether the cell j may be attended to from position p (j < the cells held is the caller's).
 __device__ __forceinline__ bool tok_seen(int j, int p, int window, int sinks)
 {
     return j <= p && (window == 0 || j > p - window || j < sinks);
 }
 
+// Cells a row of a tree may attend to: of the 32 from j0 on, a bit each (j below the cells held is the caller's).
+struct TreeRow {
+    int pos, first, words;
+    const uint32_t *bits;
+};
+__device__ __forceinline__ TreeRow tree_row(const TokBatch &b, int token)
+{
+    const int4 n = __ldg(reinterpret_cast<const int4 *>(b.node + token));
+    return {n.y + n.x, n.y, n.z, b.bits + (uint32_t)n.w};
+}
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t tree_seen(const TreeRow &t, int j0, int window, int sinks)
+{
+    uint32_t past = bits_below(t.first - j0);
+    if (window) past &= ~bits_below(t.pos - window + 1 - j0) | bits_below(sinks - j0);
+    const int c = j0 - t.first, k = c >> 5;                             // (k < 0: before the first word)
+    const uint32_t lo = k >= 0 && k < t.words ? __ldg(t.bits + k) : 0u, hi = k >= -1 && k + 1 < t.words ? __ldg(t.bits + k + 1) : 0u;
+    return past | __funnelshift_r(lo, hi, c & 31);
+}
+
 // One row of attention by the definition, by a whole warp, over the cells j0 .. j1 - 1: only cells
 // that the row may attend to are read.  q: the row's D values (any memory); the warp's lanes
 // below D / 8 hold eight output sums each in o (not divided), all lanes the maximum m of
 // scale_log2 q k (-inf: no cell) and the sum l of 2^(. - m).
-template <class T, bool E4M3>
+// TREE: p is the position of the row's token, tree what it sees.
+template <class T, bool E4M3, bool TREE = false>
 __device__ __forceinline__ void attend_row(const TokPool &pool, const int32_t *table, int h, const T *q, int qvec, int p,
                                            int j0, int j1, int window, int sinks, float scale_log2, float *o, float &m,
-                                           float &l)
+                                           float &l, TreeRow tree = {})
 {
     const int lane = threadIdx.x & 31, D = pool.d;
     // half of a small scale's power of two goes to q (exactly), so that a sum of products cannot overflow where
@@ -163,16 +209,16 @@ __device__ __forceinline__ void attend_row(const TokPool &pool, const int32_t *t
     l = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = 0.f;
-    j1 = min(j1, p + 1);
+    if (!TREE) j1 = min(j1, p + 1);
     for (int base = j0; base < j1; base += 32) {
-        if (window && base + 31 <= p - window && base >= sinks) {      // wholly before the window
-            const int first = p - window + 1;
+        const int first = TREE ? min(p - window + 1, tree.first) : p - window + 1;
+        if (window && base + 31 < first && base >= sinks) {            // wholly before the window
             base += (first - base) / 32 * 32 - 32;
             if (base + 32 >= j1) break;
             continue;
         }
         const int j = base + lane;
-        const bool see = j < j1 && tok_seen(j, p, window, sinks);
+        const bool see = j < j1 && (TREE ? tree_seen(tree, base, window, sinks) >> lane & 1u : tok_seen(j, p, window, sinks));
         float s = 0.f;
         if (see) {
             const int64_t row = cell_row(pool, table, h, j);

@@ -24,6 +24,7 @@ ACTS = {"none": 0, "relu": 1, "relu6": 2}
 PRECISIONS = {"fp32": 0, "tf32x3": 1, "bf16": 2, "tf32": 3}
 TOKEN_DTYPES = {"f32": 0, "f16": 1, "bf16": 2}
 TOKEN_FORMS = {"same": 0, "e4m3": 1}
+ROTARY_PAIRS = {"halves": 0, "adjacent": 1}
 
 # the exported entry points of include/mure.h
 EXPORTS = ("mure_create", "mure_destroy", "mure_last_error", "mure_model_load", "mure_model_free",
@@ -31,7 +32,9 @@ EXPORTS = ("mure_create", "mure_destroy", "mure_last_error", "mure_model_load", 
            "mure_eval_mutants", "mure_eval_vanilla", "mure_expand_patches", "mure_expand_patches_noalloc",
            "mure_check_descriptors", "mure_set_wait_limit", "mure_tokens_create", "mure_tokens_free",
            "mure_tokens_buffers", "mure_tokens_plan_create", "mure_tokens_plan_set", "mure_tokens_plan_free",
-           "mure_tokens_append", "mure_tokens_read", "mure_tokens_attend", "mure_synchronize")
+           "mure_tokens_plan_create_tree", "mure_tokens_plan_set_tree",
+           "mure_tokens_append", "mure_tokens_read", "mure_tokens_attend", "mure_rotary_create", "mure_rotary_free",
+           "mure_tokens_rotate", "mure_tokens_append_rotated", "mure_tokens_copy_pages", "mure_tokens_keep", "mure_synchronize")
 
 
 class MureError(RuntimeError):
@@ -101,6 +104,12 @@ class _TokensRows(C.Structure):
     _fields_ = [("p", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
+class _RotaryDesc(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("pairs", C.c_int32), ("n_axes", C.c_int32),
+                ("freq", C.c_void_p), ("base", C.c_double), ("axis", C.c_void_p), ("q_weight", C.c_void_p),
+                ("k_weight", C.c_void_p), ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
 _lib = None
 # Allocator thunks stay alive for the life of the process: a context's C object may
 # still call them while Python tears objects down in arbitrary (cyclic-GC) order.
@@ -157,11 +166,20 @@ def lib():
         L.mure_tokens_append.argtypes = [vp, vp, rows, rows]
         L.mure_tokens_read.argtypes = [vp, vp, i32, rows, rows]
         L.mure_tokens_attend.argtypes = [vp, vp, rows, rows, vp]
+        L.mure_tokens_plan_create_tree.argtypes = [vp, C.POINTER(_TokensBatch), vp, C.POINTER(vp)]
+        L.mure_tokens_plan_set_tree.argtypes = [vp, C.POINTER(_TokensBatch), vp]
+        L.mure_rotary_create.argtypes = [vp, C.POINTER(_RotaryDesc), C.POINTER(vp)]
+        L.mure_rotary_free.argtypes = [vp]
+        L.mure_rotary_free.restype = None
+        L.mure_tokens_rotate.argtypes = [vp, vp, vp, vp, i64, rows, rows, rows, rows]
+        L.mure_tokens_append_rotated.argtypes = [vp, vp, vp, vp, i64, rows, rows, rows, rows]
+        L.mure_tokens_copy_pages.argtypes = [vp, vp, i64, vp, vp]
+        L.mure_tokens_keep.argtypes = [vp, vp, vp, vp]
         L.mure_synchronize.argtypes = [vp]
         for name in EXPORTS:
             if name not in ("mure_destroy", "mure_model_free", "mure_cache_free", "mure_last_error",
                             "mure_model_n_layers", "mure_kernel_launches", "mure_tokens_free",
-                            "mure_tokens_plan_free"):
+                            "mure_tokens_plan_free", "mure_rotary_free"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -522,6 +540,24 @@ class TokensPlan:
         self.free()
 
 
+class Rotary:
+    """Tables of a norm and rotation of queries and keys (mure_rotary)."""
+
+    def __init__(self, ctx, handle, head_dim, n_axes):
+        self.ctx, self.h, self.head_dim, self.n_axes = ctx, handle, head_dim, n_axes
+        ctx._children += 1
+
+    def free(self):
+        if getattr(self, "h", None):
+            if not _finalizing():
+                lib().mure_rotary_free(self.h)
+            self.h = None
+            self.ctx._child_gone()
+
+    def __del__(self):
+        self.free()
+
+
 def _torch_dtype(name):
     import torch
     return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[name]
@@ -596,20 +632,32 @@ def _tokens_batch(n_heads, new_len, pos, kv_len, page_table, window, sinks, scal
 
 
 def mure_tokens_plan(tokens: Tokens, n_heads: int, new_len, pos, kv_len, page_table, window: int = 0, sinks: int = 0,
-                     scale: float = 0.0, plan: TokensPlan = None) -> TokensPlan:
+                     scale: float = 0.0, plan: TokensPlan = None, parents=None) -> TokensPlan:
     """Lay out a batch for caches of `tokens`' geometry: sequence b has kv_len[b] cells in the pages
     page_table[b] and new_len[b] new tokens from position pos[b] on.  plan: an existing plan that
-    takes the batch (a decoding loop's next step)."""
+    takes the batch (a decoding loop's next step).  parents: the new tokens are trees; of each new token, one
+    sequence's after the other, the new token of its sequence that it follows, or -1."""
     b, keep = _tokens_batch(n_heads, new_len, pos, kv_len, page_table, window, sinks, scale)
-    ctx = tokens.ctx
+    ctx, n_new = tokens.ctx, int(keep[0].sum(dtype=np.int64))
+    if parents is not None:
+        parents = _int32(parents, "parents").reshape(-1)
+        if len(parents) != n_new:
+            raise ValueError(f"parents: {len(parents)} of {n_new} new tokens")
+        if n_new == 0:
+            parents = np.zeros(1, np.int32)
     if plan is None:
         out = C.c_void_p()
-        ctx.check(lib().mure_tokens_plan_create(tokens.h, C.byref(b), C.byref(out)))
+        if parents is None:
+            ctx.check(lib().mure_tokens_plan_create(tokens.h, C.byref(b), C.byref(out)))
+        else:
+            ctx.check(lib().mure_tokens_plan_create_tree(tokens.h, C.byref(b), _ptr(parents), C.byref(out)))
         plan = TokensPlan(ctx, out.value, int(n_heads))
-    else:
+    elif parents is None:
         ctx.check(lib().mure_tokens_plan_set(plan.h, C.byref(b)))
-    plan.n_heads = int(n_heads)
-    plan.n_new, plan.n_cells = int(keep[0].sum(dtype=np.int64)), int(keep[2].sum(dtype=np.int64))
+    else:
+        ctx.check(lib().mure_tokens_plan_set_tree(plan.h, C.byref(b), _ptr(parents)))
+    plan.n_heads, plan.n_seqs = int(n_heads), int(b.n_seqs)
+    plan.n_new, plan.n_cells = n_new, int(keep[2].sum(dtype=np.int64))
     return plan
 
 
@@ -706,6 +754,113 @@ def mure_tokens_attend(tokens: Tokens, plan: TokensPlan, q, out=None, lse: bool 
     ctx.check(lib().mure_tokens_attend(tokens.h, plan.h, qr, orow, ls.data_ptr() if lse else None))
     _leave(st)
     return (out, ls) if lse else out
+
+
+def mure_rotary_create(ctx: Context, head_dim: int, rot_dim: int = None, layout: str = "halves", freq=None, base: float = 10000.0,
+                       axis=None, n_axes: int = 1, q_weight=None, k_weight=None, eps: float = 1e-6) -> Rotary:
+    """Norm and rotation of queries and keys.  rot_dim: how many of a head's values are rotated, its first ones (default: all);
+    layout: "halves" (pairs i, i + rot_dim / 2) or "adjacent" (2 i, 2 i + 1); freq: radians per position of each pair
+    (default: base^(-2 i / rot_dim)); axis: each pair's axis of positions; q_weight, k_weight: host arrays of
+    head_dim weights (None: no norm)."""
+    rot_dim = head_dim if rot_dim is None else rot_dim
+    half = max(int(rot_dim), 0) // 2
+
+    def host(a, dtype, n, name):
+        if a is None:
+            return None
+        a = np.asarray(a)
+        if dtype is np.uint8 and a.size and not ((a >= 0) & (a < 256) & (a == np.floor(a))).all():
+            raise ValueError(f"{name}: whole numbers from 0 on are wanted")
+        a = np.ascontiguousarray(a, dtype).reshape(-1)
+        if len(a) != n:
+            raise ValueError(f"{name}: {n} numbers are wanted, got {len(a)}")
+        return a if n else np.zeros(1, dtype)
+    keep = (host(freq, np.float64, half, "freq"), host(axis, np.uint8, half, "axis"),
+            host(q_weight, np.float32, int(head_dim), "q_weight"), host(k_weight, np.float32, int(head_dim), "k_weight"))
+    d = _RotaryDesc(_whole(head_dim, "head_dim"), _whole(rot_dim, "rot_dim"), ROTARY_PAIRS[layout], _whole(n_axes, "n_axes"),
+                    _ptr(keep[0]), float(base), _ptr(keep[1]), _ptr(keep[2]), _ptr(keep[3]), float(eps), 0)
+    out = C.c_void_p()
+    ctx.check(lib().mure_rotary_create(ctx.h, C.byref(d), C.byref(out)))
+    return Rotary(ctx, out.value, int(head_dim), int(n_axes))
+
+
+def _positions(positions, tokens, plan, rotary):
+    """(address, stride, tensor) of the new tokens' positions [n_axes][tokens] (one axis: [tokens] will do)."""
+    import torch
+    if positions is None:
+        return None, 0
+    if positions.dtype is not torch.int32 or positions.device != tokens.torch_device:
+        raise ValueError(f"positions: an int32 tensor on {tokens.torch_device} is wanted")
+    if positions.dim() == 1 and rotary.n_axes == 1:
+        positions = positions[None]
+    if positions.shape != (rotary.n_axes, plan.n_new):
+        raise ValueError(f"positions: shape {(rotary.n_axes, plan.n_new)} is wanted, got {tuple(positions.shape)}")
+    step = positions.stride(0) if rotary.n_axes > 1 else plan.n_new
+    if plan.n_new and (plan.n_new > 1 and positions.stride(1) != 1 or step < plan.n_new):
+        raise ValueError(f"positions: a dense last dimension and rows apart are wanted, got strides {positions.stride()}")
+    return positions.data_ptr(), max(step, plan.n_new)
+
+
+def mure_tokens_rotate(tokens: Tokens, plan: TokensPlan, rotary: Rotary, q=None, k=None, positions=None, out=None):
+    """(q, k) of the batch's new tokens, q [tokens][n_heads][head_dim] and k [tokens][n_kv_heads][head_dim], normed and
+    rotated; either may be None.  positions: int32 [n_axes][tokens] on the device (default: the plan's own).  out:
+    (q, k) to write to, the inputs themselves for example."""
+    import torch
+    n = plan.n_new
+    heads = (plan.n_heads, tokens.n_kv_heads)
+    if out is None:
+        out = tuple(None if x is None else torch.empty((n, h, tokens.head_dim), dtype=tokens.torch_dtype, device=tokens.torch_device)
+                    for x, h in zip((q, k), heads))
+    if (q is None) != (out[0] is None) or (k is None) != (out[1] is None):
+        raise ValueError("out: a tensor for each of q and k that is given, and None for the others")
+    at, step = _positions(positions, tokens, plan, rotary)
+    rows = [None if x is None else _token_rows(x, tokens, n, h, name)
+            for x, h, name in ((q, heads[0], "q"), (k, heads[1], "k"), (out[0], heads[0], "out[0]"), (out[1], heads[1], "out[1]"))]
+    st = _enter(tokens.ctx, (q, k, positions, *out))
+    tokens.ctx.check(lib().mure_tokens_rotate(tokens.h, plan.h, rotary.h, at, step, *rows))
+    _leave(st)
+    return out
+
+
+def mure_tokens_append_rotated(tokens: Tokens, plan: TokensPlan, rotary: Rotary, q, k, v, positions=None, out=None):
+    """mure_tokens_rotate and mure_tokens_append in one pass: the new tokens' queries normed and rotated (returned; None
+    for q None), their keys as rotated and their values written into their cells."""
+    import torch
+    n = plan.n_new
+    if out is None and q is not None:
+        out = torch.empty((n, plan.n_heads, tokens.head_dim), dtype=tokens.torch_dtype, device=tokens.torch_device)
+    if (q is None) != (out is None):
+        raise ValueError("out: a tensor where q is given")
+    at, step = _positions(positions, tokens, plan, rotary)
+    rows = [None if x is None else _token_rows(x, tokens, n, h, name)
+            for x, h, name in ((q, plan.n_heads, "q"), (k, tokens.n_kv_heads, "k"), (v, tokens.n_kv_heads, "v"), (out, plan.n_heads, "out"))]
+    st = _enter(tokens.ctx, (q, k, v, positions, out))
+    tokens.ctx.check(lib().mure_tokens_append_rotated(tokens.h, plan.h, rotary.h, at, step, *rows))
+    _leave(st)
+    return out
+
+
+def mure_tokens_copy_pages(tokens: Tokens, from_pages, to_pages, source: Tokens = None) -> None:
+    """Copy page from_pages[i] of `source` (default: of `tokens` itself) to page to_pages[i] of `tokens`."""
+    a, b = _int32(from_pages, "from_pages").reshape(-1), _int32(to_pages, "to_pages").reshape(-1)
+    if len(a) != len(b):
+        raise ValueError("from_pages and to_pages have different lengths")
+    source = tokens if source is None else source
+    st = _enter(tokens.ctx, ())
+    tokens.ctx.check(lib().mure_tokens_copy_pages(tokens.h, source.h, len(a), _ptr(a), _ptr(b)))
+    _leave(st)
+
+
+def mure_tokens_keep(tokens: Tokens, plan: TokensPlan, kept) -> None:
+    """Keep some of the batch's new tokens: kept[b] are the ascending indexes of sequence b's, whose cells move up to
+    follow its earlier ones."""
+    if len(kept) != plan.n_seqs:
+        raise ValueError(f"kept: {len(kept)} lists of {plan.n_seqs} sequences")
+    count = np.array([len(x) for x in kept], np.int32)
+    index = _int32([i for x in kept for i in x], "kept")
+    st = _enter(tokens.ctx, ())
+    tokens.ctx.check(lib().mure_tokens_keep(tokens.h, plan.h, _ptr(count), _ptr(index)))
+    _leave(st)
 
 
 def mure_synchronize(ctx: Context) -> None:
