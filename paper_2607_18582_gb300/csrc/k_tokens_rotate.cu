@@ -6,11 +6,14 @@
 // with u the position along the pair's axis times the pair's frequency.  The angle is held as a part of a turn in
 // 64-bit fixed point: the position times (frequency / 2 pi) 2^64, modulo 2^64, is exact to position 2^-64 turns, so
 // a token at position 2^30 is rotated as well as one at 5, and only the remainder goes to sine and cosine in fp32.
-// A block takes a tile of up to 16 tokens of one sequence, computes its sines and cosines once into shared memory
-// and all heads' rows from them.  A row lies with a power-of-two group of a warp, eight values a thread: with pairs
-// of halves four from either half, so that a pair never leaves its thread, the row's sum of squares is a few shuffles
-// away, and an e4m3 row is quantised in the pass that rotated it.  Everything is fp32 up to one rounding to the
-// activations' type; codes are made from that rounding, so that both ways to a cell store the same bits.
+// A row lies with a power-of-two group of a warp, eight values a thread: with pairs of halves four from either half, so
+// that a pair never leaves its thread, the row's sum of squares is a few shuffles away, and an e4m3 row is quantised in
+// the pass that rotated it.  A group takes a token and some or all of its heads: its sines and cosines, times the
+// weights, stay in registers from head to head.  A block takes a tile of up to 16 tokens of one sequence.
+// Everything is fp32 up to one rounding to the activations' type; codes are made from that rounding, so that both ways to
+// a cell store the same bits.
+#include <type_traits>
+
 #include "tokens_util.cuh"
 
 namespace mure {
@@ -19,228 +22,247 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kRows = 4;         // rows that a thread has on their way
+constexpr int kBlocks = 16;      // blocks per SM that a launch has at least, where it has the rows
 
 struct RotateParams {
     TokPool pool;
     TokBatch b;
     TokRotary r;
     TokRows q, k, v, q_out, k_out;
-    int q_heads, k_heads, rows;  // of a token: its query, key and (into cells) value rows
+    int q_heads, k_heads;
     int lanes;                   // threads per row
 };
 
 enum { kToRows = 0, kToCells = 1, kToCodes = 2 };
 
-// Four values as they lie in memory, and in fp32.
-template <class T> struct Quad;
-template <> struct Quad<float> {
-    uint4 w;
+// A thread's eight values of a row as they lie in memory: two runs of four, or (ONE) one of eight.
+template <class T, bool ONE>
+struct Eight {
+    static constexpr int kWords = sizeof(T) * 2;                     // 32-bit words
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T *p, int second, int vec)
+    {
+        if (vec) {
+            if (ONE) {
+#pragma unroll
+                for (int i = 0; i < kWords / 4; ++i)
+                    reinterpret_cast<uint4 *>(w)[i] = reinterpret_cast<const uint4 *>(p)[i];
+            } else if (sizeof(T) == 4) {
+                reinterpret_cast<uint4 *>(w)[0] = *reinterpret_cast<const uint4 *>(p);
+                reinterpret_cast<uint4 *>(w)[kWords / 4 - 1] = *reinterpret_cast<const uint4 *>(p + second);
+            } else {
+                reinterpret_cast<uint2 *>(w)[0] = *reinterpret_cast<const uint2 *>(p);
+                reinterpret_cast<uint2 *>(w)[1] = *reinterpret_cast<const uint2 *>(p + second);
+            }
+        } else {
+            T *t = reinterpret_cast<T *>(w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = p[i < 4 ? i : second + i - 4];
+        }
+    }
+    __device__ __forceinline__ void store(T *p, int second, int vec) const
+    {
+        if (vec) {
+            if (ONE) {
+#pragma unroll
+                for (int i = 0; i < kWords / 4; ++i)
+                    reinterpret_cast<uint4 *>(p)[i] = reinterpret_cast<const uint4 *>(w)[i];
+            } else if (sizeof(T) == 4) {
+                *reinterpret_cast<uint4 *>(p) = reinterpret_cast<const uint4 *>(w)[0];
+                *reinterpret_cast<uint4 *>(p + second) = reinterpret_cast<const uint4 *>(w)[kWords / 4 - 1];
+            } else {
+                *reinterpret_cast<uint2 *>(p) = reinterpret_cast<const uint2 *>(w)[0];
+                *reinterpret_cast<uint2 *>(p + second) = reinterpret_cast<const uint2 *>(w)[1];
+            }
+        } else {
+            const T *t = reinterpret_cast<const T *>(w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i < 4 ? i : second + i - 4] = t[i];
+        }
+    }
     __device__ __forceinline__ void up(float *x) const
     {
-        x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+        const T *t = reinterpret_cast<const T *>(w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = TokType<T>::up(t[i]);
     }
     __device__ __forceinline__ void down(const float *x)
     {
-        w = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-    }
-    __device__ __forceinline__ void load(const float *p, int vec)
-    {
-        if (vec) w = *reinterpret_cast<const uint4 *>(p);
-        else down(p);
-    }
-    __device__ __forceinline__ void store(float *p, int vec) const
-    {
-        if (vec) *reinterpret_cast<uint4 *>(p) = w;
-        else up(p);
-    }
-};
-template <class T> struct Quad {
-    uint2 w;
-    __device__ __forceinline__ void up(float *x) const
-    {
-        const T *t = reinterpret_cast<const T *>(&w);
+        T *t = reinterpret_cast<T *>(w);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = TokType<T>::up(t[i]);
+        for (int i = 0; i < 8; ++i) t[i] = TokType<T>::down(x[i]);
     }
-    __device__ __forceinline__ void down(const float *x)
+    // the bits of the largest magnitude, as fp32
+    __device__ __forceinline__ uint32_t most() const
     {
-        T *t = reinterpret_cast<T *>(&w);
+        uint32_t a = 0;
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t[i] = TokType<T>::down(x[i]);
-    }
-    __device__ __forceinline__ void load(const T *p, int vec)
-    {
-        if (vec) w = *reinterpret_cast<const uint2 *>(p);
-        else {
-            T *t = reinterpret_cast<T *>(&w);
+            for (int i = 0; i < kWords; ++i) a = __vmaxu2(a, w[i] & 0x7FFF7FFFu);
+            return max(a & 0xFFFFu, a >> 16);
+        } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) t[i] = p[i];
+            for (int i = 0; i < kWords; ++i) a = max(a, w[i] & 0x7FFFFFFFu);
+            return a;
         }
     }
-    __device__ __forceinline__ void store(T *p, int vec) const
+    static __device__ __forceinline__ uint32_t bits_up(uint32_t a)
     {
-        if (vec) *reinterpret_cast<uint2 *>(p) = w;
-        else {
-            const T *t = reinterpret_cast<const T *>(&w);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = t[i];
-        }
+        if constexpr (sizeof(T) == 4) return a;
+        const uint16_t h = (uint16_t)a;
+        return __float_as_uint(TokType<T>::up(*reinterpret_cast<const T *>(&h)));
     }
 };
 
 template <class T, int TO, bool ADJ>
-__global__ void __launch_bounds__(kThreads) k_tokens_rotate(RotateParams p)
+__global__ void __launch_bounds__(kThreads, 5) k_tokens_rotate(RotateParams p)
 {
-    extern __shared__ __align__(16) float shared[];
+    using X = Eight<T, ADJ>;
     TokSeq sq;
     const Tile t = tile_of(p.b, false, sq);
-    const int D = p.pool.d, half = p.r.rot / 2;
-    float *cosine = shared, *sine = shared + kTokTile * half, *weight = shared + 2 * kTokTile * half;
-    for (int u = threadIdx.x; u < t.n * half; u += kThreads) {
-        const int i = u / half, k = u - i * half;
-        const int64_t token = sq.row0 + t.i0 + i;
-        const int at = p.r.positions ? __ldg(p.r.positions + __ldg(p.r.axis + k) * p.r.position_stride + token)
-                                     : sq.pos + (p.b.node ? __ldg(&p.b.node[token].depth) : t.i0 + i);
-        const uint64_t turn = (uint64_t)(int64_t)at * __ldg(p.r.turn + k);
-        // to the nearest 2^-32 of a turn, in -1/2 .. 1/2
-        const float part = (float)(int32_t)(uint32_t)((turn + 0x80000000ull) >> 32) * 0x1p-31f;
-        sincospif(part, sine + u, cosine + u);
-    }
-    for (int u = threadIdx.x; u < 2 * D; u += kThreads) weight[u] = __ldg(p.r.weight + u);
-    __syncthreads();
-
-    const int slot = threadIdx.x & (p.lanes - 1), per = kThreads / p.lanes;
+    const int D = p.pool.d, slot = threadIdx.x & (p.lanes - 1), group = threadIdx.x / p.lanes, groups = kThreads / p.lanes;
     const bool in = slot * 8 < D, turned = slot * 8 < p.r.rot;
     // this thread's values of a row: two runs of four; with pairs of halves the rotated ones lie half a rotation apart
-    const int ia = !ADJ && turned ? slot * 4 : slot * 8, ib = !ADJ && turned ? half + slot * 4 : slot * 8 + 4;
-    const int all = t.n * p.rows, step = per * gridDim.y, step_i = step / p.rows, step_h = step - step_i * p.rows;
-    const int32_t *table = p.b.table + sq.table0;
-    int r = blockIdx.y * per + threadIdx.x / p.lanes;
-    int i = r / p.rows, h = r - i * p.rows;
+    const int half = p.r.rot / 2, at = !ADJ && turned ? slot * 4 : slot * 8, second = !ADJ && turned ? half : 4;
     const float over = 1.f / D;
-    for (int base = blockIdx.y * per; base < all; base += step * kRows) {
-        Quad<T> a[kRows], b[kRows];
-        int ri[kRows], rh[kRows];
+    // the block's groups over the tile's tokens: of fewer tokens than groups each has several, which share its heads
+    const int share = t.n < groups ? groups / t.n : 1;
+    const int parts = share * gridDim.y, part = blockIdx.y * share + group % share;
+    const int32_t *table = p.b.table + sq.table0;
+
+    for (int i0 = 0; i0 < t.n; i0 += groups / share) {
+        const int i = i0 + group / share;
+        const bool here = in && i < t.n;
+        const int64_t token = sq.row0 + t.i0 + i;
+        float cosine[4] = {1.f, 1.f, 1.f, 1.f}, sine[4] = {0.f, 0.f, 0.f, 0.f};
+        if (here && turned) {
+            const int own = p.r.positions ? 0 : sq.pos + (p.b.node ? __ldg(&p.b.node[token].depth) : t.i0 + i);
 #pragma unroll
-        for (int u = 0; u < kRows; ++u) {
-            ri[u] = r < all && in ? i : -1;
-            rh[u] = h;
-            a[u] = b[u] = Quad<T>{};
-            if (ri[u] >= 0) {
-                const TokRows &from = h < p.q_heads ? p.q : h < p.q_heads + p.k_heads ? p.k : p.v;
-                const int head = h < p.q_heads ? h : h < p.q_heads + p.k_heads ? h - p.q_heads : h - p.q_heads - p.k_heads;
-                const T *x = reinterpret_cast<const T *>(from.p) + (int64_t)(sq.row0 + t.i0 + i) * from.ts + head * from.hs;
-                a[u].load(x + ia, from.vec);
-                b[u].load(x + ib, from.vec);
-            }
-            r += step;
-            i += step_i;
-            h += step_h;
-            if (h >= p.rows) { h -= p.rows; ++i; }
-        }
-#pragma unroll
-        for (int u = 0; u < kRows; ++u) {
-            if (base + u * step >= all) break;                       // (for all threads alike)
-            const bool on = ri[u] >= 0, is_q = rh[u] < p.q_heads, is_v = TO != kToRows && rh[u] >= p.q_heads + p.k_heads;
-            float y[8];
-            a[u].up(y);
-            b[u].up(y + 4);
-            if (p.r.norm_q || p.r.norm_k) {
-                float sum = 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum = fmaf(y[e], y[e], sum);
-                for (int x = p.lanes >> 1; x; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-                float f = rsqrtf(fmaf(sum, over, p.r.eps));
-                // squares that leave fp32's range: once more, of the values times a power of two
-                const bool lost = !(sum >= 0x1p-80f && sum < INFINITY);
-                if (__any_sync(0xffffffffu, lost)) {
-                    const float g = sum < 1.f ? 0x1p60f : 0x1p-70f;
-                    float again = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) again = fmaf(y[e] * g, y[e] * g, again);
-                    for (int x = p.lanes >> 1; x; x >>= 1) again += __shfl_xor_sync(0xffffffffu, again, x);
-                    if (lost) f = rsqrtf(fmaf(again, over, p.r.eps * g * g)) * g;
-                }
-                if (is_q ? p.r.norm_q : !is_v && p.r.norm_k) {
-                    const float4 wa = *reinterpret_cast<const float4 *>(weight + (is_q ? 0 : D) + (in ? ia : 0));
-                    const float4 wb = *reinterpret_cast<const float4 *>(weight + (is_q ? 0 : D) + (in ? ib : 0));
-                    y[0] *= f * wa.x; y[1] *= f * wa.y; y[2] *= f * wa.z; y[3] *= f * wa.w;
-                    y[4] *= f * wb.x; y[5] *= f * wb.y; y[6] *= f * wb.z; y[7] *= f * wb.w;
-                }
-            }
-            if (turned && !is_v && on) {
-                const float4 c = *reinterpret_cast<const float4 *>(cosine + ri[u] * half + slot * 4);
-                const float4 s = *reinterpret_cast<const float4 *>(sine + ri[u] * half + slot * 4);
-                auto pair = [&](float &x0, float &x1, float cu, float su) {
-                    const float t0 = fmaf(x0, cu, -x1 * su), t1 = fmaf(x1, cu, x0 * su);
-                    x0 = t0;
-                    x1 = t1;
-                };
-                if (ADJ) {
-                    pair(y[0], y[1], c.x, s.x); pair(y[2], y[3], c.y, s.y);
-                    pair(y[4], y[5], c.z, s.z); pair(y[6], y[7], c.w, s.w);
-                } else {
-                    pair(y[0], y[4], c.x, s.x); pair(y[1], y[5], c.y, s.y);
-                    pair(y[2], y[6], c.z, s.z); pair(y[3], y[7], c.w, s.w);
-                }
-            }
-            if (!is_v) {                                             // the one rounding to the activations' type
-                a[u].down(y);
-                b[u].down(y + 4);
-            }
-            const int token = sq.row0 + t.i0 + ri[u];
-            if (TO == kToRows || is_q) {
-                if (on) {
-                    const TokRows &to = is_q ? p.q_out : p.k_out;
-                    T *o = reinterpret_cast<T *>(to.p) + (int64_t)token * to.ts + (is_q ? rh[u] : rh[u] - p.q_heads) * to.hs;
-                    a[u].store(o + ia, to.vec);
-                    b[u].store(o + ib, to.vec);
-                }
-            }
-            if (TO == kToRows) continue;
-            const int head = rh[u] - p.q_heads - (is_v ? p.k_heads : 0);
-            void *pool = is_v ? p.pool.v : p.pool.k;
-            if (TO == kToCells) {
-                if (on && !is_q) {
-                    T *o = static_cast<T *>(pool) + cell_row(p.pool, table, head, sq.pos + t.i0 + ri[u]) * D;
-                    a[u].store(o + ia, 1);
-                    b[u].store(o + ib, 1);
-                }
-            } else if (__any_sync(0xffffffffu, on && !is_q)) {
-                uint32_t most = 0;
-                a[u].up(y);
-                b[u].up(y + 4);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(y[e]) & 0x7FFFFFFFu);
-                for (int x = p.lanes >> 1; x; x >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, x));
-                const uint32_t byte = scale_byte(most);
-                if (on && !is_q) {
-                    const int64_t row = cell_row(p.pool, table, head, sq.pos + t.i0 + ri[u]);
-                    uint32_t w[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        w[e] = byte == 255u ? 0u
-                                            : e4m3_pair(unscale(y[4 * e], byte), unscale(y[4 * e + 1], byte)) |
-                                                  e4m3_pair(unscale(y[4 * e + 2], byte), unscale(y[4 * e + 3], byte)) << 16;
-                    uint8_t *o = static_cast<uint8_t *>(pool) + row * D;
-                    *reinterpret_cast<uint32_t *>(o + ia) = w[0];
-                    *reinterpret_cast<uint32_t *>(o + ib) = w[1];
-                    if (slot == 0) (is_v ? p.pool.vs : p.pool.ks)[row] = (uint8_t)byte;
-                }
+            for (int e = 0; e < 4; ++e) {
+                const int k = slot * 4 + e;
+                const int pos = p.r.positions ? __ldg(p.r.positions + __ldg(p.r.axis + k) * p.r.position_stride + token) : own;
+                const uint64_t turn = (uint64_t)(int64_t)pos * __ldg(p.r.turn + k);
+                // to the nearest 2^-32 of a turn, in -1/2 .. 1/2
+                const float u = (float)(int32_t)(uint32_t)((turn + 0x80000000ull) >> 32) * 0x1p-31f;
+                sincospif(u, sine + e, cosine + e);
             }
         }
+        // KIND 0: queries, 1: keys, 2: values
+        auto rows = [&](auto kind, const TokRows &from, const TokRows &to, int heads) {
+            constexpr int KIND = decltype(kind)::value;
+            constexpr bool kCells = KIND > 0 && TO != kToRows, kCodes = KIND > 0 && TO == kToCodes;
+            const bool norm = KIND == 0 ? p.r.norm_q : KIND == 1 && p.r.norm_k;
+            // x -> (a cw - b sw', b cw' + a sw): each pair's cosine and sine times its weights
+            float w[8], ca[4], sb[4], cb[4], sa[4];
+            if (KIND < 2) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    w[e] = norm && here ? __ldg(p.r.weight + (KIND == 0 ? 0 : D) + at + (e < 4 ? e : second + e - 4)) : 1.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float wa = w[ADJ ? 2 * e : e], wb = w[ADJ ? 2 * e + 1 : e + 4];
+                    ca[e] = cosine[e] * wa; sa[e] = sine[e] * wa;
+                    cb[e] = cosine[e] * wb; sb[e] = sine[e] * wb;
+                }
+            }
+            const T *src = reinterpret_cast<const T *>(from.p) + token * from.ts + at;
+            T *dst = kCells ? nullptr : reinterpret_cast<T *>(to.p) + token * to.ts + at;
+            for (int h0 = part; h0 - part < heads; h0 += parts * kRows) {
+                X x[kRows];
+#pragma unroll
+                for (int u = 0; u < kRows; ++u) {
+                    const int h = h0 + u * parts;
+#pragma unroll
+                    for (int e = 0; e < X::kWords; ++e) x[u].w[e] = 0u;
+                    if (here && h < heads) x[u].load(src + h * from.hs, second, from.vec);
+                }
+#pragma unroll
+                for (int u = 0; u < kRows; ++u) {
+                    const int h = h0 + u * parts;
+                    if (h - part >= heads) break;                    // (for all threads alike)
+                    const bool on = here && h < heads;
+                    float y[8];
+                    if (KIND < 2) {
+                        x[u].up(y);
+                        float f = 1.f;
+                        if (norm) {
+                            float sum = 0.f;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) sum = fmaf(y[e], y[e], sum);
+                            for (int s = p.lanes >> 1; s; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+                            f = rsqrtf(fmaf(sum, over, p.r.eps));
+                            // squares that leave fp32's range: once more, of the values times a power of two
+                            const bool lost = on && !(sum >= 0x1p-80f && sum < INFINITY);
+                            if (__any_sync(0xffffffffu, lost)) {
+                                const float g = sum < 1.f ? 0x1p60f : 0x1p-70f;
+                                float again = 0.f;
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) again = fmaf(y[e] * g, y[e] * g, again);
+                                for (int s = p.lanes >> 1; s; s >>= 1) again += __shfl_xor_sync(0xffffffffu, again, s);
+                                if (lost) f = rsqrtf(fmaf(again, over, p.r.eps * g * g)) * g;
+                            }
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) y[e] *= f;
+                        }
+                        if (turned) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                float &a = y[ADJ ? 2 * e : e], &b = y[ADJ ? 2 * e + 1 : e + 4];
+                                const float t0 = fmaf(a, ca[e], -b * sb[e]), t1 = fmaf(b, cb[e], a * sa[e]);
+                                a = t0;
+                                b = t1;
+                            }
+                        } else if (norm) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) y[e] *= w[e];
+                        }
+                        x[u].down(y);                                // the one rounding to the activations' type
+                    }
+                    if (!kCells) {
+                        if (on) x[u].store(dst + h * to.hs, second, to.vec);
+                    } else {
+                        void *pool = KIND == 2 ? p.pool.v : p.pool.k;
+                        const int64_t row = on ? cell_row(p.pool, table, h, sq.pos + t.i0 + i) : 0;
+                        if (!kCodes) {
+                            if (on) x[u].store(static_cast<T *>(pool) + row * D + at, second, 1);
+                        } else {
+                            uint32_t most = x[u].most();
+                            for (int s = p.lanes >> 1; s; s >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, s));
+                            const uint32_t byte = scale_byte(X::bits_up(most));
+                            if (on) {
+                                x[u].up(y);
+                                uint32_t c[2];
+#pragma unroll
+                                for (int e = 0; e < 2; ++e)
+                                    c[e] = byte == 255u ? 0u
+                                                        : e4m3_pair(unscale(y[4 * e], byte), unscale(y[4 * e + 1], byte)) |
+                                                              e4m3_pair(unscale(y[4 * e + 2], byte), unscale(y[4 * e + 3], byte)) << 16;
+                                uint8_t *o = static_cast<uint8_t *>(pool) + row * D + at;
+                                if (ADJ) *reinterpret_cast<uint2 *>(o) = make_uint2(c[0], c[1]);
+                                else {
+                                    *reinterpret_cast<uint32_t *>(o) = c[0];
+                                    *reinterpret_cast<uint32_t *>(o + second) = c[1];
+                                }
+                                if (slot == 0) (KIND == 2 ? p.pool.vs : p.pool.ks)[row] = (uint8_t)byte;
+                            }
+                        }
+                    }
+                }
+            }
+        };
+        rows(std::integral_constant<int, 0>{}, p.q, p.q_out, p.q_heads);
+        rows(std::integral_constant<int, 1>{}, p.k, p.k_out, p.k_heads);
+        if (TO != kToRows) rows(std::integral_constant<int, 2>{}, p.v, p.v, p.k_heads);
     }
 }
 
 template <class T, int TO, bool ADJ>
 int go(const RotateParams &p, int64_t tiles, cudaStream_t s)
 {
-    // where tiles are few, several blocks share one: down to one step of rows each
-    const int per = kThreads / p.lanes, most = (p.rows + per - 1) / per;
-    const int64_t want = (4 * (int64_t)sm_count() + tiles - 1) / tiles;
-    const unsigned y = (unsigned)(want < most ? want : most);
-    const size_t bytes = ((size_t)kTokTile * p.r.rot + 2 * p.pool.d) * sizeof(float);
-    k_tokens_rotate<T, TO, ADJ><<<dim3((unsigned)tiles, y), kThreads, bytes, s>>>(p);
+    // several blocks share a tile until there are enough of them, down to one row of queries each
+    const int groups = kThreads / p.lanes, heads = p.q_heads > p.k_heads ? p.q_heads : p.k_heads;
+    const int64_t want = (kBlocks * (int64_t)sm_count() + tiles - 1) / tiles, most = (heads + groups - 1) / groups;
+    k_tokens_rotate<T, TO, ADJ><<<dim3((unsigned)tiles, (unsigned)(want < most ? want : most)), kThreads, 0, s>>>(p);
     return 1;
 }
 
@@ -258,9 +280,8 @@ int by_target(const RotateParams &p, int to, int64_t tiles, cudaStream_t s)
 int launch_tokens_rotate(const TokPool &pool, const TokBatch &b, const TokRotary &r, int dtype, int form, bool cells, int q_heads,
                          int k_heads, TokRows q, TokRows k, TokRows v, TokRows q_out, TokRows k_out, int64_t tiles, cudaStream_t s)
 {
-    const int rows = q_heads + k_heads * (cells ? 2 : 1);
-    if (tiles == 0 || rows == 0) return 0;
-    const RotateParams p{pool, b, r, q, k, v, q_out, k_out, q_heads, k_heads, rows, row_lanes(pool.d)};
+    if (tiles == 0 || q_heads + k_heads == 0) return 0;
+    const RotateParams p{pool, b, r, q, k, v, q_out, k_out, q_heads, k_heads, row_lanes(pool.d)};
     const int to = !cells ? kToRows : form == MURE_FORM_E4M3 ? kToCodes : kToCells;
     if (dtype == MURE_F32) return by_target<float>(p, to, tiles, s);
     if (dtype == MURE_F16) return by_target<__half>(p, to, tiles, s);

@@ -7,6 +7,7 @@ the library has not been built, every call raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 import sys
@@ -707,6 +708,13 @@ def _token_rows(t, tokens, n, heads, name):
     return _TokensRows(t.data_ptr(), s[0], s[1])
 
 
+def _new_rows(tokens, n, heads):
+    """A dense output and its rows."""
+    import torch
+    out = torch.empty((n, heads, tokens.head_dim), dtype=tokens.torch_dtype, device=tokens.torch_device)
+    return out, _TokensRows(out.data_ptr(), heads * tokens.head_dim, tokens.head_dim)
+
+
 def mure_tokens_append(tokens: Tokens, plan: TokensPlan, k, v) -> None:
     """Write the batch's new tokens' keys and values [tokens][n_kv_heads][head_dim] (any token and head
     strides) into their cells."""
@@ -805,19 +813,21 @@ def mure_tokens_rotate(tokens: Tokens, plan: TokensPlan, rotary: Rotary, q=None,
     """(q, k) of the batch's new tokens, q [tokens][n_heads][head_dim] and k [tokens][n_kv_heads][head_dim], normed and
     rotated; either may be None.  positions: int32 [n_axes][tokens] on the device (default: the plan's own).  out:
     (q, k) to write to, the inputs themselves for example."""
-    import torch
-    n = plan.n_new
-    heads = (plan.n_heads, tokens.n_kv_heads)
-    if out is None:
-        out = tuple(None if x is None else torch.empty((n, h, tokens.head_dim), dtype=tokens.torch_dtype, device=tokens.torch_device)
-                    for x, h in zip((q, k), heads))
-    if (q is None) != (out[0] is None) or (k is None) != (out[1] is None):
-        raise ValueError("out: a tensor for each of q and k that is given, and None for the others")
+    heads, kv = plan.n_heads, tokens.n_kv_heads
     at, step = _positions(positions, tokens, plan, rotary)
-    rows = [None if x is None else _token_rows(x, tokens, n, h, name)
-            for x, h, name in ((q, heads[0], "q"), (k, heads[1], "k"), (out[0], heads[0], "out[0]"), (out[1], heads[1], "out[1]"))]
+    qr = None if q is None else _token_rows(q, tokens, plan.n_new, heads, "q")
+    kr = None if k is None else _token_rows(k, tokens, plan.n_new, kv, "k")
+    if out is None:
+        qo, qor = (None, None) if q is None else _new_rows(tokens, plan.n_new, heads)
+        ko, kor = (None, None) if k is None else _new_rows(tokens, plan.n_new, kv)
+        out = (qo, ko)
+    else:
+        if (q is None) != (out[0] is None) or (k is None) != (out[1] is None):
+            raise ValueError("out: a tensor for each of q and k that is given, and None for the others")
+        qor = None if q is None else _token_rows(out[0], tokens, plan.n_new, heads, "out[0]")
+        kor = None if k is None else _token_rows(out[1], tokens, plan.n_new, kv, "out[1]")
     st = _enter(tokens.ctx, (q, k, positions, *out))
-    tokens.ctx.check(lib().mure_tokens_rotate(tokens.h, plan.h, rotary.h, at, step, *rows))
+    tokens.ctx.check(lib().mure_tokens_rotate(tokens.h, plan.h, rotary.h, at, step, qr, kr, qor, kor))
     _leave(st)
     return out
 
@@ -825,17 +835,20 @@ def mure_tokens_rotate(tokens: Tokens, plan: TokensPlan, rotary: Rotary, q=None,
 def mure_tokens_append_rotated(tokens: Tokens, plan: TokensPlan, rotary: Rotary, q, k, v, positions=None, out=None):
     """mure_tokens_rotate and mure_tokens_append in one pass: the new tokens' queries normed and rotated (returned; None
     for q None), their keys as rotated and their values written into their cells."""
-    import torch
-    n = plan.n_new
-    if out is None and q is not None:
-        out = torch.empty((n, plan.n_heads, tokens.head_dim), dtype=tokens.torch_dtype, device=tokens.torch_device)
-    if (q is None) != (out is None):
-        raise ValueError("out: a tensor where q is given")
+    kv = tokens.n_kv_heads
     at, step = _positions(positions, tokens, plan, rotary)
-    rows = [None if x is None else _token_rows(x, tokens, n, h, name)
-            for x, h, name in ((q, plan.n_heads, "q"), (k, tokens.n_kv_heads, "k"), (v, tokens.n_kv_heads, "v"), (out, plan.n_heads, "out"))]
+    kr, vr = _token_rows(k, tokens, plan.n_new, kv, "k"), _token_rows(v, tokens, plan.n_new, kv, "v")
+    qr = qor = None
+    if q is not None:
+        qr = _token_rows(q, tokens, plan.n_new, plan.n_heads, "q")
+        if out is None:
+            out, qor = _new_rows(tokens, plan.n_new, plan.n_heads)
+        else:
+            qor = _token_rows(out, tokens, plan.n_new, plan.n_heads, "out")
+    elif out is not None:
+        raise ValueError("out without q")
     st = _enter(tokens.ctx, (q, k, v, positions, out))
-    tokens.ctx.check(lib().mure_tokens_append_rotated(tokens.h, plan.h, rotary.h, at, step, *rows))
+    tokens.ctx.check(lib().mure_tokens_append_rotated(tokens.h, plan.h, rotary.h, at, step, qr, kr, vr, qor))
     _leave(st)
     return out
 
@@ -856,10 +869,14 @@ def mure_tokens_keep(tokens: Tokens, plan: TokensPlan, kept) -> None:
     follow its earlier ones."""
     if len(kept) != plan.n_seqs:
         raise ValueError(f"kept: {len(kept)} lists of {plan.n_seqs} sequences")
-    count = np.array([len(x) for x in kept], np.int32)
-    index = _int32([i for x in kept for i in x], "kept")
+    count, index = array.array("i", [len(x) for x in kept]), array.array("i")
+    try:
+        for x in kept:
+            index.extend(x)
+    except (TypeError, OverflowError):
+        raise ValueError("kept: whole numbers of 32 bits are wanted") from None
     st = _enter(tokens.ctx, ())
-    tokens.ctx.check(lib().mure_tokens_keep(tokens.h, plan.h, _ptr(count), _ptr(index)))
+    tokens.ctx.check(lib().mure_tokens_keep(tokens.h, plan.h, count.buffer_info()[0], index.buffer_info()[0] if len(index) else None))
     _leave(st)
 
 
