@@ -125,7 +125,8 @@ struct TokRotary {
 };
 // cells: k and v go into their cells (form as given); else k's rows to k_out, and v is not used.
 int launch_tokens_rotate(const TokPool &pool, const TokBatch &b, const TokRotary &r, int dtype, int form, bool cells, int q_heads,
-                         int k_heads, TokRows q, TokRows k, TokRows v, TokRows q_out, TokRows k_out, int64_t tiles, cudaStream_t s);
+                         int k_heads, TokRows q, TokRows k, TokRows v, TokRows q_out, TokRows k_out, int64_t tokens, int64_t tiles,
+                         cudaStream_t s);
 
 // Pages pages[2 i] of one cache to pages[2 i + 1] of another of its geometry (host array, n pairs).
 int launch_tokens_copy_pages(const TokPool &from, const TokPool &to, int elt, bool scales, const int32_t *pages, int64_t n, cudaStream_t s);

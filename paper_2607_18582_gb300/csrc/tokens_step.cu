@@ -165,7 +165,7 @@ mure_status mure_tokens_rotate(mure_tokens *t, mure_tokens_plan *p, const mure_r
         r.positions = positions;
         r.position_stride = position_stride;
         c->launches += launch_tokens_rotate(pool_of(t), p->b, r, t->d.dtype, t->d.form, false, hq, hk, qr, kr, TokRows{}, qo, ko,
-                                            p->tiles_new, c->stream);
+                                            n, p->tiles_new, c->stream);
         check_launch(c);
     });
 }
@@ -195,7 +195,7 @@ mure_status mure_tokens_append_rotated(mure_tokens *t, mure_tokens_plan *p, cons
         r.positions = positions;
         r.position_stride = position_stride;
         c->launches += launch_tokens_rotate(pool_of(t), p->b, r, t->d.dtype, t->d.form, true, hq, hk, qr, kr, vr, qo, TokRows{},
-                                            p->tiles_new, c->stream);
+                                            n, p->tiles_new, c->stream);
         check_launch(c);
     });
 }
