@@ -319,18 +319,24 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp, bool tree = fals
     const FewShape fshape = mure::few_shape(d.dtype, d.form, d.head_dim);
     const Shape few_shape{kFewRows, fshape.tile, 16, fshape.blocks, 2, 3.0, 1.0};
     const Shape chunk_shape{kChunkRows, kChunkTile, chunk_box(d.page_size), chunk_blocks(), 4, 4.0, 0.9};
-    std::vector<Unit> few, chunk;
+    const Shape tree_shape{kTreeRows, kChunkTile, chunk_box(d.page_size), tree_blocks(), 2, 4.0, 0.9};
+    std::vector<Unit> few, chunk, forest;
     std::vector<int32_t> wide_table, wide_pages;
     std::unordered_map<int32_t, int32_t> wide_of;
+    int64_t most_rows = 0;
+    for (const TokSeq &q : seq) most_rows = std::max(most_rows, (int64_t)q.n_new * group);
     for (int s = 0; s < n; ++s) {
         const TokSeq &q = seq[s];
         const int64_t rows = (int64_t)q.n_new * group;
         FAILIF(rows > kMostPos, c, MURE_ERR_UNSUPPORTED, "sequence %d: more than 2^30 rows", s);
-        const bool as_chunk = d.dtype != MURE_F32 && d.head_dim <= kChunkDim && rows > few_rows_up_to(wide, d.head_dim);
-        const Shape &sh = as_chunk ? chunk_shape : few_shape;
-        FAILIF((int64_t)(few.size() + chunk.size()) + (rows + sh.rows - 1) / sh.rows * d.n_kv_heads > kMostUnits, c,
+        // (a batch of trees goes to one kernel whole: 64 trees of 3 to 40 tokens within a window, of which 18 have few rows,
+        // 45 us in two launches one after the other, 41 in one)
+        const bool as_chunk = d.dtype != MURE_F32 && d.head_dim <= kChunkDim && (tree ? most_rows : rows) > few_rows_up_to(wide, d.head_dim);
+        const bool as_tree = as_chunk && tree && !wide && most_rows <= kTreeRows;
+        const Shape &sh = as_tree ? tree_shape : as_chunk ? chunk_shape : few_shape;
+        FAILIF((int64_t)(few.size() + chunk.size() + forest.size()) + (rows + sh.rows - 1) / sh.rows * d.n_kv_heads > kMostUnits, c,
                MURE_ERR_UNSUPPORTED, "more than 2^24 pieces of work");
-        add_units(as_chunk ? chunk : few, q, tree ? nodes.data() + q.row0 : nullptr, d.n_kv_heads, group, b.window, b.sinks, sh);
+        add_units(as_tree ? forest : as_chunk ? chunk : few, q, tree ? nodes.data() + q.row0 : nullptr, d.n_kv_heads, group, b.window, b.sinks, sh);
         if (!as_chunk || !wide) continue;
         // the pages that any of its rows reads
         wide_table.resize(table.size(), 0);
@@ -344,17 +350,19 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp, bool tree = fals
             wide_table[q.table0 + i] = at.first->second;
         }
     }
-    const Shares fs = pack(few, few_shape), cs = pack(chunk, chunk_shape);
+    const Shares fs = pack(few, few_shape), cs = pack(chunk, chunk_shape), ts = pack(forest, tree_shape);
 
     Image im;
     const size_t o_seq = im.add(seq), o_table = im.add(table), o_new = im.add(tile_new), o_all = im.add(tile_all);
     const size_t o_few = im.add(fs.items), o_few1 = im.add(fs.first), o_fewc = im.add(std::vector<int32_t>(fs.cut.size(), 0));
     const size_t o_chunk = im.add(cs.items), o_chunk1 = im.add(cs.first), o_cut = im.add(cs.cut);
+    const size_t o_tree = im.add(ts.items), o_tree1 = im.add(ts.first), o_treec = im.add(ts.cut);
     const size_t o_wt = im.add(wide_table), o_wp = im.add(wide_pages), o_node = im.add(nodes), o_bits = im.add(bits);
     const size_t few_part = ((size_t)fs.parts * few_part_floats(d.head_dim) * 4 + 255) / 256 * 256;
     reserve(c, p->mem, p->mem_bytes, im.bytes.size());
-    const size_t chunk_part = (size_t)cs.parts * chunk_part_floats(d.head_dim) * 4;
-    reserve(c, p->part, p->part_bytes, few_part + chunk_part + cs.items.size() * (kChunkRows / 8));
+    const size_t chunk_part = (size_t)cs.parts * chunk_part_floats(d.head_dim) * 4, chunk_again = (cs.items.size() * (kChunkRows / 8) + 255) / 256 * 256;
+    const size_t tree_part = (size_t)ts.parts * tree_part_floats(d.head_dim) * 4;
+    reserve(c, p->part, p->part_bytes, few_part + chunk_part + chunk_again + tree_part + ts.items.size() * (kTreeRows / 8));
     if (!wide_pages.empty()) {
         const int64_t pool = (int64_t)wide_pages.size() * d.n_kv_heads * d.page_size * d.head_dim * 2;
         reserve(c, p->wide, p->wide_bytes, 2 * (size_t)pool);
@@ -375,14 +383,20 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp, bool tree = fals
     p->few.blocks = (int)fs.first.size() - 1;
     p->few.part = static_cast<float *>(p->part);
     p->few.count = reinterpret_cast<int32_t *>(m + o_fewc);
-    p->chunk.w.items = reinterpret_cast<TokItem *>(m + o_chunk);
-    p->chunk.w.first = reinterpret_cast<int32_t *>(m + o_chunk1);
-    p->chunk.w.blocks = (int)cs.first.size() - 1;
-    p->chunk.w.part = reinterpret_cast<float *>(static_cast<char *>(p->part) + few_part);
-    p->chunk.w.again = reinterpret_cast<uint32_t *>(static_cast<char *>(p->part) + few_part + chunk_part);
-    p->chunk.ml = p->chunk.w.part + (int64_t)cs.parts * (chunk_part_floats(d.head_dim) - 2 * kChunkRows);
-    p->chunk.cut = reinterpret_cast<TokItem *>(m + o_cut);
-    p->chunk.n_cut = (int)cs.cut.size();
+    char *part = static_cast<char *>(p->part) + few_part;
+    auto set_chunk = [&](TokChunk &k, const Shares &s, size_t o_items, size_t o_first, size_t o_cut, int rows, int64_t floats) {
+        k.w.items = reinterpret_cast<TokItem *>(m + o_items);
+        k.w.first = reinterpret_cast<int32_t *>(m + o_first);
+        k.w.blocks = (int)s.first.size() - 1;
+        k.w.part = reinterpret_cast<float *>(part);
+        k.w.again = reinterpret_cast<uint32_t *>(part + (size_t)s.parts * floats * 4);
+        k.ml = k.w.part + (int64_t)s.parts * (floats - 2 * rows);
+        k.cut = reinterpret_cast<TokItem *>(m + o_cut);
+        k.n_cut = (int)s.cut.size();
+    };
+    set_chunk(p->chunk, cs, o_chunk, o_chunk1, o_cut, kChunkRows, chunk_part_floats(d.head_dim));
+    part += chunk_part + chunk_again;
+    set_chunk(p->tree, ts, o_tree, o_tree1, o_treec, kTreeRows, tree_part_floats(d.head_dim));
     p->wide_table = reinterpret_cast<int32_t *>(m + o_wt);
     p->wide_pages = reinterpret_cast<int32_t *>(m + o_wp);
     p->n_wide = (int64_t)wide_pages.size();
@@ -580,6 +594,8 @@ mure_status mure_tokens_attend(mure_tokens *t, mure_tokens_plan *p, const mure_t
         CK(c, cudaSetDevice(c->device));
         const mure_tokens_desc &d = t->d;
         c->launches += launch_tokens_few(pool_of(t), p->b, p->few, d.dtype, d.form, qr, orow, lse, c->stream);
+        c->launches += launch_tokens_tree(pool_of(t), p->b, p->tree, d.dtype, qr, orow, lse, d.n_pages, t->map_k, t->map_v, c->err_dev,
+                                          c->wait_limit, c->stream);
         if (p->chunk.w.blocks > 0) {
             const TokPool codes = pool_of(t);
             TokPool pool = codes;

@@ -107,6 +107,16 @@ bool chunk_map(CUtensorMap &map, void *pool, int dtype, int hk, int d, int page_
 int launch_tokens_chunk(const TokPool &pool, const TokBatch &b, const TokChunk &c, int dtype, TokRows q, TokRows out, float *lse,
                         int64_t n_pages, const CUtensorMap &map_k, const CUtensorMap &map_v, const TokPool *codes,
                         const int32_t *code_table, int *err, int64_t spin, cudaStream_t s);
+// The parts of c's cut units, `of` rows each, joined.
+int launch_tokens_join(const TokChunk &c, int of, const TokBatch &b, int dtype, int d, TokRows out, float *lse, cudaStream_t s);
+
+// Pieces of the kernel for trees: up to 128 rows over tiles of 128 cells, two blocks on a multiprocessor.
+constexpr int kTreeRows = 128;
+int tree_blocks();
+int64_t tree_part_floats(int d);
+int launch_tokens_tree(const TokPool &pool, const TokBatch &b, const TokChunk &c, int dtype, TokRows q, TokRows out, float *lse,
+                       int64_t n_pages, const CUtensorMap &map_k, const CUtensorMap &map_v, int *err, int64_t spin, cudaStream_t s);
+
 // E4M3 pages pages[0 .. n_list) as pages 0 .. n_list - 1 of 16-bit pools k and v, which launch_tokens_chunk takes
 // together with where they come from (`codes`, `code_table`).  A value that f16 does not reach becomes a NaN:
 // the rows that meet it are done from the codes.

@@ -23,6 +23,7 @@ struct mure_tokens_plan {
     std::string append_fault;                // why the batch's new tokens cannot be written ("" if they can)
     mure::TokWork few;                             // 16-bit types: the rows that the kernel for few rows takes
     mure::TokChunk chunk;                          // ... and those that the kernel for chunks takes
+    mure::TokChunk tree;                           // ... and those that the kernel for trees takes
     // E4M3: the pages that chunks read, as 16-bit pages
     const int32_t *wide_pages = nullptr, *wide_table = nullptr;
     int64_t n_wide = 0;
