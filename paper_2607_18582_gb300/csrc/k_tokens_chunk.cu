@@ -41,20 +41,51 @@ namespace mure {
 
 namespace {
 
-constexpr int kThreads = 384;
 
-template <int DP>
+// CODES: the cells are e4m3 codes, widened on their way to the products (trees, whose cells are read once or little more).
+template <int DP, bool CODES>
 struct Chunk {
+    static constexpr int kThreads = CODES ? 512 : 384;
     static constexpr int kPanels = DP / 64;
     static constexpr uint32_t kQ = 2 * kPanels * kPanel;            // two row tiles
     static constexpr uint32_t kStage = kPanels * kPanel;            // a K or V tile
-    static constexpr int kStages = DP == 64 ? 8 : 4;
+    static constexpr int kStages = DP == 64 ? 8 : CODES ? 3 : 4;
+    static constexpr uint32_t kK = CODES && DP == 128 ? 1 : kStages / 2, kV = kStages - kK;    // of K, and of V behind them
     // Tensor memory: S of both row tiles in columns 0 .. 255, O from 256.  P lies over half of S, or for
     // up to 64 values, where O leaves room, beside it: the next scores then need not wait for P V.
     static constexpr bool kApart = DP == 64;
     static __device__ __forceinline__ uint32_t col_p(int h) { return kApart ? 384 + h * 64 : h * 128 + 64; }
     static __device__ __forceinline__ uint32_t col_o(int h) { return 256 + h * DP; }
-    static constexpr uint32_t kSmem = kQ + kStages * kStage + 1024; // (+ room to align to 1024)
+    // CODES: tiles of codes that are copied ahead of their widening
+    static constexpr uint32_t kSlot = kCells * DP, kSlots = !CODES ? 1 : DP == 64 ? 6 : 4;
+    static constexpr uint32_t kSmem = kQ + kStages * kStage + (CODES ? kSlots * kSlot : 0) + 1024; // (+ room to align to 1024)
+};
+
+// Two e4m3 codes of a cell whose scale byte is `byte` as 16-bit values, as the cells' pages widened whole would hold them.
+// Scales at which every product is exact and in range (from 2^-15; to 2^7 for f16, to 2^15 for bf16) go by 16-bit
+// factors, f16's codes by one product for both, bf16's by one for each into fp32; others by fp32 (bits shifted into
+// place and a product of both for bf16, which need a look for NaNs beside: 64 trees' tiles 208 -> 231 us).
+template <class T>
+struct Widen {
+    static constexpr bool kHalf = std::is_same<T, __half>::value;
+    static __device__ __forceinline__ bool fast(uint32_t byte) { return byte - 112u <= (kHalf ? 22u : 30u); }
+    static __device__ __forceinline__ uint32_t unit(uint32_t byte)      // 2^(byte - 127), 2^-15 is subnormal
+    {
+        return byte == 112u ? 0x02000200u : (byte - 112u) * 0x04000400u;
+    }
+    static __device__ __forceinline__ uint32_t pair(uint32_t four, uint32_t which, uint32_t unit)
+    {
+        uint32_t h, r;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(which ? four >> 16 : four)));
+        if constexpr (kHalf) asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(h), "r"(unit));
+        else {
+            float lo, hi;
+            asm("fma.rn.f32.f16 %0, %1, %2, %3;" : "=f"(lo) : "h"((uint16_t)h), "h"((uint16_t)unit), "f"(-0.f));
+            asm("fma.rn.f32.f16 %0, %1, %2, %3;" : "=f"(hi) : "h"((uint16_t)(h >> 16)), "h"((uint16_t)unit), "f"(-0.f));
+            r = narrow2<T>(lo, hi);
+        }
+        return r;
+    }
 };
 
 struct ChunkParams {
@@ -73,17 +104,23 @@ struct ChunkParams {
     CUtensorMap map_k, map_v;
 };
 
-template <class T, int DP, bool TREE>
-__global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_constant__ ChunkParams p)
+// A value of a widened page: what f16 does not reach is a NaN.
+template <class T>
+__device__ __forceinline__ float widened(float x) { return std::is_same<T, __half>::value && !(fabsf(x) <= 65504.f) ? NAN : x; }
+
+template <class T, int DP, bool TREE, bool CODES>
+__global__ void __launch_bounds__(Chunk<DP, CODES>::kThreads, 1) k_tokens_chunk(const __grid_constant__ ChunkParams p)
 {
-    using C = Chunk<DP>;
+    using C = Chunk<DP, CODES>;
     extern __shared__ char smem_raw[];
-    // stages 0 .. kStages / 2 - 1 hold K tiles, the others V tiles
+    // the first kK stages hold K tiles, the others V tiles
     __shared__ __align__(8) uint64_t bar_full[C::kStages], bar_empty[C::kStages], bar_q[2], bar_s[2], bar_p[2][2], bar_o[2], bar_pv[2], bar_turn[2], bar_drain[2];
     __shared__ uint32_t tmem_sh;
     __shared__ int again_sh;                  // rows are marked
     __shared__ WaitCtl ctl_sh;
-    __shared__ TokItem item_sh[12];           // each warp's piece of work
+    __shared__ __align__(8) uint64_t bar_code[C::kSlots], bar_read[C::kSlots];   // codes there, and read
+    __shared__ TokItem item_sh[C::kThreads / 32];   // each warp's piece of work
+    __shared__ TokItem copy_sh;               // CODES: the copies' piece of work
     __shared__ int page_sh[2][2][16];         // copying warps: the pages of a tile's boxes
     volatile WaitCtl *ctl = &ctl_sh;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -100,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
         ctl_sh.abort = 0;
         ctl_sh.limit = p.spin > 0 ? p.spin : kSpin;
         for (int i = 0; i < C::kStages; ++i) {
-            mbar_init(smem_u32(&bar_full[i]), 1);
+            mbar_init(smem_u32(&bar_full[i]), CODES ? 4 : 1);
             mbar_init(smem_u32(&bar_empty[i]), 2);      // the products of both row tiles
         }
         for (int h = 0; h < 2; ++h) {
@@ -112,6 +149,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
             mbar_init(smem_u32(&bar_pv[h]), 1);
             mbar_init(smem_u32(&bar_turn[h]), 1);
             mbar_init(smem_u32(&bar_drain[h]), 1);
+        }
+        for (uint32_t i = 0; i < C::kSlots; ++i) {
+            mbar_init(smem_u32(&bar_code[i]), 1);
+            mbar_init(smem_u32(&bar_read[i]), 4);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -194,8 +235,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 auto mask = [&](uint32_t *x, int i0) {               // 32 cells: a bit each
                     if (open) return;
                     auto below = [&](int n) { return n <= i0 ? 0u : n >= i0 + 32 ? ~0u : (1u << (n - i0)) - 1u; };
-                    const uint32_t bits = TREE ? below(tc.end - tc.start) & tree_seen(tree, tc.start + i0, p.b.window, p.b.sinks)
-                                               : below(last + 1) & (~below(first) | below(sink));
+                    const uint32_t bits = TREE ? below(tc.end - tc.start) & tree_seen(tree, tc.start + i0, p.b.window, p.b.sinks) : below(last + 1) & (~below(first) | below(sink));
 #pragma unroll
                     for (int i = 0; i < 32; ++i) x[i] = bits & (1u << i) ? x[i] : 0xFF800000u;
                 };
@@ -389,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
         // Measured per 256 rows x 128 cells (D = 128; 2,270 cycles of tensor pipe): one warp for both 3,200
         // cycles (what it does between two batches leaves the pipe empty), two warps without turns 3,300
         // (the pipe interleaves them and both softmaxes wait at a time), with turns 2,800.
-        constexpr uint32_t NS = C::kStages / 2;
+        constexpr uint32_t NK = C::kK, NV = C::kV;
         const int h = warp == 8 ? 0 : 1;
         uint32_t n_q = 0, n_p = 0, n_turn = 0, n_k = 0, n_v = 0;     // phases; K and V tiles taken
         const uint32_t id_s = idesc_16<T>(kCells, false), id_o = idesc_16<T>((D + 15) & ~15, true);
@@ -426,29 +466,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 // no rows here: the stages go by one at a time (a barrier's parity names a phase only to
                 // a waiter that is at most one behind)
                 for (int t = t0; t < t1 && ok; ++t, ++n_k, ++n_v) {
-                    ok = warp_wait(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
-                    if (ok && lane == 0) mbar_arrive(smem_u32(&bar_empty[n_k % NS]));
-                    ok = ok && warp_wait(smem_u32(&bar_full[NS + n_v % NS]), (n_v / NS) & 1, ctl);
-                    if (ok && lane == 0) mbar_arrive(smem_u32(&bar_empty[NS + n_v % NS]));
+                    ok = warp_wait(smem_u32(&bar_full[n_k % NK]), (n_k / NK) & 1, ctl);
+                    if (ok && lane == 0) mbar_arrive(smem_u32(&bar_empty[n_k % NK]));
+                    ok = ok && warp_wait(smem_u32(&bar_full[NK + n_v % NV]), (n_v / NV) & 1, ctl);
+                    if (ok && lane == 0) mbar_arrive(smem_u32(&bar_empty[NK + n_v % NV]));
                 }
                 continue;
             }
             if (t1 <= t0) continue;                                  // (rows without cells: no Q, no products)
             ok = warp_wait(smem_u32(&bar_q[h]), n_q++ & 1, ctl);
             if (!ok) break;
-            ok = warp_wait(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
+            ok = warp_wait(smem_u32(&bar_full[n_k % NK]), (n_k / NK) & 1, ctl);
             if (!ok) break;
             fence_after();
-            scores(n_k % NS, false);
+            scores(n_k % NK, false);
             ++n_k;
             for (int t = t0; t < t1; ++t, ++n_v) {
                 const TileCells tc = tile_cells(w, t, p.box);
                 const int ks_v = min(kCells, tc.end - tc.start + 15) / 16;   // cells past the end have probability 0
-                const uint32_t v_stage = NS + n_v % NS;
+                const uint32_t v_stage = NK + n_v % NV;
                 const bool more = t + 1 < t1;
                 const uint64_t b = mn_desc(ring + v_stage * C::kStage);
                 // (turn n of warp 8 follows turn n - 1 of warp 11, turn n of warp 11 turn n of warp 8)
-                ok = warp_wait(smem_u32(&bar_full[v_stage]), (n_v / NS) & 1, ctl) &&
+                ok = warp_wait(smem_u32(&bar_full[v_stage]), (n_v / NV) & 1, ctl) &&
                      warp_wait(smem_u32(&bar_p[h][1]), n_p & 1, ctl) &&
                      (rows <= 128 || (h == 0 && n_turn == 0) || warp_wait(smem_u32(&bar_turn[h]), (n_turn - (h == 0)) & 1, ctl));
                 if (!ok) break;
@@ -470,10 +510,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 ++n_p;
                 fence_after();
                 if (C::kApart && more) {
-                    ok = warp_wait(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
+                    ok = warp_wait(smem_u32(&bar_full[n_k % NK]), (n_k / NK) & 1, ctl);
                     if (!ok) break;
                     fence_after();
-                    scores(n_k % NS, false);
+                    scores(n_k % NK, false);
                     ++n_k;
                 }
                 if (elect_one()) {                                   // cells 32 .. 63
@@ -487,10 +527,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
                 __syncwarp();
                 if (C::kApart) {
                 } else if (more) {
-                    ok = warp_wait(smem_u32(&bar_full[n_k % NS]), (n_k / NS) & 1, ctl);
+                    ok = warp_wait(smem_u32(&bar_full[n_k % NK]), (n_k / NK) & 1, ctl);
                     if (!ok) break;
                     fence_after();
-                    scores(n_k % NS, rows > 128);
+                    scores(n_k % NK, rows > 128);
                     ++n_k;
                 } else if (rows > 128 && lane == 0) {
                     mbar_arrive(smem_u32(&bar_turn[1 - h]));
@@ -502,7 +542,146 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
         if (elect_one()) mma_commit(smem_u32(&bar_drain[h]));
         __syncwarp();
         wait_phase_drain(smem_u32(&bar_drain[h]), 0);
-    } else if (warp == 9 || warp == 10) {
+    } else if (CODES && warp == 9) {
+        // ------------------------------------- copies of codes: a tile's K, then its V, into slots in turn --
+        const uint32_t codes = ring + C::kStages * C::kStage;
+        // the next one: the tile c_t of the piece c_it (c_which: its V)
+        const int boxes = kCells / p.box, page_mask = (1 << p.pool.page_log2) - 1;
+        uint32_t copied = 0;
+        int c_it = it0 - 1, c_t = 0, c_which = 0, page_next = 0;
+        auto page_of = [&](int t) {                                  // the page of box `lane` (none: past the last one, zeros)
+            if (t >= copy_sh.t1 || lane >= boxes) return 0;
+            const TileCells tc = tile_cells(copy_sh, t, p.box);
+            const int j = tc.start + lane * p.box;
+            return j < tc.end ? __ldg(p.b.table + copy_sh.table0 + (j >> p.pool.page_log2)) : (int)p.n_pages;
+        };
+        auto copy = [&] {                                            // false: no more, or a wait ran out
+            while (c_it < it1 && (c_it < it0 || c_t >= copy_sh.t1)) {
+                if (++c_it == it1) break;
+                __syncwarp();
+                if (lane < (int)sizeof(TokItem) / 4)
+                    reinterpret_cast<int32_t *>(&copy_sh)[lane] = __ldg(reinterpret_cast<const int32_t *>(p.w.items + c_it) + lane);
+                __syncwarp();
+                c_t = copy_sh.t0;
+                page_next = page_of(c_t);
+            }
+            if (c_it >= it1) return false;
+            const uint32_t s = copied % C::kSlots, bar = smem_u32(&bar_code[s]);
+            if (copied >= C::kSlots && !warp_wait(smem_u32(&bar_read[s]), (copied / C::kSlots - 1) & 1, ctl)) return false;
+            int *pages = page_sh[0][c_t & 1];
+            if (c_which == 0) {
+                if (lane < 16) pages[lane] = page_next;
+                page_next = page_of(c_t + 1);
+            }
+            __syncwarp();
+            const int start = tile_cells(copy_sh, c_t, p.box).start;
+            if (elect_one()) {
+                const CUtensorMap *map = c_which ? &p.map_v : &p.map_k;
+                mbar_expect_tx(bar, C::kSlot);
+                uint32_t dst = codes + s * C::kSlot;
+                for (int bx = 0; bx < boxes; ++bx, dst += p.box * DP)
+                    copy_box(dst, map, 0, (start + bx * p.box) & page_mask, copy_sh.h, pages[bx], bar);
+            }
+            __syncwarp();
+            ++copied;
+            if (c_which) ++c_t;
+            c_which ^= 1;
+            return true;
+        };
+        while (c_it < it1 && copy()) {
+        }
+        // copies in flight land before shared memory is released
+        for (uint32_t i = copied > C::kSlots ? copied - C::kSlots : 0; i < copied; ++i)
+            wait_phase_drain(smem_u32(&bar_code[i % C::kSlots]), (i / C::kSlots) & 1);
+    } else if (CODES && warp >= 12) {
+        // ------------------------------------------------ widening: a thread per cell of a tile --
+        // Its row of codes, 16 at a time and each thread of a phase at another sixteen (no bank conflicts), goes into the
+        // swizzled tile that the products read, with the row's scale on the way.
+        const int r = threadIdx.x - 384;
+        const uint32_t codes = ring + C::kStages * C::kStage;
+        bool ok = true;
+        uint32_t load = 0, tiles = 0;                                // slots, and tiles of K and of V, done
+        for (int it = it0; it < it1 && ok; ++it) {
+            take(it);
+            const int t1 = w.t1, hh = w.h;
+            const int32_t *table = p.b.table + w.table0;
+            // the scale bytes of the thread's cell, K's and V's (past the end: 256), a tile ahead, and as they are loaded: what
+            // would work on them at once would wait for them
+            uint32_t next[2];
+            auto scales = [&](int t) {
+                const TileCells tc = tile_cells(w, t, p.box);
+                const int j = tc.start + r;
+                next[0] = next[1] = 256u;
+                if (t < t1 && j < tc.end) {
+                    const int64_t row = cell_row(p.pool, table, hh, j);
+                    next[0] = __ldg(p.pool.ks + row);
+                    next[1] = __ldg(p.pool.vs + row);
+                }
+            };
+            scales(w.t0);
+            for (int t = w.t0; t < t1 && ok; ++t, ++tiles) {
+                const uint32_t bytes[2] = {next[0], next[1]};
+                scales(t + 1);
+#pragma unroll 1
+                for (int which = 0; which < 2; ++which, ++load) {
+                    const uint32_t slot = load % C::kSlots, of = which ? C::kV : C::kK, stage = which ? C::kK + tiles % C::kV : tiles % C::kK;
+                    ok = warp_wait(smem_u32(&bar_code[slot]), (load / C::kSlots) & 1, ctl) &&
+                         (tiles < of || warp_wait(smem_u32(&bar_empty[stage]), (tiles / of - 1) & 1, ctl));
+                    if (!ok) break;
+                    const uint32_t to = ring + stage * C::kStage;
+                    {
+                        const uint32_t byte = which ? bytes[1] : bytes[0];
+                        const uint32_t from = codes + slot * C::kSlot + r * DP;
+                        const uint32_t unit = Widen<T>::unit(byte);
+                        const bool fast = Widen<T>::fast(byte);
+                        auto put = [&](int k, uint4 lo, uint4 hi) {
+                            const uint32_t panel = to + (k >> 2) * kPanel;
+                            st_shared16(panel + sw128_off(r, 2 * k & 7), lo);
+                            st_shared16(panel + sw128_off(r, (2 * k & 7) + 1), hi);
+                        };
+                        if (fast) {
+                            // (two at a time: the loop unrolled whole costs more in instruction fetches, 189 -> 209 us)
+#pragma unroll 1
+                            for (int c0 = 0; c0 < DP / 16; c0 += 2) {
+                                uint4 v[2];
+                                int k[2];
+#pragma unroll
+                                for (int c = 0; c < 2; ++c) {
+                                    k[c] = DP == 128 ? (c0 + c + r) & 7 : (c0 + c + (r >> 1)) & 3;
+                                    v[c] = ld_shared16(from + k[c] * 16);
+                                }
+#pragma unroll
+                                for (int c = 0; c < 2; ++c)
+                                    put(k[c],
+                                        make_uint4(Widen<T>::pair(v[c].x, 0, unit), Widen<T>::pair(v[c].x, 1, unit),
+                                                   Widen<T>::pair(v[c].y, 0, unit), Widen<T>::pair(v[c].y, 1, unit)),
+                                        make_uint4(Widen<T>::pair(v[c].z, 0, unit), Widen<T>::pair(v[c].z, 1, unit),
+                                                   Widen<T>::pair(v[c].w, 0, unit), Widen<T>::pair(v[c].w, 1, unit)));
+                            }
+                        } else {
+                            const float s = scale_of(byte & 255u);
+                            auto slow = [&](uint32_t four, int half) {
+                                const float2 f = e4m3_values((uint16_t)(half ? four >> 16 : four));
+                                return byte == 256u ? 0u : narrow2<T>(widened<T>(f.x * s), widened<T>(f.y * s));
+                            };
+#pragma unroll 1
+                            for (int k = 0; k < DP / 16; ++k) {
+                                const uint4 v = ld_shared16(from + k * 16);
+                                put(k, make_uint4(slow(v.x, 0), slow(v.x, 1), slow(v.y, 0), slow(v.y, 1)),
+                                    make_uint4(slow(v.z, 0), slow(v.z, 1), slow(v.w, 0), slow(v.w, 1)));
+                            }
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(smem_u32(&bar_read[slot]));
+                        mbar_arrive(smem_u32(&bar_full[stage]));
+                    }
+                }
+            }
+        }
+    } else if (!CODES) {
         // -------------------------------------------- copies: warp 9 K tiles, warp 10 V tiles --
         constexpr uint32_t NS = C::kStages / 2;
         const int which = warp - 9, boxes = kCells / p.box, slots = (1 << p.pool.page_log2) - 1;
@@ -563,7 +742,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
     // infinity has met a probability of 0.  Here, where no wait is left that their time could run out on.
     for (int it = it0; it < it1; ++it) {
         take(it);
-        for (int r = warp; r < w.rows; r += kThreads / 32) {
+        for (int r = warp; r < w.rows; r += C::kThreads / 32) {
             if (!(p.w.again[(int64_t)it * (kChunkRows / 32) + r / 32] >> (r & 31) & 1)) continue;
             const int row = w.r0 + r, token = w.row0 + row / p.b.group, head = w.h * p.b.group + row % p.b.group;
             const T *q = reinterpret_cast<const T *>(p.q.p) + token * p.q.ts + head * p.q.hs;
@@ -572,7 +751,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tokens_chunk(const __grid_const
             TreeRow tree{};
             if (TREE) tree = tree_row(p.b, token);
             const int pos = TREE ? tree.pos : w.pos + row / p.b.group, j0 = first.start, j1 = min(end.end, end.start + kCells);
-            if (p.code_table)
+            if (CODES || p.code_table)
                 attend_row<T, true, TREE>(p.codes, p.code_table + w.table0, w.h, q, p.q.vec, pos, j0, j1, p.b.window, p.b.sinks,
                                           p.b.scale_log2, y, m, l, tree);
             else
@@ -627,18 +806,20 @@ __global__ void __launch_bounds__(256) k_tokens_join(const TokItem *cut, int of,
     if (lse && lane == 0) lse[(int64_t)token * b.n_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945f;
 }
 
-template <class T, int DP, bool TREE>
+template <class T, int DP, bool TREE, bool CODES>
 void pieces(const ChunkParams &p, cudaStream_t s)
 {
-    allow_dynamic_smem_once<k_tokens_chunk<T, DP, TREE>>(Chunk<DP>::kSmem);
-    k_tokens_chunk<T, DP, TREE><<<p.w.blocks, kThreads, Chunk<DP>::kSmem, s>>>(p);
+    using C = Chunk<DP, CODES>;
+    allow_dynamic_smem_once<k_tokens_chunk<T, DP, TREE, CODES>>(C::kSmem);
+    k_tokens_chunk<T, DP, TREE, CODES><<<p.w.blocks, C::kThreads, C::kSmem, s>>>(p);
 }
 
 template <class T, int DP>
-int go(const ChunkParams &p, const TokChunk &c, cudaStream_t s)
+int go(const ChunkParams &p, const TokChunk &c, bool fused, cudaStream_t s)
 {
-    if (p.b.node) pieces<T, DP, true>(p, s);
-    else pieces<T, DP, false>(p, s);
+    if (p.b.node && fused) pieces<T, DP, true, true>(p, s);
+    else if (p.b.node) pieces<T, DP, true, false>(p, s);
+    else pieces<T, DP, false, false>(p, s);
     return 1 + launch_tokens_join(c, kChunkRows, p.b, std::is_same<T, __half>::value ? MURE_F16 : MURE_BF16, p.pool.d, p.out, p.lse, s);
 }
 
@@ -673,9 +854,21 @@ bool chunk_map(CUtensorMap &map, void *pool, int dtype, int hk, int d, int page_
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool chunk_code_map(CUtensorMap &map, void *pool, int hk, int d, int page_size, int64_t n_pages)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 enc = tensor_map_encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)page_size, (cuuint64_t)hk, (cuuint64_t)n_pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)d, (cuuint64_t)d * page_size, (cuuint64_t)d * page_size * hk};
+    const cuuint32_t box[4] = {d <= 64 ? 64u : 128u, (cuuint32_t)chunk_box(page_size), 1, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return enc(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int launch_tokens_chunk(const TokPool &pool, const TokBatch &b, const TokChunk &c, int dtype, TokRows q, TokRows out, float *lse,
                         int64_t n_pages, const CUtensorMap &map_k, const CUtensorMap &map_v, const TokPool *codes,
-                        const int32_t *code_table, int *err, int64_t spin, cudaStream_t s)
+                        const int32_t *code_table, bool fused, int *err, int64_t spin, cudaStream_t s)
 {
     if (c.w.blocks == 0) return 0;
     ChunkParams p{};
@@ -691,8 +884,8 @@ int launch_tokens_chunk(const TokPool &pool, const TokBatch &b, const TokChunk &
     p.spin = spin;
     p.map_k = map_k;
     p.map_v = map_v;
-    if (dtype == MURE_F16) return pool.d <= 64 ? go<__half, 64>(p, c, s) : go<__half, 128>(p, c, s);
-    return pool.d <= 64 ? go<__nv_bfloat16, 64>(p, c, s) : go<__nv_bfloat16, 128>(p, c, s);
+    if (dtype == MURE_F16) return pool.d <= 64 ? go<__half, 64>(p, c, fused, s) : go<__half, 128>(p, c, fused, s);
+    return pool.d <= 64 ? go<__nv_bfloat16, 64>(p, c, fused, s) : go<__nv_bfloat16, 128>(p, c, fused, s);
 }
 
 }  // namespace mure

@@ -350,6 +350,19 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp, bool tree = fals
             wide_table[q.table0 + i] = at.first->second;
         }
     }
+    // Trees on codes: their pieces widen the tiles that they read themselves, unless so many read the same ones that
+    // widening the pages once costs less (48 trees of 48 tokens over 4,000 cells, as many on the same pages: 1 tree 282 us
+    // against 418, 2 282 / 297, 3 282 / 260, 8 282 / 213).
+    p->fused = false;
+    if (tree && wide && d.head_dim % 16 == 0 && !chunk.empty()) {
+        int64_t read = 0;                                           // tiles, by all pieces
+        for (const Unit &u : chunk) read += u.tiles;
+        p->fused = 2 * read * kChunkTile <= 5 * ((int64_t)wide_pages.size() << page_log2) * d.n_kv_heads;
+    }
+    if (p->fused) {
+        wide_table.clear();
+        wide_pages.clear();
+    }
     const Shares fs = pack(few, few_shape), cs = pack(chunk, chunk_shape), ts = pack(forest, tree_shape);
 
     Image im;
@@ -489,6 +502,12 @@ mure_status mure_tokens_create(mure_ctx *c, const mure_tokens_desc *desc, mure_t
             if (e != cudaSuccess) dfree(c, m);
             CK(c, e);
         }
+        if (d.dtype != MURE_F32 && q && d.head_dim <= kChunkDim && d.head_dim % 16 == 0) {
+            const bool ok = chunk_code_map(t->map_k, t->d.k, d.n_kv_heads, d.head_dim, d.page_size, d.n_pages) &&
+                            chunk_code_map(t->map_v, t->d.v, d.n_kv_heads, d.head_dim, d.page_size, d.n_pages);
+            if (!ok) dfree(c, t->own);
+            FAILIF(!ok, c, MURE_ERR_CUDA, "no tensor map of the pools");
+        }
         if (d.dtype != MURE_F32 && !q && d.head_dim <= kChunkDim) {
             const bool ok = chunk_map(t->map_k, t->d.k, d.dtype, d.n_kv_heads, d.head_dim, d.page_size, d.n_pages) &&
                             chunk_map(t->map_v, t->d.v, d.dtype, d.n_kv_heads, d.head_dim, d.page_size, d.n_pages);
@@ -600,7 +619,7 @@ mure_status mure_tokens_attend(mure_tokens *t, mure_tokens_plan *p, const mure_t
             const TokPool codes = pool_of(t);
             TokPool pool = codes;
             TokBatch b = p->b;
-            const bool wide = d.form == MURE_FORM_E4M3;
+            const bool codes_in = d.form == MURE_FORM_E4M3, wide = codes_in && !p->fused;
             if (wide) {
                 const int64_t bytes = p->n_wide * d.n_kv_heads * d.page_size * d.head_dim * 2;
                 pool.k = p->wide;
@@ -609,8 +628,8 @@ mure_status mure_tokens_attend(mure_tokens *t, mure_tokens_plan *p, const mure_t
                 c->launches += launch_tokens_widen(codes, d.dtype, p->wide_pages, p->n_wide, pool.k, pool.v, c->stream);
             }
             c->launches += launch_tokens_chunk(pool, b, p->chunk, d.dtype, qr, orow, lse, wide ? p->n_wide : d.n_pages,
-                                               wide ? p->map_k : t->map_k, wide ? p->map_v : t->map_v, wide ? &codes : nullptr,
-                                               p->b.table, c->err_dev, c->wait_limit, c->stream);
+                                               wide ? p->map_k : t->map_k, wide ? p->map_v : t->map_v, codes_in ? &codes : nullptr,
+                                               p->b.table, p->fused, c->err_dev, c->wait_limit, c->stream);
         }
         check_launch(c);
     });

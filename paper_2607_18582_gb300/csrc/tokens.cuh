@@ -104,9 +104,11 @@ int chunk_blocks();
 int chunk_box(int page_size);         // cells of a box its copies take (and its tiles' alignment)
 int64_t chunk_part_floats(int d);
 bool chunk_map(CUtensorMap &map, void *pool, int dtype, int hk, int d, int page_size, int64_t n_pages);
+// The map of a pool of codes, d a multiple of 16: with it (fused) a tree's pieces widen the codes themselves.
+bool chunk_code_map(CUtensorMap &map, void *pool, int hk, int d, int page_size, int64_t n_pages);
 int launch_tokens_chunk(const TokPool &pool, const TokBatch &b, const TokChunk &c, int dtype, TokRows q, TokRows out, float *lse,
                         int64_t n_pages, const CUtensorMap &map_k, const CUtensorMap &map_v, const TokPool *codes,
-                        const int32_t *code_table, int *err, int64_t spin, cudaStream_t s);
+                        const int32_t *code_table, bool fused, int *err, int64_t spin, cudaStream_t s);
 // The parts of c's cut units, `of` rows each, joined.
 int launch_tokens_join(const TokChunk &c, int of, const TokBatch &b, int dtype, int d, TokRows out, float *lse, cudaStream_t s);
 

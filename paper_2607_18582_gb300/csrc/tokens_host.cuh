@@ -8,7 +8,7 @@ struct mure_tokens {
     mure_ctx *ctx = nullptr;
     mure_tokens_desc d{};
     void *own = nullptr;      // the library's allocation of the pools (null: the caller's pools)
-    CUtensorMap map_k, map_v; // 16-bit cells of up to kChunkDim values: the pools
+    CUtensorMap map_k, map_v; // 16-bit types of up to kChunkDim values: the pools (codes: of multiples of 16 values)
 };
 
 struct mure_tokens_plan {
@@ -27,6 +27,7 @@ struct mure_tokens_plan {
     // E4M3: the pages that chunks read, as 16-bit pages
     const int32_t *wide_pages = nullptr, *wide_table = nullptr;
     int64_t n_wide = 0;
+    bool fused = false;                      // E4M3 trees: the pieces widen codes themselves
     CUtensorMap map_k, map_v;
     void *mem = nullptr, *part = nullptr, *wide = nullptr;    // tables; partial results; 16-bit pages
     size_t mem_bytes = 0, part_bytes = 0, wide_bytes = 0;
