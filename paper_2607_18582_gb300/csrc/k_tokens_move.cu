@@ -69,8 +69,7 @@ void copy(const TokPool &from, const TokPool &to, int64_t bytes, int64_t scale_b
 }
 
 // ------------------------------------------------------------------- cells --
-constexpr int kKeepSeqs = 512, kKeepIndex = 6000;
-
+template <int S, int I>                      // sequences and indexes of a launch: two sizes, as above
 struct KeepParams {
     TokPool pool;
     const TokSeq *seq;
@@ -78,8 +77,8 @@ struct KeepParams {
     int elt;                                 // bytes of a value, or of a code
     int scales;
     int lanes;                               // threads of a row, a power of two: 8 values each
-    int32_t of[kKeepSeqs], first[kKeepSeqs + 1], to[kKeepSeqs];
-    int32_t index[kKeepIndex];
+    int32_t of[S], first[S + 1], to[S];
+    int32_t index[I];
 };
 
 struct alignas(16) Wide { uint4 a, b; };
@@ -87,8 +86,8 @@ struct alignas(16) Wide { uint4 a, b; };
 // A block moves one sequence's cells, a group of threads a cached head's rows at a time.  A thread takes its part
 // of four cells to registers before it writes any: as the indexes ascend, the fifth source lies past the fourth target,
 // and so does every later one.
-template <class W>                           // eight values: Wide (fp32), uint4 (16 bits), uint2 (codes)
-__global__ void __launch_bounds__(128) k_tokens_keep(const __grid_constant__ KeepParams p)
+template <class W, int S, int I>             // eight values: Wide (fp32), uint4 (16 bits), uint2 (codes)
+__global__ void __launch_bounds__(128) k_tokens_keep(const __grid_constant__ KeepParams<S, I> p)
 {
     const int b = blockIdx.x;
     const TokSeq sq = p.seq[p.of[b]];
@@ -125,6 +124,43 @@ __global__ void __launch_bounds__(128) k_tokens_keep(const __grid_constant__ Kee
     }
 }
 
+template <int S, int I>
+int keep(const TokPool &pool, const TokBatch &b, int elt, bool scales, const int32_t *seq, const int32_t *first, const int32_t *end,
+         const int32_t *to, const int32_t *index, int64_t n, cudaStream_t s)
+{
+    static_assert(sizeof(KeepParams<S, I>) <= 32764, "more than a kernel's arguments");
+    const int lanes = row_lanes(pool.d), per = 128 / lanes;
+    int launches = 0;
+    int64_t i = 0;
+    int32_t at = first[0];                   // the next index of sequence i's
+    while (i < n) {
+        KeepParams<S, I> p;
+        p.pool = pool; p.seq = b.seq; p.table = b.table;
+        p.elt = elt; p.scales = scales; p.lanes = lanes;
+        int seqs = 0, used = 0;
+        while (i < n && seqs < S && used < I) {
+            const int take = end[i] - at < I - used ? end[i] - at : I - used;
+            p.of[seqs] = seq[i];
+            p.first[seqs] = used;
+            p.to[seqs] = to[i] + (at - first[i]);
+            memcpy(p.index + used, index + at, (size_t)take * sizeof(int32_t));
+            used += take;
+            at += take;
+            ++seqs;
+            if (at < end[i]) break;          // the rest of a long list follows in the stream's order
+            ++i;
+            if (i < n) at = first[i];
+        }
+        p.first[seqs] = used;
+        const dim3 grid(seqs, (pool.hk + per - 1) / per);
+        if (elt == 4) k_tokens_keep<Wide, S, I><<<grid, 128, 0, s>>>(p);
+        else if (elt == 2) k_tokens_keep<uint4, S, I><<<grid, 128, 0, s>>>(p);
+        else k_tokens_keep<uint2, S, I><<<grid, 128, 0, s>>>(p);
+        ++launches;
+    }
+    return launches;
+}
+
 }  // namespace
 
 int launch_tokens_copy_pages(const TokPool &from, const TokPool &to, int elt, bool scales, const int32_t *pages, int64_t n, cudaStream_t s)
@@ -145,37 +181,11 @@ int launch_tokens_copy_pages(const TokPool &from, const TokPool &to, int elt, bo
 int launch_tokens_keep(const TokPool &pool, const TokBatch &b, int elt, bool scales, const int32_t *seq, const int32_t *first,
                        const int32_t *end, const int32_t *to, const int32_t *index, int64_t n, cudaStream_t s)
 {
-    static_assert(sizeof(KeepParams) <= 32764, "more than a kernel's arguments");
-    const int lanes = row_lanes(pool.d), per = 128 / lanes;
-    int launches = 0;
-    int64_t i = 0;
-    int32_t at = n > 0 ? first[0] : 0;       // the next index of sequence i's
-    while (i < n) {
-        KeepParams p;
-        p.pool = pool; p.seq = b.seq; p.table = b.table;
-        p.elt = elt; p.scales = scales; p.lanes = lanes;
-        int seqs = 0, used = 0;
-        while (i < n && seqs < kKeepSeqs && used < kKeepIndex) {
-            const int take = end[i] - at < kKeepIndex - used ? end[i] - at : kKeepIndex - used;
-            p.of[seqs] = seq[i];
-            p.first[seqs] = used;
-            p.to[seqs] = to[i] + (at - first[i]);
-            memcpy(p.index + used, index + at, (size_t)take * sizeof(int32_t));
-            used += take;
-            at += take;
-            ++seqs;
-            if (at < end[i]) break;    // the rest of a long list follows in the stream's order
-            ++i;
-            if (i < n) at = first[i];
-        }
-        p.first[seqs] = used;
-        const dim3 grid(seqs, (pool.hk + per - 1) / per);
-        if (elt == 4) k_tokens_keep<Wide><<<grid, 128, 0, s>>>(p);
-        else if (elt == 2) k_tokens_keep<uint4><<<grid, 128, 0, s>>>(p);
-        else k_tokens_keep<uint2><<<grid, 128, 0, s>>>(p);
-        ++launches;
-    }
-    return launches;
+    if (n == 0) return 0;
+    int64_t total = 0;
+    for (int64_t i = 0; i < n; ++i) total += end[i] - first[i];
+    return n <= 64 && total <= 768 ? keep<64, 768>(pool, b, elt, scales, seq, first, end, to, index, n, s)
+                                   : keep<512, 6000>(pool, b, elt, scales, seq, first, end, to, index, n, s);
 }
 
 }  // namespace mure
