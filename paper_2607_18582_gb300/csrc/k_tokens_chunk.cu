@@ -11,7 +11,8 @@
 //   0-3, 4-7  softmax of the two row tiles, a thread per row: no shuffles; they also fetch Q and
 //             write the rows out;
 //   8, 11     issue the MMAs of either row tile;
-//   9, 10     copy K and V tiles by tensor maps, a box per page (or 128 cells of a larger page).
+//   9, 10     copy K and V tiles by tensor maps, a box per page (or 128 cells of a larger page);
+//   12-15     (on codes) widen them, see below.
 // What a row's scores are taken relative to lies 7 below their running maximum and moves only when that
 // grows by more than 8 (in powers of two; f16 holds powers up to 2^15, and those down to 2^-21 of the
 // largest keep all its bits), so O is hardly ever rescaled; where it is, S's arrival (or, where P lies
@@ -32,6 +33,15 @@
 // (pieces of a few dozen tiles, 12,000 cycles of beginning and end each).  Chunks within a window
 // (64 values): 72 us: the softmax's latency, 1,800 cycles per tile of which 1,024 exponentials, and a beginning
 // and end for every ten tiles, not measured by themselves for 64 values.
+//
+// Trees (TREE): a row sees all cells before its sequence's new ones that its position allows, and of the new ones' those
+// whose bits are set.  On e4m3 cells (CODES) a tree's pieces may widen the codes themselves: warp 9 copies tiles of codes into
+// slots of their own, and warps 12 to 15 turn them into the 16-bit tiles that the products read, a thread per cell.
+// Widening whole pages first moves 5 bytes for each code, which only readers of a page in numbers are worth: 48 trees of 17
+// to 64 tokens over 500 to 6,000 cells of 8 heads of 128, 345 us so (191 of them the widening), 189 us by the pieces
+// themselves.  What bounds these is the chain from a tile of codes to the products (2,950 ns per tile of 256 rows; the same
+// with the codes copied as they are, 2,560 ns without touching them), not the conversions.  Trees of 200 to 256 rows over
+// 100,000 to 131,000 cells of 16 bits: 192 to 205 us, 5.0 TB/s.
 #include <type_traits>
 
 #include "simt_tile.cuh"

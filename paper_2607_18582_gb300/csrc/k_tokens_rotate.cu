@@ -10,8 +10,15 @@
 // that a pair never leaves its thread, the row's sum of squares is a few shuffles away, and an e4m3 row is quantised in
 // the pass that rotated it.  A group takes a token and some or all of its heads: its sines and cosines, times the
 // weights, stay in registers from head to head.  A block takes a tile of up to 16 tokens of one sequence.
-// Everything is fp32 up to one rounding to the activations' type; codes are made from that rounding, so that both ways to
+// A thread's rows are copied ahead through shared memory, where only it reads them, so that no barrier is needed and
+// registers hold one row at a time.  Everything is fp32 up to one rounding to the activations' type; codes are made from that rounding, so that both ways to
 // a cell store the same bits.
+//
+// Measured (GB300): 57,000 tokens of 32 and 8 heads of 128 bf16 values, normed and rotated, keys and values into e4m3 cells:
+// 216 us, 5.9 TB/s of what it has to move; 168 million warp instructions, issue slots 65 % busy at 3.8 warps per scheduler.
+// 28,000 tokens of 16 heads of 80 f16 values, positions along three axes, no norm: 72 us, 4.0 TB/s: latency and issue, a
+// group has one token and five of its eight lanes a part of the row.  (Groups of as many lanes as a row needs: 71 us, but
+// 216 -> 236 with the sums over five lanes; eight values a thread 364 and 82 us.)
 #include <type_traits>
 
 #include "simt_tile.cuh"

@@ -12,6 +12,13 @@
 //   5    copies K and V tiles by tensor maps.
 // A cell before the tree's is seen by its position, as anywhere; of the tree's own a row sees those whose bits are set
 // (its token and its ancestors), 32 at a time.
+//
+// Measured (GB300): 64 trees of 3 to 40 tokens within a window of 1,024, 15 heads of 64 f16 values on 5: 37 us and 4 for the
+// join (the kernel for chunks: 55 and 3; with the few rows' kernel before this one for the smaller trees, 27 and 18).  One
+// tree of 24 tokens over 700 cells: 15 us, of which a piece's beginning and end are some 9 (sequence, piece, page and cells in a
+// chain of loads, then scores, softmax and product) and a tile 2.1.  Trees of more than 128 rows are slower here than where two row
+// tiles share each K and V tile: 200 to 256 rows over 100,000 cells 215 us against 192, 120 to 256 over 700 to 3,000 71
+// against 66.
 #include "simt_tile.cuh"
 #include "tokens_tc.cuh"
 

@@ -17,7 +17,12 @@ def grow(n, branch, rng, roots=0.1):
 
 
 class Tree(Batch):
-    """Batch, its new tokens trees."""
+    """Batch, its new tokens trees.
+
+    Beside test_gpu_tokens.py's tolerances, f16: a probability is held as an f16 number P = 2^(s - m), m at least 7 below the
+    row's largest score, so that the largest P is 2^7 or more and one below f16's normal numbers is off by
+    2^-25, half their least step: by 2^-25 / 2^7 = 2^-32 of the row's sum or less.  Over all cells that is
+    2^-32 sum |v|.  Cells of codes are f16 numbers for the products: half a least step, 2^-25, off, as the output is."""
 
     def __init__(self, M, ctx, new, pos, kv, *a, parents=None, branch=4, **k):  # noqa: F811
         rng = np.random.default_rng(k.get("seed", 0))
@@ -75,6 +80,8 @@ class Tree(Batch):
                 E = torch.where(see, q[:, h].abs() @ kf[:, j].abs().T * scale, torch.zeros_like(s)).amax(-1)
                 c = 2.0 ** -24 * (8 * math.sqrt(self.d) * E + 8 * math.sqrt(self.kv[b]) + 64)
                 tol[:, h] = u * out[:, h].abs() + (u + c[:, None]) * A + 1e-30
+                if self.dtype == "f16":
+                    tol[:, h] += 2.0 ** -32 * (see.double() @ vf[:, j].abs()) + 2.0 ** -24
                 ltol[:, h] = c * (1 + lse[:, h].abs())
             empty = ~see.any(-1)
             out[empty], lse[empty], tol[empty] = 0.0, -math.inf, 0.0
@@ -156,6 +163,67 @@ def test_masked_cells_may_hold_anything(M, ctx, dtype, form, new):  # noqa: F811
     ref, tol, _, _ = t.reference()
     assert bool(((got[0].double() - ref).abs() <= tol)[free].all())
     assert bool(((got[0].double() - clean.double()).abs() <= 2 * tol)[free].all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [128, 64, 96, 40])
+def test_codes_of_all_scales(M, ctx, dtype, d):  # noqa: F811
+    """Scale bytes from the least to far past the common ones, NaN codes in masked cells and in one that some rows see: trees
+    of many rows widen codes by short cuts that have to give the definition's values."""
+    t = Tree(M, ctx, [90, 70], [700, 130], [790, 200], 8, 2, d, 16, dtype, "e4m3", seed=d, branch=6)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for which, (lo, hi) in ((2, (100, 128)), (3, (96, 134) if dtype == "f16" else (96, 150))):
+        t.pools[which].copy_(torch.randint(lo, hi, t.pools[which].shape, generator=g, device="cuda").to(torch.uint8))
+    t.pools[3][:, :, ::5] = 0
+    t.pools[2][:, :, 1::7] = 0
+    t.pools[2][:, :, 2::7] = 111
+    t.pools[2][:, :, 3::7] = 112
+    t.check()
+    cell = 40                                              # of sequence 0's tree: its own row and its descendants'
+    at = (int(t.table[0, (700 + cell) // 16]), slice(None), (700 + cell) % 16)
+    t.pools[1].view(torch.uint8)[at][:, d // 2] = 0x7F
+    t.pools[0].view(torch.uint8)[(int(t.table[1, 3]), slice(None), 5)][:, 1] = 0xFF
+    out, _ = M.mure_tokens_attend(t.cache, t.plan, t.q, lse=True)
+    M.mure_synchronize(ctx)
+    hit = t.seen(0)[:, 700 + cell]
+    assert bool(torch.isnan(out[:90][hit][..., d // 2]).all()) and bool(torch.isfinite(out[:90][~hit]).all())
+    assert bool(torch.isnan(out[90:]).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [128, 64])
+def test_shared_pages_of_codes(M, ctx, dtype, d):  # noqa: F811
+    """Trees over one sequence's pages (which are then widened once) give the bits that they give over pages of their
+    own (which each piece widens)."""
+    n, new, past, pages = 4, 60, 1000, -(-1060 // 16)
+    own = Tree(M, ctx, [new] * n, [past] * n, [past + new] * n, 8, 2, d, 16, dtype, "e4m3", parents=[grow(new, 5, np.random.default_rng(2))] * n)
+    for p in own.pools:                                     # all sequences' cells are sequence 0's
+        p = p.view(torch.uint8)
+        first = torch.from_numpy(own.table[0, :pages].astype(np.int64)).cuda()
+        for b in range(1, n):
+            p[torch.from_numpy(own.table[b, :pages].astype(np.int64)).cuda()] = p[first]
+    apart = own.check()
+    plan = M.mure_tokens_plan(own.cache, 8, own.new, own.pos, own.kv, np.repeat(own.table[:1], n, 0), parents=[p for x in own.parents for p in x])
+    shared = M.mure_tokens_attend(own.cache, plan, own.q, lse=True)
+    M.mure_synchronize(ctx)
+    assert torch.equal(apart[0], shared[0]) and torch.equal(apart[1], shared[1])
+
+
+def test_expired_waits(M):
+    """Trees whose waits run out at once give TIMEOUT, and the same plans work again after it."""
+    ctx = M.mure_create(0)  # noqa: F811
+    trees = [Tree(M, ctx, [60, 20], [900, 300], [960, 320], heads, 2, 128, 16, "bf16", form)
+             for heads, form in ((8, "same"), (4, "same"), (8, "e4m3"))]
+    for t in trees:
+        t.check()
+    for t in trees:
+        M.mure_set_wait_limit(ctx, 1)
+        M.mure_tokens_attend(t.cache, t.plan, t.q)
+        with pytest.raises(M.MureError) as ei:
+            M.mure_synchronize(ctx)
+        assert ei.value.status == 5
+        M.mure_set_wait_limit(ctx, 0)
+        t.check()
 
 
 def test_long_pasts(M, ctx):  # noqa: F811
