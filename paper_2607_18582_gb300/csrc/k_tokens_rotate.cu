@@ -132,8 +132,9 @@ __global__ void __launch_bounds__(kThreads, 4) k_tokens_rotate(RotateParams p)
     const Tile t = tile_of(p.b, false, sq);
     const int D = p.pool.d, slot = threadIdx.x & (p.lanes - 1), group = threadIdx.x / p.lanes, groups = kThreads / p.lanes;
     const bool in = slot * N < D, turned = slot * N < p.r.rot;
-    // this thread's values of a row: two runs; with pairs of halves the rotated ones lie half a rotation apart
-    const int half = p.r.rot / 2, at = !ADJ && turned ? slot * (N / 2) : slot * N, second = !ADJ && turned ? half : N / 2;
+    // this thread's values of a row: two runs, half of the rotated values apart (or of the others): a pair of halves has one in
+    // either, neighbours are in one, and the lanes' copies lie side by side
+    const int half = p.r.rot / 2, at = turned ? slot * (N / 2) : p.r.rot + (slot * N - p.r.rot) / 2, second = turned ? half : (D - p.r.rot) / 2;
     const float over = 1.f / D;
     // the block's groups over the tile's tokens: of fewer tokens than groups each has several, which share its heads
     const int share = t.n < groups ? groups / t.n : 1, together = groups / share;
@@ -221,7 +222,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_tokens_rotate(RotateParams p)
             const int own = p.r.positions ? 0 : sq.pos + (p.b.node ? __ldg(&p.b.node[token].depth) : t.i0 + i);
 #pragma unroll
             for (int e = 0; e < N / 2; ++e) {
-                const int k = slot * (N / 2) + e;
+                const int k = !ADJ ? at + e : e < N / 4 ? at / 2 + e : (half + at) / 2 + e - N / 4;
                 const int pos = p.r.positions ? __ldg(p.r.positions + __ldg(p.r.axis + k) * p.r.position_stride + token) : own;
                 const uint64_t turn = (uint64_t)(int64_t)pos * __ldg(p.r.turn + k);
                 // to the nearest 2^-32 of a turn, in -1/2 .. 1/2
