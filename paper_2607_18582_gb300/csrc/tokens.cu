@@ -24,6 +24,10 @@ namespace {
 // widened first, 128 values, 64 rows 126 / 137, 128 rows 225 / 138, 64 values 90 / 92 and 164 / 93.
 // (Measured at that one shape.  fp32 rows, and heads of more than 128 values, have no other kernel.)
 int few_rows_up_to(bool codes, int d) { return codes ? 64 : d <= 64 ? 32 : 16; }
+// Trees, whose pieces widen codes themselves (48 sequences of 4,000 cells, 8 heads; few / the others, us): codes of 128
+// values, 24 rows 177 / 200, 32 177 / 201, 48 248 / 202, of 64 values, 32 128 / 193, 48 182 / 193, 64 236 / 193; cells as they are, of
+// 128 values, 16 rows 144 / 154, 24 163 / 155, of 64 values, 32 95 / 115, 48 124 / 112.
+int few_tree_rows_up_to(bool codes, int d) { return codes && d % 16 == 0 ? (d <= 64 ? 48 : 32) : few_rows_up_to(codes, d); }
 
 constexpr int64_t kMostPos = int64_t(1) << 30, kMostUnits = int64_t(1) << 24;
 
@@ -329,9 +333,11 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp, bool tree = fals
         const TokSeq &q = seq[s];
         const int64_t rows = (int64_t)q.n_new * group;
         FAILIF(rows > kMostPos, c, MURE_ERR_UNSUPPORTED, "sequence %d: more than 2^30 rows", s);
-        // (a batch of trees goes to one kernel whole: 64 trees of 3 to 40 tokens within a window, of which 18 have few rows,
-        // 45 us in two launches one after the other, 41 in one)
-        const bool as_chunk = d.dtype != MURE_F32 && d.head_dim <= kChunkDim && (tree ? most_rows : rows) > few_rows_up_to(wide, d.head_dim);
+        // (a batch of trees on cells as they are goes to one kernel whole: 64 trees of 3 to 40 tokens within a window, of which 18
+        // have few rows, 45 us in two launches one after the other, 41 in one; the kernel for few rows is little faster
+        // on those even by itself, but on codes twice as fast)
+        const int up_to = tree ? few_tree_rows_up_to(wide, d.head_dim) : few_rows_up_to(wide, d.head_dim);
+        const bool as_chunk = d.dtype != MURE_F32 && d.head_dim <= kChunkDim && (tree && !wide ? most_rows : rows) > up_to;
         const bool as_tree = as_chunk && tree && !wide && most_rows <= kTreeRows;
         const Shape &sh = as_tree ? tree_shape : as_chunk ? chunk_shape : few_shape;
         FAILIF((int64_t)(few.size() + chunk.size() + forest.size()) + (rows + sh.rows - 1) / sh.rows * d.n_kv_heads > kMostUnits, c,
