@@ -85,36 +85,37 @@ struct KeepParams {
 
 struct alignas(16) Wide { uint4 a, b; };
 
-// A block moves one sequence's cells, a group of threads a cached head's rows at a time.  A thread takes its part
-// of four cells to registers before it writes any: as the indexes ascend, the fifth source lies past the fourth target,
-// and so does every later one.
+// A block moves the cells of one sequence and cached head, a group of threads one cell's rows: four cells a group are
+// in registers before any is written.  As the indexes ascend, a later source lies behind every target before it, so that
+// the next round's sources are still whole.
 template <class W, int S, int I>             // eight values: Wide (fp32), uint4 (16 bits), uint2 (codes)
 __global__ void __launch_bounds__(128) k_tokens_keep(const __grid_constant__ KeepParams<S, I> p)
 {
-    const int b = blockIdx.x;
+    const int b = blockIdx.x, h = blockIdx.y;
     const TokSeq sq = p.seq[p.of[b]];
     const int32_t *table = p.table + sq.table0;
-    const int D = p.pool.d, slot = threadIdx.x & (p.lanes - 1), c = slot * 8;
-    const int h = blockIdx.y * (128 / p.lanes) + threadIdx.x / p.lanes;
-    if (c >= D || h >= p.pool.hk) return;
+    const int D = p.pool.d, slot = threadIdx.x & (p.lanes - 1), c = slot * 8, group = threadIdx.x / p.lanes, groups = 128 / p.lanes;
     const int i0 = p.first[b], n = p.first[b + 1] - i0;
     constexpr int U = 4;
-    for (int i = 0; i < n; i += U) {
+    for (int base = 0; base < n; base += groups * U) {
         W k[U], v[U];
         uint32_t scale[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (i + u < n) {
-                const int64_t row = cell_row(p.pool, table, h, sq.pos + p.index[i0 + i + u]);
+            const int i = base + group + u * groups;
+            if (i < n && c < D) {
+                const int64_t row = cell_row(p.pool, table, h, sq.pos + p.index[i0 + i]);
                 k[u] = *reinterpret_cast<const W *>(static_cast<const char *>(p.pool.k) + (row * D + c) * p.elt);
                 v[u] = *reinterpret_cast<const W *>(static_cast<const char *>(p.pool.v) + (row * D + c) * p.elt);
                 if (p.scales && slot == 0) scale[u] = p.pool.ks[row] | (uint32_t)p.pool.vs[row] << 8;
             }
         }
+        __syncthreads();
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (i + u < n) {
-                const int64_t row = cell_row(p.pool, table, h, sq.pos + p.to[b] + i + u);
+            const int i = base + group + u * groups;
+            if (i < n && c < D) {
+                const int64_t row = cell_row(p.pool, table, h, sq.pos + p.to[b] + i);
                 *reinterpret_cast<W *>(static_cast<char *>(p.pool.k) + (row * D + c) * p.elt) = k[u];
                 *reinterpret_cast<W *>(static_cast<char *>(p.pool.v) + (row * D + c) * p.elt) = v[u];
                 if (p.scales && slot == 0) {
@@ -131,7 +132,7 @@ int keep(const TokPool &pool, const TokBatch &b, int elt, bool scales, const int
          const int32_t *to, const int32_t *index, int64_t n, cudaStream_t s)
 {
     static_assert(sizeof(KeepParams<S, I>) <= 32764, "more than a kernel's arguments");
-    const int lanes = row_lanes(pool.d), per = 128 / lanes;
+    const int lanes = row_lanes(pool.d);
     int launches = 0;
     int64_t i = 0;
     int32_t at = first[0];                   // the next index of sequence i's
@@ -154,7 +155,7 @@ int keep(const TokPool &pool, const TokBatch &b, int elt, bool scales, const int
             if (i < n) at = first[i];
         }
         p.first[seqs] = used;
-        const dim3 grid(seqs, (pool.hk + per - 1) / per);
+        const dim3 grid(seqs, pool.hk);
         if (elt == 4) k_tokens_keep<Wide, S, I><<<grid, 128, 0, s>>>(p);
         else if (elt == 2) k_tokens_keep<uint4, S, I><<<grid, 128, 0, s>>>(p);
         else k_tokens_keep<uint2, S, I><<<grid, 128, 0, s>>>(p);
