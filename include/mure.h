@@ -456,6 +456,7 @@ mure_status mure_tokens_buffers(const mure_tokens *tokens, mure_tokens_desc *out
  * fails the plan is left without a batch.  A batch whose tables take more than 1 MiB (some
  * 200,000 pages) is copied once the stream's earlier work is done: the call then waits for
  * it.  A plan holds its tables, room for partial sums
+ * (so graphs that are captured from calls of one plan are replayed one after the other, as the stream has the calls)
  * and, for chunks on e4m3 cells, the pages they read widened to 16 bits (each page once
  * however many sequences share it).  Errors: INVALID_ARG (a NULL array, a negative
  * length, positions past 2^30, a page id out of range, head counts that do not divide,

@@ -185,6 +185,8 @@ def test_cells_are_those_of_the_two_calls(M, ctx, dtype, form, layout, heads, hk
     assert torch.equal(qa, qb)
     for a, b in zip(t.pools, u.pools):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    q = u.q.clone()
+    assert M.mure_tokens_append_rotated(u.cache, u.plan, r, q, u.k, u.v, out=q) is q and torch.equal(q, qa)
     for p in u.pools:
         p.view(torch.uint8).zero_()
     assert M.mure_tokens_append_rotated(u.cache, u.plan, r, None, u.k, u.v) is None

@@ -166,7 +166,7 @@ def test_masked_cells_may_hold_anything(M, ctx, dtype, form, new):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("d", [128, 64, 96, 40])
+@pytest.mark.parametrize("d", [128, 64, 96, 40, 16])
 def test_codes_of_all_scales(M, ctx, dtype, d):  # noqa: F811
     """Scale bytes from the least to far past the common ones, NaN codes in masked cells and in one that some rows see: trees
     of many rows widen codes by short cuts that have to give the definition's values."""
