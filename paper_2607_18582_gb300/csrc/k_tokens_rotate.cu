@@ -16,9 +16,9 @@
 //
 // Measured (GB300): 57,000 tokens of 32 and 8 heads of 128 bf16 values, normed and rotated, keys and values into e4m3 cells:
 // 216 us, 5.9 TB/s of what it has to move; 168 million warp instructions, issue slots 65 % busy at 3.8 warps per scheduler.
-// 28,000 tokens of 16 heads of 80 f16 values, positions along three axes, no norm: 72 us, 4.0 TB/s: latency and issue, a
-// group has one token and five of its eight lanes a part of the row.  (Groups of as many lanes as a row needs: 71 us, but
-// 216 -> 236 with the sums over five lanes; eight values a thread 364 and 82 us.)
+// 28,000 tokens of 16 heads of 80 f16 values, neighbouring pairs, positions along three axes, no norm: 60 us, 4.8 TB/s:
+// latency and issue, a group has one token and five of its eight lanes a part of the row.  (Groups of as many lanes as a row
+// needs: as fast, but 216 -> 236 us with the sums over five lanes; eight values a thread 364 and 82 us.)
 #include <type_traits>
 
 #include "simt_tile.cuh"
