@@ -788,6 +788,8 @@ template <class T>
 __global__ void __launch_bounds__(256) k_tokens_join(const TokItem *cut, int of, int DP, TokBatch b, int D, TokRows out, float *lse,
                                                      const float *part, const float *ml)
 {
+    // (launched while the parts are still made, see launch_tokens_join, or after them: then this waits for nothing)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const TokItem &w = cut[blockIdx.x];
     const int r = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (r >= w.rows) return;
@@ -830,18 +832,29 @@ int go(const ChunkParams &p, const TokChunk &c, bool fused, cudaStream_t s)
     if (p.b.node && fused) pieces<T, DP, true, true>(p, s);
     else if (p.b.node) pieces<T, DP, true, false>(p, s);
     else pieces<T, DP, false, false>(p, s);
-    return 1 + launch_tokens_join(c, kChunkRows, p.b, std::is_same<T, __half>::value ? MURE_F16 : MURE_BF16, p.pool.d, p.out, p.lse, s);
+    return 1 + launch_tokens_join(c, kChunkRows, p.b, std::is_same<T, __half>::value ? MURE_F16 : MURE_BF16, p.pool.d, p.out, p.lse, false, s);
 }
 
 }  // namespace
 
-int launch_tokens_join(const TokChunk &c, int of, const TokBatch &b, int dtype, int d, TokRows out, float *lse, cudaStream_t s)
+int launch_tokens_join(const TokChunk &c, int of, const TokBatch &b, int dtype, int d, TokRows out, float *lse, bool early, cudaStream_t s)
 {
     if (c.n_cut == 0) return 0;
-    const dim3 grid(c.n_cut, of / 8);
     const int dp = d <= 64 ? 64 : 128;
-    if (dtype == MURE_F16) k_tokens_join<__half><<<grid, 256, 0, s>>>(c.cut, of, dp, b, d, out, lse, c.w.part, c.ml);
-    else k_tokens_join<__nv_bfloat16><<<grid, 256, 0, s>>>(c.cut, of, dp, b, d, out, lse, c.w.part, c.ml);
+    // early: the parts' kernel lets this launch begin at once, and its blocks wait for it (one tree's two launches 20 -> 19 us;
+    // behind the two-tile kernel's long runs 189 -> 194).
+    cudaLaunchAttribute attribute{};
+    attribute.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attribute.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3(c.n_cut, of / 8);
+    config.blockDim = 256;
+    config.stream = s;
+    config.attrs = &attribute;
+    config.numAttrs = early ? 1 : 0;
+    const float *part = c.w.part, *ml = c.ml;
+    if (dtype == MURE_F16) cudaLaunchKernelEx(&config, k_tokens_join<__half>, c.cut, of, dp, b, d, out, lse, part, ml);
+    else cudaLaunchKernelEx(&config, k_tokens_join<__nv_bfloat16>, c.cut, of, dp, b, d, out, lse, part, ml);
     return 1;
 }
 

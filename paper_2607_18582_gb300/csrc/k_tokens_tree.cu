@@ -99,6 +99,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_tokens_tree(const __grid_consta
     __syncthreads();
     fence_after();
     const uint32_t tmem = tmem_sh;
+    asm volatile("griddepcontrol.launch_dependents;");               // (the join may begin; it waits for this grid's end)
     const int it0 = p.w.first[blockIdx.x], it1 = p.w.first[blockIdx.x + 1];
     const TokItem &w = item_sh[warp];
     auto take = [&](int it) {
@@ -548,7 +549,7 @@ int launch_tokens_tree(const TokPool &pool, const TokBatch &b, const TokChunk &c
     p.map_v = map_v;
     const int launches = dtype == MURE_F16 ? (pool.d <= 64 ? go<__half, 64>(p, s) : go<__half, 128>(p, s))
                                            : (pool.d <= 64 ? go<__nv_bfloat16, 64>(p, s) : go<__nv_bfloat16, 128>(p, s));
-    return launches + launch_tokens_join(c, kTreeRows, b, dtype, pool.d, out, lse, s);
+    return launches + launch_tokens_join(c, kTreeRows, b, dtype, pool.d, out, lse, true, s);
 }
 
 }  // namespace mure

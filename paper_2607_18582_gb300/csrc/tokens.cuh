@@ -109,8 +109,8 @@ bool chunk_code_map(CUtensorMap &map, void *pool, int hk, int d, int page_size, 
 int launch_tokens_chunk(const TokPool &pool, const TokBatch &b, const TokChunk &c, int dtype, TokRows q, TokRows out, float *lse,
                         int64_t n_pages, const CUtensorMap &map_k, const CUtensorMap &map_v, const TokPool *codes,
                         const int32_t *code_table, bool fused, int *err, int64_t spin, cudaStream_t s);
-// The parts of c's cut units, `of` rows each, joined.
-int launch_tokens_join(const TokChunk &c, int of, const TokBatch &b, int dtype, int d, TokRows out, float *lse, cudaStream_t s);
+// The parts of c's cut units, `of` rows each, joined (early: their kernel lets dependent launches begin).
+int launch_tokens_join(const TokChunk &c, int of, const TokBatch &b, int dtype, int d, TokRows out, float *lse, bool early, cudaStream_t s);
 
 // Pieces of the kernel for trees: up to 128 rows over tiles of 128 cells, two blocks on a multiprocessor.
 constexpr int kTreeRows = 128;

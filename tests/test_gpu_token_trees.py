@@ -521,6 +521,30 @@ def test_captured_steps(M):
                     assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
 
 
+def test_captured_joins(M):
+    """Trees whose rows are split and joined, captured: replays give the calls' bits, also behind other work."""
+    s = torch.cuda.Stream()
+    ctx = M.mure_create(0, stream=s)  # noqa: F811
+    with torch.cuda.stream(s):
+        for heads, form in ((4, "same"), (16, "same"), (16, "e4m3")):
+            t = Tree(M, ctx, [30, 12], [6000, 3000], [6030, 3012], heads, 2, 128, 16, "bf16", form)
+            before = M.mure_kernel_launches(ctx)
+            want = [x.clone() for x in M.mure_tokens_attend(t.cache, t.plan, t.q, lse=True)]
+            assert M.mure_kernel_launches(ctx) - before >= 2
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=s):
+                x = torch.zeros(1 << 22, device="cuda")
+                x += 1
+                got = M.mure_tokens_attend(t.cache, t.plan, t.q, lse=True)
+                y = got[0].clone()
+            for _ in range(20):
+                for g in got:
+                    g.fill_(7)
+                graph.replay()
+                assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(y, want[0])
+            M.mure_synchronize(ctx)
+
+
 def test_another_stream(M):
     """A context on a stream of its own, called from torch's current one."""
     ctx = M.mure_create(0, stream=torch.cuda.Stream())  # noqa: F811
