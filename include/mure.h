@@ -472,7 +472,7 @@ void mure_tokens_plan_free(mure_tokens_plan *plan);
  * i, or -1 for one that follows the earlier cells.  depth(i) is the number of its ancestors among the new tokens, its
  * position pos[b] + depth(i), and its cell, as for any batch, the one at pos[b] + i.  It attends to itself, to its
  * ancestors, and to the cells before pos[b], all within kv_len[b] and, where window > 0, by their positions as above.
- * A chain (parents i - 1) is an ordinary batch, and gives its results.  Every call takes such a plan.  Errors: as above;
+ * A chain (parents i - 1) means what an ordinary batch does.  Every call takes such a plan.  Errors: as above;
  * INVALID_ARG (NULL parents with new tokens, a parent that is not before its token), UNSUPPORTED (a tree of more than
  * MURE_TREE_MAX tokens). */
 enum { MURE_TREE_MAX = 1024 };

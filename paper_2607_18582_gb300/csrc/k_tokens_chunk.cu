@@ -51,7 +51,6 @@ namespace mure {
 
 namespace {
 
-
 // CODES: the cells are e4m3 codes, widened on their way to the products (trees, whose cells are read once or little more).
 template <int DP, bool CODES>
 struct Chunk {
@@ -639,47 +638,45 @@ __global__ void __launch_bounds__(Chunk<DP, CODES>::kThreads, 1) k_tokens_chunk(
                          (tiles < of || warp_wait(smem_u32(&bar_empty[stage]), (tiles / of - 1) & 1, ctl));
                     if (!ok) break;
                     const uint32_t to = ring + stage * C::kStage;
-                    {
-                        const uint32_t byte = which ? bytes[1] : bytes[0];
-                        const uint32_t from = codes + slot * C::kSlot + r * DP;
-                        const uint32_t unit = Widen<T>::unit(byte);
-                        const bool fast = Widen<T>::fast(byte);
-                        auto put = [&](int k, uint4 lo, uint4 hi) {
-                            const uint32_t panel = to + (k >> 2) * kPanel;
-                            st_shared16(panel + sw128_off(r, 2 * k & 7), lo);
-                            st_shared16(panel + sw128_off(r, (2 * k & 7) + 1), hi);
+                    const uint32_t byte = which ? bytes[1] : bytes[0];
+                    const uint32_t from = codes + slot * C::kSlot + r * DP;
+                    const uint32_t unit = Widen<T>::unit(byte);
+                    const bool fast = Widen<T>::fast(byte);
+                    auto put = [&](int k, uint4 lo, uint4 hi) {
+                        const uint32_t panel = to + (k >> 2) * kPanel;
+                        st_shared16(panel + sw128_off(r, 2 * k & 7), lo);
+                        st_shared16(panel + sw128_off(r, (2 * k & 7) + 1), hi);
+                    };
+                    if (fast) {
+                        // (two at a time: the loop unrolled whole costs more in instruction fetches, 189 -> 209 us)
+#pragma unroll 1
+                        for (int c0 = 0; c0 < DP / 16; c0 += 2) {
+                            uint4 v[2];
+                            int k[2];
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                k[c] = DP == 128 ? (c0 + c + r) & 7 : (c0 + c + (r >> 1)) & 3;
+                                v[c] = ld_shared16(from + k[c] * 16);
+                            }
+#pragma unroll
+                            for (int c = 0; c < 2; ++c)
+                                put(k[c],
+                                    make_uint4(Widen<T>::pair(v[c].x, 0, unit), Widen<T>::pair(v[c].x, 1, unit),
+                                               Widen<T>::pair(v[c].y, 0, unit), Widen<T>::pair(v[c].y, 1, unit)),
+                                    make_uint4(Widen<T>::pair(v[c].z, 0, unit), Widen<T>::pair(v[c].z, 1, unit),
+                                               Widen<T>::pair(v[c].w, 0, unit), Widen<T>::pair(v[c].w, 1, unit)));
+                        }
+                    } else {
+                        const float s = scale_of(byte & 255u);
+                        auto slow = [&](uint32_t four, int half) {
+                            const float2 f = e4m3_values((uint16_t)(half ? four >> 16 : four));
+                            return byte == 256u ? 0u : narrow2<T>(widened<T>(f.x * s), widened<T>(f.y * s));
                         };
-                        if (fast) {
-                            // (two at a time: the loop unrolled whole costs more in instruction fetches, 189 -> 209 us)
 #pragma unroll 1
-                            for (int c0 = 0; c0 < DP / 16; c0 += 2) {
-                                uint4 v[2];
-                                int k[2];
-#pragma unroll
-                                for (int c = 0; c < 2; ++c) {
-                                    k[c] = DP == 128 ? (c0 + c + r) & 7 : (c0 + c + (r >> 1)) & 3;
-                                    v[c] = ld_shared16(from + k[c] * 16);
-                                }
-#pragma unroll
-                                for (int c = 0; c < 2; ++c)
-                                    put(k[c],
-                                        make_uint4(Widen<T>::pair(v[c].x, 0, unit), Widen<T>::pair(v[c].x, 1, unit),
-                                                   Widen<T>::pair(v[c].y, 0, unit), Widen<T>::pair(v[c].y, 1, unit)),
-                                        make_uint4(Widen<T>::pair(v[c].z, 0, unit), Widen<T>::pair(v[c].z, 1, unit),
-                                                   Widen<T>::pair(v[c].w, 0, unit), Widen<T>::pair(v[c].w, 1, unit)));
-                            }
-                        } else {
-                            const float s = scale_of(byte & 255u);
-                            auto slow = [&](uint32_t four, int half) {
-                                const float2 f = e4m3_values((uint16_t)(half ? four >> 16 : four));
-                                return byte == 256u ? 0u : narrow2<T>(widened<T>(f.x * s), widened<T>(f.y * s));
-                            };
-#pragma unroll 1
-                            for (int k = 0; k < DP / 16; ++k) {
-                                const uint4 v = ld_shared16(from + k * 16);
-                                put(k, make_uint4(slow(v.x, 0), slow(v.x, 1), slow(v.y, 0), slow(v.y, 1)),
-                                    make_uint4(slow(v.z, 0), slow(v.z, 1), slow(v.w, 0), slow(v.w, 1)));
-                            }
+                        for (int k = 0; k < DP / 16; ++k) {
+                            const uint4 v = ld_shared16(from + k * 16);
+                            put(k, make_uint4(slow(v.x, 0), slow(v.x, 1), slow(v.y, 0), slow(v.y, 1)),
+                                make_uint4(slow(v.z, 0), slow(v.z, 1), slow(v.w, 0), slow(v.w, 1)));
                         }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
