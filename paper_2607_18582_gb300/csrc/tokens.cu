@@ -327,6 +327,7 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp, bool tree = fals
     std::vector<Unit> few, chunk, forest;
     std::vector<int32_t> wide_table, wide_pages;
     std::unordered_map<int32_t, int32_t> wide_of;
+    std::vector<int> widen;                     // the sequences whose codes are wanted as 16-bit cells
     int64_t most_rows = 0;
     for (const TokSeq &q : seq) most_rows = std::max(most_rows, (int64_t)q.n_new * group);
     for (int s = 0; s < n; ++s) {
@@ -343,32 +344,41 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp, bool tree = fals
         FAILIF((int64_t)(few.size() + chunk.size() + forest.size()) + (rows + sh.rows - 1) / sh.rows * d.n_kv_heads > kMostUnits, c,
                MURE_ERR_UNSUPPORTED, "more than 2^24 pieces of work");
         add_units(as_tree ? forest : as_chunk ? chunk : few, q, tree ? nodes.data() + q.row0 : nullptr, d.n_kv_heads, group, b.window, b.sinks, sh);
-        if (!as_chunk || !wide) continue;
-        // the pages that any of its rows reads
-        wide_table.resize(table.size(), 0);
+        if (as_chunk && wide) widen.push_back(s);
+    }
+    // the pages that any of a sequence's rows reads, with where they are in the table; false from f: enough
+    auto read_pages = [&](const TokSeq &q, auto f) {
         const int64_t end = std::min<int64_t>(q.kv, (int64_t)q.pos + q.n_new);
         const int64_t from = b.window > 0 ? std::max(0, q.pos - b.window + 1) : 0;
         for (int64_t i = 0; i << page_log2 < end; ++i) {
             if (((i + 1) << page_log2) <= from && i << page_log2 >= b.sinks) continue;
-            const int32_t id = table[q.table0 + i];
-            const auto at = wide_of.emplace(id, (int32_t)wide_pages.size());
-            if (at.second) wide_pages.push_back(id);
-            wide_table[q.table0 + i] = at.first->second;
+            if (!f(q.table0 + i, table[q.table0 + i])) return;
         }
-    }
+    };
     // Trees on codes: their pieces widen the tiles that they read themselves, unless so many read the same ones that
     // widening the pages once costs less (48 trees of 48 tokens over 4,000 cells, as many on the same pages: 1 tree 282 us
     // against 418, 2 282 / 297, 3 282 / 260, 8 282 / 213).
     p->fused = false;
-    if (tree && wide && d.head_dim % 16 == 0 && !chunk.empty()) {
-        int64_t read = 0;                                           // tiles, by all pieces
-        for (const Unit &u : chunk) read += u.tiles;
-        p->fused = 2 * read * kChunkTile <= 5 * ((int64_t)wide_pages.size() << page_log2) * d.n_kv_heads;
+    if (tree && d.head_dim % 16 == 0 && !widen.empty()) {
+        int64_t tiles = 0, most = 0, different = 0;
+        for (const Unit &u : chunk) tiles += u.tiles;
+        const int64_t page_cells = (int64_t)d.page_size * d.n_kv_heads, enough = (2 * tiles * kChunkTile + 5 * page_cells - 1) / (5 * page_cells);
+        for (int s : widen) most += ((int64_t)seq[s].kv + d.page_size - 1) >> page_log2;
+        IdSet ids(std::min<int64_t>(most, d.n_pages));
+        for (int s : widen)
+            if (different < enough) read_pages(seq[s], [&](int64_t, int32_t id) { return (different += ids.insert(id)) < enough; });
+        p->fused = different >= enough;
     }
-    if (p->fused) {
-        wide_table.clear();
-        wide_pages.clear();
-    }
+    if (!p->fused)
+        for (int s : widen) {
+            wide_table.resize(table.size(), 0);
+            read_pages(seq[s], [&](int64_t at, int32_t id) {
+                const auto known = wide_of.emplace(id, (int32_t)wide_pages.size());
+                if (known.second) wide_pages.push_back(id);
+                wide_table[at] = known.first->second;
+                return true;
+            });
+        }
     const Shares fs = pack(few, few_shape), cs = pack(chunk, chunk_shape), ts = pack(forest, tree_shape);
 
     Image im;

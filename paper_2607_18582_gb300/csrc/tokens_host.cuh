@@ -37,6 +37,33 @@ namespace mure {
 
 constexpr int64_t kMostStride = int64_t(1) << 40;
 
+// Ids of a set, by open addressing: whether one of them, twice or a probe, is there.
+struct IdSet {
+    std::vector<int32_t> slot;
+    uint32_t mask;
+    explicit IdSet(int64_t n)
+    {
+        uint32_t size = 16;
+        while (size < 2 * (uint64_t)n && size < (1u << 31)) size *= 2;
+        slot.assign(size, -1);
+        mask = size - 1;
+    }
+    uint32_t at(int32_t id) const
+    {
+        uint32_t i = (uint32_t)id * 2654435761u & mask;
+        while (slot[i] != -1 && slot[i] != id) i = (i + 1) & mask;
+        return i;
+    }
+    bool insert(int32_t id)                     // false: it was there
+    {
+        const uint32_t i = at(id);
+        if (slot[i] == id) return false;
+        slot[i] = id;
+        return true;
+    }
+    bool has(int32_t id) const { return slot[at(id)] == id; }
+};
+
 inline int elt_bytes(int dtype) { return dtype == MURE_F32 ? 4 : 2; }
 
 inline int log2_of(int n)

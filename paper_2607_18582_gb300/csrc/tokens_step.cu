@@ -41,33 +41,6 @@ void check_rotary(mure_ctx *c, const mure_tokens *t, const mure_tokens_plan *p, 
            "position_stride %lld is not in %lld..2^40", (long long)stride, (long long)p->n_new);
 }
 
-// Ids of a set, by open addressing: whether one of them, twice or a probe, is there.
-struct IdSet {
-    std::vector<int32_t> slot;
-    uint32_t mask;
-    explicit IdSet(int64_t n)
-    {
-        uint32_t size = 16;
-        while (size < 2 * (uint64_t)n && size < (1u << 31)) size *= 2;
-        slot.assign(size, -1);
-        mask = size - 1;
-    }
-    uint32_t at(int32_t id) const
-    {
-        uint32_t i = (uint32_t)id * 2654435761u & mask;
-        while (slot[i] != -1 && slot[i] != id) i = (i + 1) & mask;
-        return i;
-    }
-    bool insert(int32_t id)                     // false: it was there
-    {
-        const uint32_t i = at(id);
-        if (slot[i] == id) return false;
-        slot[i] = id;
-        return true;
-    }
-    bool has(int32_t id) const { return slot[at(id)] == id; }
-};
-
 int cell_bytes(const mure_tokens_desc &d) { return d.form == MURE_FORM_E4M3 ? 1 : elt_bytes(d.dtype); }
 
 }  // namespace
