@@ -120,6 +120,22 @@ struct Part {
     }
 };
 
+// Sine and cosine of t 2^-32 turns: quarter turns aside, the eighth of a turn that is left as an fp32 number, and what that
+// rounding leaves (below 2^-27 of a turn) by the first order.
+__device__ __forceinline__ void of_turn(uint32_t t, float &sine, float &cosine)
+{
+    const uint32_t q = (t + 0x20000000u) >> 30;
+    const int32_t r = (int32_t)(t - (q << 30));
+    const float near = (float)r, rest = (float)(r - (int32_t)near) * (3.14159265f * 0x1p-31f);
+    float s, c;
+    sincospif(near * 0x1p-31f, &s, &c);
+    const float s1 = fmaf(c, rest, s), c1 = fmaf(-s, rest, c);
+    sine = q & 1 ? c1 : s1;
+    cosine = q & 1 ? s1 : c1;
+    sine = q & 2 ? -sine : sine;
+    cosine = (q + 1) & 2 ? -cosine : cosine;
+}
+
 template <class T, int TO, bool ADJ, int N>
 __global__ void __launch_bounds__(kThreads, 4) k_tokens_rotate(RotateParams p)
 {
@@ -225,10 +241,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_tokens_rotate(RotateParams p)
                 const int k = !ADJ ? at + e : e < N / 4 ? at / 2 + e : (half + at) / 2 + e - N / 4;
                 const int pos = p.r.positions ? __ldg(p.r.positions + __ldg(p.r.axis + k) * p.r.position_stride + token) : own;
                 const uint64_t turn = (uint64_t)(int64_t)pos * __ldg(p.r.turn + k);
-                // to the nearest 2^-32 of a turn, in -1/2 .. 1/2
-                const float u = (float)(int32_t)(uint32_t)((turn + 0x80000000ull) >> 32) * 0x1p-31f;
                 float sine, cosine;
-                sincospif(u, &sine, &cosine);
+                of_turn((uint32_t)((turn + 0x80000000ull) >> 32), sine, cosine);
                 sines[e][threadIdx.x] = cosine;
                 sines[N / 2 + e][threadIdx.x] = sine;
             }
