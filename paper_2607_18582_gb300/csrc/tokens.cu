@@ -268,9 +268,11 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp, bool tree = fals
     int past_end = -1;
     std::vector<TokNode> nodes;
     std::vector<uint32_t> bits;
+    // (all of them before any list is read whose length they add up to)
+    for (int s = 0; s < n; ++s)
+        FAILIF(b.new_len[s] < 0 || b.pos[s] < 0 || b.kv_len[s] < 0, c, MURE_ERR_INVALID_ARG, "sequence %d: a negative length or position", s);
     for (int s = 0; s < n; ++s) {
         const int64_t nn = b.new_len[s], pos = b.pos[s], kv = b.kv_len[s];
-        FAILIF(nn < 0 || pos < 0 || kv < 0, c, MURE_ERR_INVALID_ARG, "sequence %d: a negative length or position", s);
         FAILIF(pos + nn > kMostPos || kv > kMostPos, c, MURE_ERR_INVALID_ARG, "sequence %d: positions past 2^30", s);
         const int64_t pages = (kv + d.page_size - 1) >> page_log2;
         FAILIF(pages > 0 && (!b.page_table || b.table_stride < pages), c, MURE_ERR_INVALID_ARG,

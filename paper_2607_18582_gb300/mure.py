@@ -642,6 +642,8 @@ def mure_tokens_plan(tokens: Tokens, n_heads: int, new_len, pos, kv_len, page_ta
     ctx, n_new = tokens.ctx, int(keep[0].sum(dtype=np.int64))
     if parents is not None:
         parents = _int32(parents, "parents").reshape(-1)
+        if (keep[0] < 0).any():
+            raise ValueError("new_len: a negative length")
         if len(parents) != n_new:
             raise ValueError(f"parents: {len(parents)} of {n_new} new tokens")
         if n_new == 0:
