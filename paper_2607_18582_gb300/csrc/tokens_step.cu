@@ -234,9 +234,10 @@ mure_status mure_tokens_keep(mure_tokens *t, mure_tokens_plan *p, const int32_t 
         FAILIF(!count, c, MURE_ERR_INVALID_ARG, "NULL count");
         std::vector<int32_t> seq, first, end, to;
         int64_t at = 0;
-        for (int b = 0; b < n; ++b) {
+        for (int b = 0; b < n; ++b)              // (all of them before any index, whose number they add up to)
             FAILIF(count[b] < 0 || count[b] > p->seq[b].n_new, c, MURE_ERR_INVALID_ARG, "sequence %d: %d kept of %d new tokens", b, count[b],
                    p->seq[b].n_new);
+        for (int b = 0; b < n; ++b) {
             if (count[b] == 0) continue;
             FAILIF(!index, c, MURE_ERR_INVALID_ARG, "NULL index");
             int still = 0;                       // the first ones that are where they are to be

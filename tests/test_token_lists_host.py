@@ -88,3 +88,27 @@ def test_negative_lengths_of_trees_are_refused(new, parents):
 
     with pytest.raises(ValueError):
         mure.mure_tokens_plan(Cache, 1, new, [0] * len(new), [0] * len(new), [[0]] * len(new), parents=parents)
+
+
+def test_kept_indexes_are_read_after_all_counts(tmp_path):
+    """Counts of which a later one cannot be name more indexes than there are: the count is refused first."""
+    said = run(tmp_path, "tokens_step.cu", r"""
+int main()
+{
+    mure_ctx c;
+    mure_tokens t;
+    mure_tokens_plan p;
+    t.ctx = p.ctx = &c;
+    t.d = p.d = geometry();
+    p.ready = true;
+    p.seq = {{0, 50, 0, 50, 0, 0}, {50, 50, 0, 50, 4, 50}};
+    const int32_t counts[][2] = {{50, -49}, {-1, 2}, {50, -50}, {50, 51}};
+    for (auto &n : counts) {
+        const int status = mure_tokens_keep(&t, &p, n, at_the_end({0}));
+        printf("%d %s\n", status, c.err.c_str());
+        fflush(stdout);
+    }
+    return 0;
+}
+""")
+    assert said == [f"1 sequence {s}: {n} kept of 50 new tokens" for s, n in ((1, -49), (0, -1), (1, -50), (1, 51))]
