@@ -37,20 +37,22 @@ namespace mure {
 
 constexpr int64_t kMostStride = int64_t(1) << 40;
 
-// Ids of a set, by open addressing: whether one of them, twice or a probe, is there.
+// Ids of a set, by open addressing: whether one of them, twice or a probe, is there.  A slot goes by the product's high bits,
+// which all of an id's bits reach: by its low ones, ids that are multiples of a power of two would share few slots.
 struct IdSet {
     std::vector<int32_t> slot;
     uint32_t mask;
+    int shift = 28;                             // 32 less the bits of a slot's number
     explicit IdSet(int64_t n)
     {
         uint32_t size = 16;
-        while (size < 2 * (uint64_t)n && size < (1u << 31)) size *= 2;
+        for (; size < 2 * (uint64_t)n && size < (1u << 31); size *= 2) --shift;
         slot.assign(size, -1);
         mask = size - 1;
     }
     uint32_t at(int32_t id) const
     {
-        uint32_t i = (uint32_t)id * 2654435761u & mask;
+        uint32_t i = (uint32_t)id * 2654435761u >> shift;
         while (slot[i] != -1 && slot[i] != id) i = (i + 1) & mask;
         return i;
     }

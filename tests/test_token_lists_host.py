@@ -112,3 +112,31 @@ int main()
 }
 """)
     assert said == [f"1 sequence {s}: {n} kept of 50 new tokens" for s, n in ((1, -49), (0, -1), (1, -50), (1, 51))]
+
+
+def test_sets_of_ids_far_apart(tmp_path):
+    """Page ids that are multiples of a power of two, or any distance apart, lie few slots behind the first one that they look
+    at: linear probing of a set half full looks at 1.5 slots on average if ids fall on them by chance, and 16 are
+    allowed here (all on one slot, 2^15 ids look at 2^14 each)."""
+    said = run(tmp_path, "tokens_host.cuh", r"""
+int main()
+{
+    const int32_t n = 1 << 15;
+    for (int32_t step : {1, 3, 1 << 4, 1 << 9, 1 << 12, 1 << 16, (1 << 16) - 1, 10007}) {
+        mure::IdSet ids(n), empty(n);
+        bool ok = true;
+        int64_t probes = 0;
+        for (int32_t i = 0; i < n; ++i) ok = ids.insert((n - 1 - i) * step) && ok;
+        for (int32_t i = 0; i < n; ++i) {
+            ok = ok && ids.has(i * step) && !ids.insert(i * step) && (step == 1 || !ids.has(i * step + 1));
+            probes += 1 + ((ids.at(i * step) - empty.at(i * step)) & ids.mask);
+        }
+        printf("%d %d\n", ok, probes <= 16 * n);
+    }
+    mure::IdSet few(0);
+    const bool first = few.insert(INT32_MAX), again = few.insert(INT32_MAX);
+    printf("%d %d %d\n", first, again, few.has(0));
+    return 0;
+}
+""")
+    assert said == ["1 1"] * 8 + ["1 0 0"]
