@@ -319,18 +319,23 @@ __global__ void __launch_bounds__(kThreads, 4) k_tokens_rotate(RotateParams p)
                             for (int e = 0; e < N / 2; ++e) two = fma2(y[e], y[e], two);
                             const float sum = over_lanes(two);
                             float f = rsqrtf(fmaf(sum, over, p.r.eps));
-                            // squares that leave fp32's range: once more, of the values times a power of two
-                            const bool lost = on && !(sum >= 0x1p-80f && sum < INFINITY);
+                            // squares that leave fp32's range: once more, of the values times a power of two.  Small ones (below
+                            // an eps of 2^-100 they do not count) are multiplied by it and then by the root, large ones the other
+                            // way round: no step then leaves the range where the outcome does not, the least numbers' either
+                            const bool small = sum < 0x1p-80f, lost = on && (small ? p.r.eps < 0x1p-100f : !(sum < INFINITY));
                             if (__any_sync(0xffffffffu, lost)) {
-                                const float g = sum < 1.f ? 0x1p60f : 0x1p-70f;
+                                const float g = small ? 0x1p100f : 0x1p-70f;
                                 f32x2 again = 0;
 #pragma unroll
                                 for (int e = 0; e < N / 2; ++e) {
                                     const f32x2 z = mul2(y[e], pack2(g, g));
                                     again = fma2(z, z, again);
                                 }
-                                const float f2 = rsqrtf(fmaf(over_lanes(again), over, p.r.eps * g * g)) * g;
-                                if (lost) f = f2;
+                                const float root = rsqrtf(fmaf(over_lanes(again), over, p.r.eps * g * g));
+                                const float before = !lost ? 1.f : small ? g : root;
+#pragma unroll
+                                for (int e = 0; e < N / 2; ++e) y[e] = mul2(y[e], pack2(before, before));
+                                if (lost) f = small ? root : g;
                             }
 #pragma unroll
                             for (int e = 0; e < N / 2; ++e) y[e] = mul2(y[e], pack2(f, f));
