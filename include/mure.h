@@ -524,7 +524,8 @@ mure_status mure_tokens_attend(mure_tokens *tokens, mure_tokens_plan *plan, cons
  *   y = x w / sqrt(mean(x^2) + eps)                              where a weight w is given, else y = x;
  *   each pair (a, b) of y's first rot_dim values becomes (a cos u - b sin u, b cos u + a sin u), u = position * freq[i]
  * with the position of the token along the pair's axis; the values from rot_dim on stay.  All in fp32, rounded once to
- * the activations' type; angles are exact to 2^-32 of a turn at any 32-bit position. */
+ * the activations' type; angles are exact to 2^-32 of a turn at any 32-bit position, and their sines and cosines to some
+ * units of fp32's last place, small ones too. */
 enum { MURE_PAIRS_HALVES = 0, MURE_PAIRS_ADJACENT = 1 };  /* pair i: values i and i + rot_dim / 2, or 2 i and 2 i + 1 */
 
 typedef struct {

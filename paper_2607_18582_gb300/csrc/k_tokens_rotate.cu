@@ -5,7 +5,7 @@
 //
 // with u the position along the pair's axis times the pair's frequency.  The angle is held as a part of a turn in
 // 64-bit fixed point: the position times (frequency / 2 pi) 2^64, modulo 2^64, is exact to position 2^-64 turns, so
-// a token at position 2^30 is rotated as well as one at 5, and only the remainder goes to sine and cosine in fp32.
+// a token at position 2^30 is rotated as well as one at 5, and only the remainder goes to sine and cosine, in fp32 and what that leaves.
 // A row lies with a power-of-two group of a warp, 16 (or eight) values a thread: with pairs of halves half of them from either half, so
 // that a pair never leaves its thread, the row's sum of squares is a few shuffles away, and an e4m3 row is quantised in
 // the pass that rotated it.  A group takes a token and some or all of its heads: its sines and cosines, times the
@@ -120,13 +120,14 @@ struct Part {
     }
 };
 
-// Sine and cosine of t 2^-32 turns: quarter turns aside, the eighth of a turn that is left as an fp32 number, and what that
-// rounding leaves (below 2^-27 of a turn) by the first order.
-__device__ __forceinline__ void of_turn(uint32_t t, float &sine, float &cosine)
+// Sine and cosine of t 2^-64 turns: quarter turns aside, the eighth of a turn that is left as an fp32 multiple of 2^-32, and what
+// that leaves (below 2^-27 of a turn) by the first order.  The low half of t counts where the angle is small: its sine then has
+// fp32's relative bits as well.
+__device__ __forceinline__ void of_turn(uint64_t t, float &sine, float &cosine)
 {
-    const uint32_t q = (t + 0x20000000u) >> 30;
-    const int32_t r = (int32_t)(t - (q << 30));
-    const float near = (float)r, rest = (float)(r - (int32_t)near) * (3.14159265f * 0x1p-31f);
+    const uint32_t hi = (uint32_t)((t + 0x80000000ull) >> 32), q = (hi + 0x20000000u) >> 30;
+    const int32_t lo = (int32_t)(uint32_t)t, r = (int32_t)(hi - (q << 30));
+    const float near = (float)r, rest = fmaf((float)lo, 0x1p-32f, (float)(r - (int32_t)near)) * (3.14159265f * 0x1p-31f);
     float s, c;
     sincospif(near * 0x1p-31f, &s, &c);
     const float s1 = fmaf(c, rest, s), c1 = fmaf(-s, rest, c);
@@ -242,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_tokens_rotate(RotateParams p)
                 const int pos = p.r.positions ? __ldg(p.r.positions + __ldg(p.r.axis + k) * p.r.position_stride + token) : own;
                 const uint64_t turn = (uint64_t)(int64_t)pos * __ldg(p.r.turn + k);
                 float sine, cosine;
-                of_turn((uint32_t)((turn + 0x80000000ull) >> 32), sine, cosine);
+                of_turn(turn, sine, cosine);
                 sines[e][threadIdx.x] = cosine;
                 sines[N / 2 + e][threadIdx.x] = sine;
             }

@@ -1,12 +1,21 @@
-"""The norm and rotation at the ends of their ranges on the GPU: rows whose squares leave fp32.  Tolerances as in
-test_gpu_token_rotate.py."""
+"""The norm and rotation at the ends of their ranges on the GPU: rows whose squares leave fp32, and
+angles beside a quarter turn's multiples.  Tolerances as in test_gpu_token_rotate.py, but for the angles.
+
+There sine or cosine is small, and its relative error counts, e = 2^-24: the angle's fraction of a turn is right to 2 units
+of 2^-64 for each position; its nearest multiple of 2^-32 goes to sine and cosine (2 e), which what is left, at most half
+of that multiple or all there is, corrects to the first order: three roundings (its own, pi's and the
+product's) and one of the sum, in which at most half of the sine is cancelled: within 2 (2 + 3) + 1 = 11 e; the product with
+the value one more."""
+import math
+from fractions import Fraction
+
 import numpy as np
 import pytest
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
-from test_gpu_token_rotate import E, near  # noqa: E402
+from test_gpu_token_rotate import E, TWO_PI, near  # noqa: E402
 from test_gpu_tokens import M, TYPES, Batch, ctx  # noqa: E402,F401
 
 
@@ -59,3 +68,34 @@ def test_norms_of_values_far_apart(M, ctx):  # noqa: F811
     got, want = normed(M, ctx, x, "f32", 0.0)
     err = (got.double() - want).abs()
     assert bool((err <= 16 * E * want.abs() + 2.0 ** -149).all()), (err / want.abs()).nan_to_num(0).max()
+
+
+@pytest.mark.parametrize("layout", ["halves", "adjacent"])
+@pytest.mark.parametrize("quarters", [0, 1, 2, 3])
+@pytest.mark.parametrize("position", [1, -3, 1000, 2 ** 30])
+def test_angles_beside_quarter_turns(M, ctx, layout, quarters, position):  # noqa: F811
+    """A pair whose other value is 0 keeps fp32's relative bits however near its angle lies to a multiple of a quarter turn."""
+    d, half, e = 64, 32, 2.0 ** -24
+    # quarters of a turn at that position, and 2^-50 to 2^-3 radians of either sign beside them
+    beside = [(-1) ** i * 2.0 ** x * 1.3 for i, x in enumerate(np.linspace(-50, -3, half))]
+    freq = [float((TWO_PI * quarters / 4 + Fraction(b)) / position) for b in beside]
+    r = M.mure_rotary_create(ctx, d, d, layout=layout, freq=freq)
+    t = Batch(M, ctx, [2], [0], [2], 1, 1, d, 16, "f32", "same")
+    first = [i for i in range(half)] if layout == "halves" else [2 * i for i in range(half)]
+    second = [i + half for i in range(half)] if layout == "halves" else [2 * i + 1 for i in range(half)]
+    x = torch.zeros(2, 1, d, device="cuda")
+    x[0, 0, first], x[1, 0, second] = 1.5, 1.5
+    at = torch.full((1, 2), position, dtype=torch.int32, device="cuda")
+    got = M.mure_tokens_rotate(t.cache, t.plan, r, x, positions=at)[0].double().cpu()
+    M.mure_synchronize(ctx)
+    for i in range(half):
+        # what is left of the angle beside the nearest quarter turn, exactly
+        angle = position * Fraction(freq[i])
+        q = round(angle / TWO_PI * 4)
+        left = float(angle - q * TWO_PI / 4)
+        s, c = [(math.sin(left), math.cos(left)), (math.cos(left), -math.sin(left)),
+                (-math.sin(left), -math.cos(left)), (-math.cos(left), math.sin(left))][q % 4]
+        tol = 14 * e * 1.5 + 2.0 ** -64 * 2 * abs(position) * 2 * math.pi * 1.5 / min(abs(s), abs(c))       # of either one
+        for row, a, b in ((0, c, s), (1, -s, c)):
+            for j, v in ((first[i], a), (second[i], b)):
+                assert abs(float(got[row, 0, j]) - 1.5 * v) <= tol * abs(v) + 1e-45, (i, row, v, float(got[row, 0, j]) / (1.5 * v))
