@@ -1,5 +1,5 @@
-"""The norm and rotation at the ends of their ranges on the GPU: rows whose squares leave fp32, and
-angles beside a quarter turn's multiples.  Tolerances as in test_gpu_token_rotate.py, but for the angles.
+"""The norm and rotation at the ends of their ranges on the GPU: rows whose squares leave fp32,
+angles beside a quarter turn's multiples, and batches of more tiles than blocks that run at a time.  Tolerances as in test_gpu_token_rotate.py, but for the angles.
 
 There sine or cosine is small, and its relative error counts, e = 2^-24: the angle's fraction of a turn is right to 2 units
 of 2^-64 for each position; its nearest multiple of 2^-32 goes to sine and cosine (2 e), which what is left, at most half
@@ -15,7 +15,7 @@ import pytest
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
-from test_gpu_token_rotate import E, TWO_PI, near  # noqa: E402
+from test_gpu_token_rotate import E, TWO_PI, near, rotary, turned  # noqa: E402
 from test_gpu_tokens import M, TYPES, Batch, ctx  # noqa: E402,F401
 
 
@@ -99,3 +99,38 @@ def test_angles_beside_quarter_turns(M, ctx, layout, quarters, position):  # noq
         for row, a, b in ((0, c, s), (1, -s, c)):
             for j, v in ((first[i], a), (second[i], b)):
                 assert abs(float(got[row, 0, j]) - 1.5 * v) <= tol * abs(v) + 1e-45, (i, row, v, float(got[row, 0, j]) / (1.5 * v))
+
+
+@pytest.mark.parametrize("dtype,form", [("bf16", "e4m3"), ("f16", "same"), ("f32", "same")])
+@pytest.mark.parametrize("layout", ["halves", "adjacent"])
+def test_more_tiles_than_blocks(M, ctx, dtype, form, layout):  # noqa: F811
+    """Prompts in numbers: a block then takes all heads of its tile.  Rows are the formula's, those of a batch of a few of the
+    sequences, and what the two calls store."""
+    n, heads, hk, d, rot = 700, 12, 3, 64, 16
+    new, pos = [1 + 7 * b % 45 for b in range(n)], [3 * b % 50 for b in range(n)]
+    kv = [a + b for a, b in zip(new, pos)]
+    assert sum(-(-x // 16) for x in new) > 4 * 152
+    t = Batch(M, ctx, new, pos, kv, heads, hk, d, 16, dtype, form)
+    r, freq, axis, w = rotary(M, ctx, d, rot, layout, "qk")
+    q, k = M.mure_tokens_rotate(t.cache, t.plan, r, t.q, t.k)
+    M.mure_synchronize(ctx)
+    at = [[p + i for a, p in zip(new, pos) for i in range(a)]]
+    near(q, *turned(t.q, at, freq, axis, layout, w["q"], 1e-5), dtype)
+    near(k, *turned(t.k, at, freq, axis, layout, w["k"], 1e-5), dtype)
+    few = 9
+    rows = sum(new[:few])
+    plan = M.mure_tokens_plan(t.cache, heads, new[:few], pos[:few], kv[:few], t.table)
+    a, b = M.mure_tokens_rotate(t.cache, plan, r, t.q[:rows], t.k[:rows])
+    M.mure_synchronize(ctx)
+    assert torch.equal(a, q[:rows]) and torch.equal(b, k[:rows])
+    for p in t.pools:
+        p.view(torch.uint8).zero_()
+    M.mure_tokens_append(t.cache, t.plan, k, t.v)
+    want = [p.clone() for p in t.pools]
+    for p in t.pools:
+        p.view(torch.uint8).zero_()
+    got = M.mure_tokens_append_rotated(t.cache, t.plan, r, t.q, t.k, t.v)
+    M.mure_synchronize(ctx)
+    assert torch.equal(got, q)
+    for x, y in zip(t.pools, want):
+        assert bool(y.view(torch.uint8).any()) and torch.equal(x.view(torch.uint8), y.view(torch.uint8))
