@@ -323,8 +323,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_tokens_rotate(RotateParams p)
                             // squares that leave fp32's range: once more, of the values times a power of two.  Small ones (below
                             // an eps of 2^-100 they do not count) are multiplied by it and then by the root, large ones the other
                             // way round: no step then leaves the range where the outcome does not, the least numbers' either
-                            const bool small = sum < 0x1p-80f, lost = on && (small ? p.r.eps < 0x1p-100f : !(sum < INFINITY));
-                            if (__any_sync(0xffffffffu, lost)) {
+                            if (__any_sync(0xffffffffu, on && !(sum >= 0x1p-80f && sum < INFINITY))) {
+                                const bool small = sum < 0x1p-80f, lost = small ? p.r.eps < 0x1p-100f : !(sum < INFINITY);
                                 const float g = small ? 0x1p100f : 0x1p-70f;
                                 f32x2 again = 0;
 #pragma unroll
