@@ -24,7 +24,6 @@ struct PageParams {
     const char *from[4];                     // k, v, and their scales
     char *to[4];
     int64_t bytes[2];                        // of a page of codes or values, of its scales
-    int n;
     int32_t page[2 * N];
 };
 
@@ -65,7 +64,6 @@ void copy(const TokPool &from, const TokPool &to, int64_t bytes, int64_t scale_b
     p.to[0] = static_cast<char *>(to.k); p.to[1] = static_cast<char *>(to.v);
     p.to[2] = reinterpret_cast<char *>(to.ks); p.to[3] = reinterpret_cast<char *>(to.vs);
     p.bytes[0] = bytes; p.bytes[1] = scale_bytes;
-    p.n = n;
     memcpy(p.page, pages, (size_t)n * 2 * sizeof(int32_t));
     const int64_t z = (bytes / 16 + kThreads * kWords - 1) / (kThreads * kWords);
     k_tokens_copy<N><<<dim3(n, 2, (unsigned)(z < 1024 ? z : 1024)), kThreads, 0, s>>>(p);

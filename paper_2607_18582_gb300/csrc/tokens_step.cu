@@ -9,7 +9,7 @@ using namespace mure;
 
 struct mure_rotary {
     mure_ctx *ctx = nullptr;
-    int head_dim = 0, n_axes = 1;
+    int head_dim = 0;
     TokRotary r;
     void *mem = nullptr;
 };
@@ -84,7 +84,6 @@ mure_status mure_rotary_create(mure_ctx *c, const mure_rotary_desc *desc, mure_r
         auto r = std::make_unique<mure_rotary>();
         r->ctx = c;
         r->head_dim = D;
-        r->n_axes = d.n_axes;
         char *m = static_cast<char *>(dalloc(c, image.size()));
         // (a few KB from pageable memory: taken in when the call returns)
         const cudaError_t e = cudaMemcpyAsync(m, image.data(), image.size(), cudaMemcpyHostToDevice, c->stream);
