@@ -454,7 +454,7 @@ mure_status mure_tokens_buffers(const mure_tokens *tokens, mure_tokens_desc *out
  * form, n_pages), not that one alone.  mure_tokens_plan_set gives an existing plan a new
  * batch (the next step of the same sequences, say) and keeps its device memory; when it
  * fails the plan is left without a batch.  A batch whose tables take more than 1 MiB (some
- * 200,000 pages) is copied once the stream's earlier work is done: the call then waits for
+ * 200,000 pages, or eight trees of 1,024 tokens) is copied once the stream's earlier work is done: the call then waits for
  * it.  A plan holds its tables, room for partial sums
  * (so graphs that are captured from calls of one plan are replayed one after the other, as the stream has the calls)
  * and, for chunks on e4m3 cells, the pages they read widened to 16 bits (each page once
@@ -472,7 +472,8 @@ void mure_tokens_plan_free(mure_tokens_plan *plan);
  * i, or -1 for one that follows the earlier cells.  depth(i) is the number of its ancestors among the new tokens, its
  * position pos[b] + depth(i), and its cell, as for any batch, the one at pos[b] + i.  It attends to itself, to its
  * ancestors, and to the cells before pos[b], all within kv_len[b] and, where window > 0, by their positions as above.
- * A chain (parents i - 1) means what an ordinary batch does.  Every call takes such a plan.  Errors: as above;
+ * A chain (parents i - 1) means what an ordinary batch does.  A tree of n tokens adds 16 n + 4 n ceil(n / 32) bytes
+ * to the plan's tables.  Every call takes such a plan.  Errors: as above;
  * INVALID_ARG (NULL parents with new tokens, a parent that is not before its token), UNSUPPORTED (a tree of more than
  * MURE_TREE_MAX tokens). */
 enum { MURE_TREE_MAX = 1024 };
@@ -524,8 +525,8 @@ mure_status mure_tokens_attend(mure_tokens *tokens, mure_tokens_plan *plan, cons
  *   y = x w / sqrt(mean(x^2) + eps)                              where a weight w is given, else y = x;
  *   each pair (a, b) of y's first rot_dim values becomes (a cos u - b sin u, b cos u + a sin u), u = position * freq[i]
  * with the position of the token along the pair's axis; the values from rot_dim on stay.  All in fp32, rounded once to
- * the activations' type; angles are exact to 2^-32 of a turn at any 32-bit position, and their sines and cosines to some
- * units of fp32's last place, small ones too. */
+ * the activations' type; angles are exact to 2^-32 of a turn at any 32-bit position (at position p, to |p| 2^-63 turns), their
+ * sines and cosines, small ones too, to some units of fp32's last place beside that. */
 enum { MURE_PAIRS_HALVES = 0, MURE_PAIRS_ADJACENT = 1 };  /* pair i: values i and i + rot_dim / 2, or 2 i and 2 i + 1 */
 
 typedef struct {

@@ -41,7 +41,8 @@
 // to 64 tokens over 500 to 6,000 cells of 8 heads of 128, 345 us so (191 of them the widening), 189 us by the pieces
 // themselves.  What bounds these is the chain from a tile of codes to the products (2.75 us per tile of 256 rows; the same
 // with the codes copied as they are, 2.4 us without touching them), not the conversions.  Trees of 200 to 256 rows over
-// 100,000 to 131,000 cells of 16 bits: 192 to 205 us, 5.0 TB/s, 1.75 us per tile as in any chunk.
+// 100,000 to 131,000 cells of 16 bits: 187 to 202 us and 8 to 12 for the join, 201 to 221 both (one card and another), 4.4 to 4.9
+// TB/s, 1.75 us per tile as in any chunk.
 #include <type_traits>
 
 #include "simt_tile.cuh"

@@ -15,10 +15,11 @@
 // a cell store the same bits.
 //
 // Measured (GB300): 57,000 tokens of 32 and 8 heads of 128 bf16 values, normed and rotated, keys and values into e4m3 cells:
-// 216 us, 5.9 TB/s of what it has to move; 168 million warp instructions, issue slots 65 % busy at 3.8 warps per scheduler.
-// 28,000 tokens of 16 heads of 80 f16 values, neighbouring pairs, positions along three axes, no norm: 60 us, 4.8 TB/s:
+// 216 to 220 us, 5.9 TB/s of what it has to move, issue slots 62 % busy at 3.8 warps per scheduler.
+// 28,000 tokens of 16 heads of 80 f16 values, neighbouring pairs, positions along three axes, no norm: 61 us, 4.7 TB/s:
 // latency and issue, a group has one token and five of its eight lanes a part of the row.  (Groups of as many lanes as a row
-// needs: as fast, but 216 -> 236 us with the sums over five lanes; eight values a thread 364 and 82 us.)
+// needs: as fast, but 216 -> 236 us with the sums over five lanes; eight values a thread 364 and 82 us.)  What small
+// angles and rows of subnormal numbers cost is in these figures: 218 -> 220 us on one card.
 #include <type_traits>
 
 #include "simt_tile.cuh"

@@ -24,7 +24,7 @@ namespace {
 // widened first, 128 values, 64 rows 126 / 137, 128 rows 225 / 138, 64 values 90 / 92 and 164 / 93.
 // (Measured at that one shape.  fp32 rows, and heads of more than 128 values, have no other kernel.)
 int few_rows_up_to(bool codes, int d) { return codes ? 64 : d <= 64 ? 32 : 16; }
-// Trees, whose pieces widen codes themselves (48 sequences of 4,000 cells, 8 heads; few / the others, us): codes of 128
+// Trees, whose pieces widen codes themselves (48 sequences of 4,000 cells, 8 heads, no other shape; few / the others, us): codes of 128
 // values, 24 rows 177 / 200, 32 177 / 201, 48 248 / 202, of 64 values, 32 128 / 193, 48 182 / 193, 64 236 / 193; cells as they are, of
 // 128 values, 16 rows 144 / 154, 24 163 / 155, of 64 values, 32 95 / 115, 48 124 / 112.
 int few_tree_rows_up_to(bool codes, int d) { return codes && d % 16 == 0 ? (d <= 64 ? 48 : 32) : few_rows_up_to(codes, d); }
@@ -338,7 +338,10 @@ void set_plan(mure_tokens_plan *p, const mure_tokens_batch *bp, bool tree = fals
         FAILIF(rows > kMostPos, c, MURE_ERR_UNSUPPORTED, "sequence %d: more than 2^30 rows", s);
         // (a batch of trees on cells as they are goes to one kernel whole: 64 trees of 3 to 40 tokens within a window, of which 18
         // have few rows, 45 us in two launches one after the other, 41 in one; the kernel for few rows is little faster
-        // on those even by itself, but on codes twice as fast)
+        // on those even by itself, but on codes twice as fast.  One tree of more than kTreeRows rows takes the others along to the
+        // two-tile kernel.  63 small ones alone, one of 134 rows over 2,000 cells alone, all in one plan, in two plans, us: 4 to 30 tokens, 32 heads on 8 of
+        // 128 values, 154, 31, 170, 185; single tokens of these 150, 31, 168, 180; 3 to 40 tokens within a window, 15 heads
+        // on 5 of 64, 43, 27, 55, 71; but single tokens of 8 heads on 8 of 64 84, 29, 127, 113)
         const int up_to = tree ? few_tree_rows_up_to(wide, d.head_dim) : few_rows_up_to(wide, d.head_dim);
         const bool as_chunk = d.dtype != MURE_F32 && d.head_dim <= kChunkDim && (tree && !wide ? most_rows : rows) > up_to;
         const bool as_tree = as_chunk && tree && !wide && most_rows <= kTreeRows;
